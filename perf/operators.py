@@ -1,0 +1,580 @@
+"""The serving operators around an E4M3 KV cache, at the sizes they are called with.
+
+Operators: ``rope`` (rotary positions), ``cache_append`` (rotation, quantisation and
+the write into the pages), ``cache_fwd`` (attention over the cache), ``cache_weights``
+(attention weight each cached token has received) and ``cache_evict`` (the tokens
+with the most of it move into new pages).
+
+The cache: ``k``, ``v`` E4M3 codes [pages][Hkv][page][d], ``k_scale``, ``v_scale``
+bytes [pages][Hkv]; a code stands for code * 2^(byte - 127).  Sequence b holds
+``lens[b]`` tokens, the new ones among them, in the pages ``table[b]``.  Tokens of a
+call are packed [T][heads][d], those of sequence b from ``cu[b]`` on.
+
+Fields of a case: op, B sequences, Hq, Hkv heads, n the longest cache, nq the most new
+tokens of a sequence, d, page, ragged (lengths and token counts differ), kind (element
+type of the inputs), rot and layout (rotary), budget (evict).
+"""
+import math
+
+import torch
+
+own = False
+
+LOG2E = 1.4426950408889634
+N_SINK = 4
+N_RECENT = 32
+E4M3 = torch.float8_e4m3fn
+KINDS = {"bf16": torch.bfloat16, "fp16": torch.float16, "fp32": torch.float32, "e4m3": E4M3}
+
+
+def _case(name, op, B, Hq, Hkv, n, nq, d, page, *, ragged=False, kind="bf16", rot=0, layout="half", budget=0):
+    c = dict(op=op, B=B, Hq=Hq, Hkv=Hkv, n=n, nq=nq, d=d, page=page, ragged=ragged, kind=kind, rot=rot,
+             layout=layout, budget=budget)
+    return dict(name=name, **c) if name else c
+
+
+def listed():
+    return [
+        # the query heads of one decode step of a batch of 16
+        _case("rope_t16_h32_d128", "rope", 16, 32, 8, 8192, 1, 128, 128, rot=128),
+        # the query heads of a prefill of 8192 tokens, half of each head rotated, pairs side by side
+        _case("rope_t8192_h32_d128_part", "rope", 1, 32, 8, 8192, 8192, 128, 128, rot=64, layout="interleaved"),
+        # the write of a decode step: one token of each of 16 requests, q rotated along
+        _case("append_decode_b16_h32kv8_d128", "append", 16, 32, 8, 8192, 1, 128, 128, ragged=True, rot=128),
+        # the write of a chunk of a chunked prefill: up to 2048 tokens of each of 4 prompts
+        _case("append_chunk_b4_q2048_h32kv8_d128", "append", 4, 32, 8, 8192, 2048, 128, 128, ragged=True, rot=128),
+        # a few short requests, small heads and pages: what a call costs at the least
+        _case("fwd_decode_b4_h8kv2_n777_d64", "fwd", 4, 8, 2, 777, 1, 64, 64, ragged=True),
+        # decode of a batch: one query per request against its cache
+        _case("fwd_decode_b16_h32kv8_n8192_d128", "fwd", 16, 32, 8, 8192, 1, 128, 128),
+        # decode of one long-context request, E4M3 queries, length not a multiple of the page
+        _case("fwd_decode_b1_h32kv8_n131001_d128", "fwd", 1, 32, 8, 131001, 1, 128, 128, kind="e4m3"),
+        # the last chunk of a long prompt: 2048 queries against a 16k cache; the largest call
+        _case("fwd_chunk_b1_q2048_h32kv8_n16384_d128", "fwd", 1, 32, 8, 16384, 2048, 128, 128),
+        # the weights of a decode step's attention
+        _case("weights_decode_b16_h32kv8_n8192_d128", "weights", 16, 32, 8, 8192, 1, 128, 128),
+        # the weights of a chunk, ragged
+        _case("weights_chunk_b2_q256_h32kv8_n8192_d128", "weights", 2, 32, 8, 8192, 256, 128, 128, ragged=True),
+        # one request's cache cut to a quarter
+        _case("evict_b1_h8_n4096_d128", "evict", 1, 8, 8, 4096, 1, 128, 128, budget=1024),
+        # the same for a batch of long ones of different lengths
+        _case("evict_b16_h8_n8192_d128", "evict", 16, 32, 8, 8192, 1, 128, 128, ragged=True, budget=2048),
+    ]
+
+
+def _log(rng, lo, hi):
+    return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+
+
+def draw(rng):
+    """One more call of the listed kinds."""
+    op = rng.choice(["rope", "append", "append", "fwd", "fwd", "fwd", "weights", "weights", "evict"])
+    d, page = rng.choice([64, 128, 128]), rng.choice([64, 128, 128])
+    hkv = rng.choice([1, 2, 4, 8])
+    hq = hkv * rng.choice([1, 2, 4, 8])
+    ragged = rng.random() < 0.6
+    rot = rng.choice([d, d, d // 2, d // 4])
+    layout = rng.choice(["half", "interleaved"])
+    kind = rng.choice(["bf16", "bf16", "fp16", "fp32"])
+    if op == "rope":
+        nq = _log(rng, 1, 8192)
+        B = _log(rng, 1, max(1, min(64, 8192 // nq)))
+        return _case(None, op, B, min(hq, 32), hkv, max(nq, 8192), nq, d, page, kind=kind, rot=rot, layout=layout)
+    if op == "append":
+        nq = rng.choice([1, 1, 2, _log(rng, 3, 2048)])
+        B = _log(rng, 1, max(1, min(64, 8192 // nq)))
+        n = nq + _log(rng, 1, 8192)
+        return _case(None, op, B, min(hq, 32), hkv, n, nq, d, page, ragged=ragged, kind=kind, rot=rot, layout=layout)
+    if op == "evict":
+        n = _log(rng, 256, 16384)
+        B = _log(rng, 1, max(1, min(32, 131072 // n)))
+        return _case(None, op, B, hq, hkv, n, 1, d, page, ragged=ragged, budget=min(n - 1, max(64, _log(rng, n // 16, n))))
+    nq = rng.choice([1, 1, 1, 2, 5, _log(rng, 8, 1024)])
+    n = nq + _log(rng, 1, 131072 if nq < 8 else 16384)
+    B = max(1, min(_log(rng, 1, 64), int(1.6e6 / (hkv * n)), int((5e8 if op == "fwd" else 1e8) / (hq * nq * n))))
+    return _case(None, op, B, hq, hkv, n, nq, d, page, ragged=ragged, kind=rng.choice(["bf16", "bf16", "e4m3"]))
+
+
+# ---- inputs ----
+
+def _lengths(case):
+    """(lens, new tokens) of the sequences: the first is the longest, the others spread below it."""
+    B, n, nq = case["B"], case["n"], case["nq"]
+    if not case["ragged"]:
+        return [n] * B, [nq] * B
+    lens = [max(1, n - (n * 7 * i // (8 * B)) - 13 * i % 29) for i in range(B)]
+    new = [max(1, min(lens[i], nq - (nq * i // (2 * B)) - (i % 3 if nq > 8 else 0))) for i in range(B)]
+    return lens, new
+
+
+def _quantise(x):
+    """[..., page, d] in 32 bits -> E4M3 codes and bytes, one scale per block."""
+    f, t = torch.frexp(x.abs().amax((-2, -1)))
+    e = (t - 9 + (f > 0.875).int()).clamp_(min=-127)
+    return (x * torch.exp2(-e.float())[..., None, None]).to(E4M3), (e + 127).to(torch.uint8)
+
+
+def _make_table(n_pos, rot, device):
+    """cos and sin of position * 10000^(-2i / rot), in 64 bits, rounded once."""
+    i = torch.arange(rot // 2, dtype=torch.float64, device=device)
+    ang = torch.arange(n_pos, dtype=torch.float64, device=device)[:, None] * 10000.0 ** (-2 * i / rot)
+    return torch.stack((torch.cos(ang), torch.sin(ang)), -1).float().contiguous()
+
+
+def prepare(case, seed):
+    dev = torch.device("cuda")
+    g = torch.Generator(device=dev)
+    g.manual_seed(int(seed))
+    op, B, Hq, Hkv, d, page = (case[x] for x in ("op", "B", "Hq", "Hkv", "d", "page"))
+    lens, new = _lengths(case)
+    T = sum(new)
+    cu = [0]
+    for x in new:
+        cu.append(cu[-1] + x)
+    st = dict(op=op, page=page, max_q=max(new), layout=case["layout"], d=d,
+              lens=torch.tensor(lens, dtype=torch.int32, device=dev),
+              cu=torch.tensor(cu, dtype=torch.int32, device=dev) if case["ragged"] else None)
+    pos = [lens[b] - new[b] + i for b in range(B) for i in range(new[b])]
+    st["pos"] = torch.tensor(pos, dtype=torch.int32, device=dev)
+
+    def normal(*shape):
+        return torch.randn(shape, generator=g, device=dev)
+
+    kind = KINDS[case["kind"]]
+    if op in ("rope", "append"):
+        # the heads as they leave the projection: one row of q, k and v heads per token
+        qkv = normal(T, Hq + 2 * Hkv, d).to(kind)
+        st["q"], st["k"], st["v"] = qkv[:, :Hq], qkv[:, Hq:Hq + Hkv], qkv[:, Hq + Hkv:]
+        st["table"] = _make_table(max(lens), case["rot"], dev)
+        if op == "rope":
+            return st
+    # the cache: keys and values of a size that differs from block to block; four sink keys
+    # lifted by 7 (the last channel of the queries is 1)
+    W = max(-(-x // page) for x in lens)
+    used = [-(-x // page) for x in lens]
+    total = sum(used)
+    k = normal(total, Hkv, page, d) * torch.exp2(normal(total, Hkv, 1, 1) * 0.5)
+    v = normal(total, Hkv, page, d) * torch.exp2(normal(total, Hkv, 1, 1))
+    start = torch.tensor([sum(used[:b]) for b in range(B)], device=dev)
+    k[..., d - 1] = 0.0
+    k[start, :, :N_SINK, d - 1] = 7.0 * math.sqrt(d)
+    spare = 3
+    perm = torch.randperm(total + spare, generator=g, device=dev)
+    # (the spare pages and the keys behind a sequence's end hold what an earlier one left)
+    kc = torch.empty((total + spare, Hkv, page, d), dtype=E4M3, device=dev)
+    vc, ks, vs = torch.empty_like(kc), torch.empty((total + spare, Hkv), dtype=torch.uint8, device=dev), None
+    vs = torch.empty_like(ks)
+    for c, s, x in ((kc, ks, k), (vc, vs, v)):
+        code, byte = _quantise(x)
+        c.view(torch.uint8)[perm[:total]] = code.view(torch.uint8)
+        c.view(torch.uint8)[perm[total:]] = 0x35
+        s[perm[:total]], s[perm[total:]] = byte, 127
+    table = torch.full((B, W), -1, dtype=torch.int32)
+    at, ids = 0, perm.cpu().int()
+    for b in range(B):
+        table[b, :used[b]] = ids[at:at + used[b]]
+        at += used[b]
+    st["pages"] = table.to(dev)
+    st["cache"] = (kc, vc, ks, vs)
+    if op in ("fwd", "weights"):
+        q = normal(T, Hq, d)
+        q[..., d - 1] = 1.0
+        st["q"] = q.clamp_(-8, 8).to(kind)
+    if op == "weights":
+        st["lse"] = _plain_fwd(st, want_out=False)[1]
+        st["w"] = torch.rand((B, Hkv, W * page), generator=g, device=dev)
+    if op == "evict":
+        # sums over many steps: most tokens little, a few much; equal ones among them
+        w = torch.exp2(torch.round(normal(B, Hkv, W * page) * 64) / 16)
+        st["w"] = w
+        nb = -(-case["budget"] // page)
+        st["budget"] = case["budget"]
+        # the new pages: of a part of the pool that no sequence uses
+        st["new_cache"] = tuple(torch.zeros((B * nb, *x.shape[1:]), dtype=x.dtype, device=dev) for x in (kc, vc, ks, vs))
+        st["new_pages"] = torch.randperm(B * nb, generator=g, device=dev).int().view(B, nb)
+    return st
+
+
+# ---- the plain forms ----
+
+def _e4m3_64(y):
+    """64-bit values to the nearest E4M3 value, ties to even, saturating at 448."""
+    _, e = torch.frexp(y)
+    step = torch.exp2(((e - 1).clamp_(min=-6) - 3).double())
+    return (torch.round(y / step) * step).clamp_(-448.0, 448.0)
+
+
+def _rotated(x, table, pos, layout):
+    """x [T][H][d] of a 32- or 64-bit type, the first rot channels rotated."""
+    cs = table[pos.long()].to(x.dtype)[:, None]
+    c, s = cs[..., 0], cs[..., 1]
+    h = table.shape[1]
+    r = x[..., :2 * h]
+    a, b = (r[..., :h], r[..., h:]) if layout == "half" else (r[..., 0::2], r[..., 1::2])
+    p, q = a * c - b * s, b * c + a * s
+    r = torch.cat((p, q), -1) if layout == "half" else torch.stack((p, q), -1).flatten(-2)
+    return torch.cat((r, x[..., 2 * h:]), -1)
+
+
+def _counts(st):
+    """(first new token, new tokens) of each sequence, on the GPU."""
+    B = st["lens"].numel()
+    if st["cu"] is None:
+        return torch.arange(B, device=st["lens"].device) * st["max_q"], torch.full_like(st["lens"], st["max_q"]).long()
+    return st["cu"][:-1].long(), (st["cu"][1:] - st["cu"][:-1]).long()
+
+
+def _plain_append(st):
+    kc, vc, ks, vs = st["cache"]
+    page, dev = st["page"], kc.device
+    B, W = st["pages"].shape
+    first, new = _counts(st)
+    lens = st["lens"].long()
+    old = lens - new
+    # the blocks that get tokens: up to `most` of each sequence, from the one that holds the first
+    most = (st["max_q"] + page - 2) // page + 1
+    blk = old[:, None] // page + torch.arange(most, device=dev)
+    touched = blk * page < lens[:, None]
+    pid = st["pages"].long().gather(1, blk.clamp(max=W - 1))
+    slot = blk[..., None] * page + torch.arange(page, device=dev)                     # [B][most][page]
+    is_old = slot < old[:, None, None]
+    is_new = ~is_old & (slot < lens[:, None, None])
+    tok = (slot - old[:, None, None] + first[:, None, None]).clamp(0, st["k"].shape[0] - 1)
+    sel = touched.flatten()
+    pid, tok, is_old, is_new = pid.flatten()[sel], tok.flatten(0, 1)[sel], is_old.flatten(0, 1)[sel], is_new.flatten(0, 1)[sel]
+    any_old = is_old.any(-1)[:, None]
+    for c, s, x, rotate in ((kc, ks, st["k"], True), (vc, vs, st["v"], False)):
+        y = x.double()
+        if rotate:
+            y = _rotated(y, st["table"], st["pos"], st["layout"])
+        y = y[tok].transpose(1, 2)                                                    # [blocks][Hkv][page][d]
+        y = torch.where(is_new[:, None, :, None], y, 0.0)
+        f, t = torch.frexp(y.abs().amax((-2, -1)))
+        e = (t - 9 + (f > 0.875).int()).clamp_(min=-127)
+        was = s[pid].int() - 127
+        e = torch.where(any_old, torch.maximum(e, was), e)
+        here = c[pid].double() * torch.exp2(was.double())[..., None, None]
+        y = torch.where(is_old[:, None, :, None], here, y)
+        code = _e4m3_64(y * torch.exp2(-e.double())[..., None, None]).float().to(E4M3)
+        keep = (is_old | is_new)[:, None, :, None]
+        c.view(torch.uint8)[pid] = torch.where(keep, code.view(torch.uint8), c.view(torch.uint8)[pid])
+        s[pid] = (e + 127).to(torch.uint8)
+    q = _rotated(st["q"].float(), st["table"], st["pos"], st["layout"]).to(st["q"].dtype)
+    return dict(k=kc, v=vc, k_scale=ks, v_scale=vs, q=q)
+
+
+def _gathered(st, code, byte):
+    """[B][Hkv][W * page][d] in 32 bits: a sequence's blocks side by side."""
+    pid = st["pages"].clamp(min=0).long()
+    x = code[pid].float() * torch.exp2(byte[pid].float() - 127.0)[..., None, None]
+    B, W, Hkv, page, d = x.shape
+    return x.transpose(1, 2).reshape(B, Hkv, W * page, d)
+
+
+def _scores(st):
+    """Scores in units of log2 [B][Hkv][max_q][G][keys], -inf where a query does not see a key, and each
+    query's row in the packed tokens."""
+    kc, _, ks, _ = st["cache"]
+    first, new = _counts(st)
+    T, Hq, d = st["q"].shape
+    Hkv = kc.shape[1]
+    i = torch.arange(st["max_q"], device=kc.device)
+    row = (first[:, None] + i).clamp(max=T - 1)
+    q = st["q"].float()[row].view(*row.shape, Hkv, Hq // Hkv, d).permute(0, 2, 1, 3, 4)
+    k = _gathered(st, kc, ks)
+    B, _, n, _ = k.shape
+    x = torch.matmul(q.reshape(B, Hkv, -1, d), k.transpose(2, 3)).view(B, Hkv, st["max_q"], Hq // Hkv, n)
+    x *= LOG2E / math.sqrt(d)
+    lens = st["lens"].long()
+    last = (lens - new)[:, None] + i
+    last = torch.where(i < new[:, None], last, -1)
+    x.masked_fill_((torch.arange(n, device=k.device) > last[..., None])[:, None, :, None], -math.inf)
+    return x, row, i < new[:, None]
+
+
+def _packed(y, row, valid, T):
+    """[B][Hkv][max_q][G]... -> [T][Hq]..."""
+    y = y.transpose(1, 2).flatten(2, 3)
+    return y[valid]
+
+
+def _plain_fwd(st, want_out=True):
+    x, row, valid = _scores(st)
+    T = st["q"].shape[0]
+    top = x.amax(-1, keepdim=True)
+    m = torch.ceil(torch.where(top == -math.inf, 0.0, top))
+    if not want_out:
+        ell = torch.exp2(x.sub_(m)).sum(-1)
+        return None, _packed((m[..., 0] + torch.log2(ell)) * math.log(2.0), row, valid, T).contiguous()
+    _, vc, _, vs = st["cache"]
+    B, Hkv, nq, G, n = x.shape
+    x = x.view(B, Hkv, nq, G, n // 32, 32)
+    mg = torch.ceil(x.amax(-1, keepdim=True))
+    mg = torch.where(mg == -math.inf, m[..., None], mg)
+    p = torch.exp2(x.sub_(mg))
+    lift = torch.exp2(mg - m[..., None])
+    ell = (p.sum(-1, keepdim=True) * lift).sum((-2, -1))
+    p = p.mul_(256.0).to(E4M3).float().mul_(lift)
+    o = torch.matmul(p.view(B, Hkv, nq * G, n), _gathered(st, vc, vs)).view(B, Hkv, nq, G, -1)
+    o = o / (256.0 * ell)[..., None]
+    lse = (m[..., 0] + torch.log2(ell)) * math.log(2.0)
+    return _packed(o, row, valid, T).to(torch.bfloat16), _packed(lse, row, valid, T).contiguous()
+
+
+def _plain_weights(st):
+    x, row, valid = _scores(st)
+    B, Hkv, nq, G, n = x.shape
+    lse = st["lse"][row].view(B, nq, Hkv, G).transpose(1, 2) * LOG2E
+    x = torch.where(valid[:, None, :, None, None], x.sub_(lse[..., None]), -math.inf)
+    return st["w"].add_(torch.exp2(x).sum((2, 3)))
+
+
+def _plain_evict(st):
+    kc, vc, ks, vs = st["cache"]
+    nk, nv, nks, nvs = st["new_cache"]
+    page, budget, dev = st["page"], st["budget"], kc.device
+    w = st["w"]
+    B, Hkv, n = w.shape
+    lens = st["lens"].long()[:, None, None]
+    t = torch.arange(n, device=dev)
+    new_len = lens.clamp(max=budget)
+    always = (t < N_SINK) | (t >= lens - N_RECENT)
+    rank = torch.where(always, math.inf, w)
+    rank = torch.where(t < lens, rank, -1.0)
+    # the budget's first in descending order, equal ones by their place
+    order = torch.sort(rank, dim=-1, descending=True, stable=True).indices[..., :budget]
+    order = torch.where(torch.arange(order.shape[-1], device=dev) < new_len, order, n)
+    kept = torch.sort(order, dim=-1).values
+    if kept.shape[-1] < budget:
+        kept = torch.nn.functional.pad(kept, (0, budget - kept.shape[-1]), value=n)
+    there = kept < n
+    src = kept.clamp(max=n - 1)
+    new_w = torch.where(there, w.gather(-1, src), 0.0)
+    pid = st["pages"].long().clamp(min=0)[:, None].expand(B, Hkv, -1).gather(-1, src // page)
+    nb = st["new_pages"].shape[1]
+    pad = nb * page - budget
+    dst = st["new_pages"].long()
+    h = torch.arange(Hkv, device=dev)[None, :, None]
+    ok = torch.nn.functional.pad(there, (0, pad)).view(B, Hkv, nb, page)
+    for c, s, nc, ns in ((kc, ks, nk, nks), (vc, vs, nv, nvs)):
+        y = c[pid, h, src % page].float() * torch.exp2(s[pid, h].float() - 127.0)[..., None]
+        y = torch.nn.functional.pad(torch.where(there[..., None], y, 0.0), (0, 0, 0, pad)).view(B, Hkv, nb, page, -1)
+        f, tt = torch.frexp(y.abs().amax((-2, -1)))
+        e = (tt - 9 + (f > 0.875).int()).clamp_(min=-127)
+        code = (y * torch.exp2(-e.float())[..., None, None]).to(E4M3).view(torch.uint8).transpose(1, 2)
+        full = ok.any(-1).transpose(1, 2)
+        nc.view(torch.uint8)[dst] = torch.where(ok.transpose(1, 2)[..., None], code, nc.view(torch.uint8)[dst])
+        ns[dst] = torch.where(full, (e + 127).to(torch.uint8).transpose(1, 2), ns[dst])
+    kept = torch.where(there, kept, -1).int()
+    return dict(kept=kept, lens=new_len.view(-1).int(), w=new_w, k=nk, v=nv, k_scale=nks, v_scale=nvs)
+
+
+def run(state):
+    st = state
+    op = st["op"]
+    if own:
+        from paper_2606_06521_amd import attn_fp8 as A
+        if op == "rope":
+            return A.rope(st["q"], st["table"], st["pos"], layout=st["layout"])
+        cache = A.KVCache(*st["cache"])
+        if op == "append":
+            q = A.cache_append(cache, st["k"], st["v"], st["pages"], st["lens"], cu=st["cu"], max_q=st["max_q"],
+                               table=st["table"], positions=st["pos"], layout=st["layout"], q=st["q"])
+            return dict(k=cache.k, v=cache.v, k_scale=cache.k_scale, v_scale=cache.v_scale, q=q)
+        if op == "fwd":
+            return A.cache_fwd(st["q"], cache, st["pages"], st["lens"], cu=st["cu"], max_q=st["max_q"])
+        if op == "weights":
+            return A.cache_weights(st["q"], st["lse"], cache, st["pages"], st["lens"], st["w"], cu=st["cu"],
+                                   max_q=st["max_q"])
+        new = A.KVCache(*st["new_cache"])
+        kept, lens, w = A.cache_evict(cache, st["pages"], st["lens"], st["w"], new, st["new_pages"], st["budget"],
+                                      n_sink=N_SINK, n_recent=N_RECENT)
+        return dict(kept=kept, lens=lens, w=w, k=new.k, v=new.v, k_scale=new.k_scale, v_scale=new.v_scale)
+    if op == "rope":
+        return _rotated(st["q"].float(), st["table"], st["pos"], st["layout"]).to(st["q"].dtype)
+    if op == "append":
+        return _plain_append(st)
+    if op == "fwd":
+        return _plain_fwd(st)
+    if op == "weights":
+        return _plain_weights(st)
+    return _plain_evict(st)
+
+
+# ---- what a pass cannot do without ----
+
+def _pairs(case):
+    """(visible keys summed over the query tokens, cached tokens)."""
+    lens, new = _lengths(case)
+    return sum(n * (m - n) + n * (n + 1) // 2 for m, n in zip(lens, new)), sum(lens)
+
+
+def work(case):
+    op, Hq, Hkv, d, page = (case[x] for x in ("op", "Hq", "Hkv", "d", "page"))
+    lens, new = _lengths(case)
+    T = sum(new)
+    pairs, keys = _pairs(case)
+    e = KINDS[case["kind"]].itemsize
+    blocks = sum(-(-x // page) for x in lens)
+    if op == "rope":
+        return {"bytes": 2 * T * Hq * d * e + T * (case["rot"] * 4 + 4), "flops": 3.0 * T * Hq * case["rot"]}
+    if op == "append":
+        touched = sum((x - 1) // page - (x - y) // page + 1 for x, y in zip(lens, new))
+        return {"bytes": 2 * T * Hq * d * e + 2 * T * Hkv * d * (e + 1) + T * (case["rot"] * 4 + 4) + 4 * touched * Hkv,
+                "flops": 3.0 * T * (Hq + Hkv) * case["rot"] + 4.0 * T * Hkv * d}
+    if op == "fwd":
+        return {"bytes": keys * Hkv * 2 * d + 2 * blocks * Hkv + T * Hq * (d * (e + 2) + 4), "flops": 4.0 * d * Hq * pairs}
+    if op == "weights":
+        return {"bytes": keys * Hkv * (d + 8) + blocks * Hkv + T * Hq * (d * e + 4), "flops": 2.0 * d * Hq * pairs}
+    moved = sum(min(x, case["budget"]) for x in lens)
+    return {"bytes": 4 * keys * Hkv + moved * Hkv * (4 * d + 8) + 2 * blocks * Hkv, "flops": 2.0 * moved * Hkv * d}
+
+
+# ---- the same in 64 bits ----
+
+def _unit(b):
+    """2^(byte - 127) in 64 bits."""
+    return torch.ldexp(torch.ones((), dtype=torch.float64, device=b.device), b.int() - 127)
+
+
+def _turn(x, cs, layout):
+    """One head's channels as complex numbers times cos + i sin."""
+    h = cs.shape[-2]
+    z = torch.view_as_complex(cs.double().contiguous())
+    y = x.double().clone()
+    at = (slice(0, h), slice(h, 2 * h)) if layout == "half" else (slice(0, 2 * h, 2), slice(1, 2 * h, 2))
+    r = torch.complex(y[..., at[0]], y[..., at[1]]) * z[:, None]
+    y[..., at[0]], y[..., at[1]] = r.real, r.imag
+    return y
+
+
+def _block(y):
+    """Codes (as values) and byte of one block of true values [Hkv][tokens][d]."""
+    top = y.abs().flatten(1).amax(1)
+    e = torch.where(top > 0, torch.ceil(torch.log2(top / 448.0)), -127.0)
+    # (log2 next to an integer may be off by one either way)
+    e = torch.where(top > 448.0 * torch.exp2(e), e + 1, e)
+    e = torch.where(top <= 448.0 * torch.exp2(e - 1), e - 1, e).clamp(min=-127)
+    return e
+
+
+def _codes(y, e):
+    z = y * torch.exp2(-e)[:, None, None]
+    quantum = torch.exp2(torch.floor(torch.log2(z.abs().clamp(min=2.0 ** -6))).clamp(min=-6) - 3)
+    return (torch.round(z / quantum) * quantum).clamp(-448, 448)
+
+
+def _exact_append(st, new):
+    kc, vc, ks, vs = st["cache"]
+    page, at = st["page"], 0
+    out = {}
+    cs = st["table"][st["pos"].long()]
+    rk = _turn(st["k"], cs, st["layout"])
+    kinds = (("k", "k_scale", kc, ks, rk), ("v", "v_scale", vc, vs, st["v"].double()))
+    for name, sname, c, s, _ in kinds:
+        out[name], out[sname] = c.clone(), s.clone()
+    for b, length in enumerate(st["lens"].tolist()):
+        old = length - new[b]
+        for j in range(old // page, (length - 1) // page + 1):
+            p = int(st["pages"][b, j])
+            a, z = max(old, j * page), min(length, (j + 1) * page)
+            for name, sname, c, s, y in kinds:
+                t = y[at + a - old:at + z - old].transpose(0, 1)
+                e = _block(t)
+                o = a - j * page
+                if o:
+                    was = s[p].double() - 127
+                    e = torch.maximum(e, was)
+                    t = torch.cat((c[p, :, :o].double() * torch.exp2(was)[:, None, None], t), 1)
+                out[name][p, :, :z - j * page] = _codes(t, e).float().to(E4M3)
+                out[sname][p] = (e + 127).to(torch.uint8)
+        at += new[b]
+    out["q"] = _turn(st["q"], cs, st["layout"])
+    return out
+
+
+def _exact_rows(st, new, want_out, want_w):
+    """Attention by sequence, KV head and run of queries."""
+    kc, vc, ks, vs = st["cache"]
+    T, Hq, d = st["q"].shape
+    Hkv, dev = kc.shape[1], kc.device
+    G = Hq // Hkv
+    out = torch.zeros((T, Hq, d), dtype=torch.float64, device=dev) if want_out else None
+    lse = torch.full((T, Hq), -math.inf, dtype=torch.float64, device=dev)
+    w = st["w"].double() if want_w else None
+    at = 0
+    for b, n in enumerate(st["lens"].tolist()):
+        pid = st["pages"][b, :-(-n // st["page"])].long()
+        for h in range(Hkv):
+            k = (kc[pid, h].double() * _unit(ks[pid, h])[:, None, None]).flatten(0, 1)[:n]
+            v = (vc[pid, h].double() * _unit(vs[pid, h])[:, None, None]).flatten(0, 1)[:n] if want_out else None
+            for i0 in range(0, new[b], 512):
+                i1 = min(new[b], i0 + 512)
+                q = st["q"][at + i0:at + i1, h * G:(h + 1) * G].double().reshape(-1, d)
+                z = q @ k.T.contiguous() / math.sqrt(d)
+                own_pos = torch.arange(n - new[b] + i0, n - new[b] + i1, device=dev).repeat_interleave(G)
+                z = z.masked_fill(torch.arange(n, device=dev) > own_pos[:, None], -math.inf)
+                s = torch.logsumexp(z, 1)
+                lse[at + i0:at + i1, h * G:(h + 1) * G] = s.view(-1, G)
+                if want_w:
+                    given = st["lse"][at + i0:at + i1, h * G:(h + 1) * G].double().reshape(-1, 1)
+                    w[b, h, :n] += torch.exp(z - given).sum(0)
+                if want_out:
+                    x = torch.nn.functional.pad(z * math.log2(math.e), (0, -n % 32), value=-math.inf).view(z.shape[0], -1, 32)
+                    top = torch.ceil(x.amax(2, keepdim=True)).clamp(min=-1e300)
+                    y = 256 * torch.exp2(x - top)
+                    quantum = torch.exp2(torch.floor(torch.log2(y.clamp(min=2.0 ** -6))) - 3)
+                    y = torch.round(y / quantum) * quantum / 256 * torch.exp2(top - (s * math.log2(math.e))[:, None, None])
+                    out[at + i0:at + i1, h * G:(h + 1) * G] = (y.flatten(1)[:, :n] @ v).view(-1, G, d)
+        at += new[b]
+    return out, lse, w
+
+
+def _exact_evict(st):
+    kc, vc, ks, vs = st["cache"]
+    page, budget = st["page"], st["budget"]
+    nb = st["new_pages"].shape[1]
+    B, Hkv, _ = st["w"].shape
+    out = {n: x.clone() for n, x in zip(("k", "v", "k_scale", "v_scale"), st["new_cache"])}
+    kept = torch.full((B, Hkv, budget), -1, dtype=torch.int32)
+    w = torch.zeros((B, Hkv, budget), dtype=torch.float64, device=kc.device)
+    lens = st["lens"].tolist()
+    for b, n in enumerate(lens):
+        m = min(n, budget)
+        for h in range(Hkv):
+            row = st["w"][b, h, :n]
+            ids = list(range(n))
+            if n > budget:
+                mid = row[N_SINK:n - N_RECENT].cpu().tolist()
+                best = sorted(range(len(mid)), key=lambda i: (-mid[i], i))[:budget - N_SINK - N_RECENT]
+                ids = (list(range(N_SINK)) + sorted(N_SINK + i for i in best) + list(range(n - N_RECENT, n)))
+            kept[b, h, :m] = torch.tensor(ids, dtype=torch.int32)
+            ids = torch.tensor(ids, device=kc.device)
+            w[b, h, :m] = row[ids].double()
+            p = st["pages"][b].long()[ids // page]
+            for name, sname, c, s in (("k", "k_scale", kc, ks), ("v", "v_scale", vc, vs)):
+                y = c[p, h, ids % page].double() * _unit(s[p, h])[:, None]
+                y = torch.nn.functional.pad(y, (0, 0, 0, nb * page - m)).view(nb, page, -1)[:-(-m // page)]
+                e = _block(y)
+                code = _codes(y, e).float().to(E4M3).view(-1, y.shape[-1])
+                dst = st["new_pages"][b].long()[:-(-m // page)]
+                at = torch.arange(m, device=kc.device)
+                out[name].view(torch.uint8)[dst[at // page], h, at % page] = code[:m].view(torch.uint8)
+                out[sname][dst, h] = (e + 127).to(torch.uint8)
+    return dict(kept=kept, lens=torch.tensor([min(n, budget) for n in lens], dtype=torch.int32), w=w, **out)
+
+
+def exact(case, seed):
+    if case["op"] == "evict" and case["B"] * case["Hkv"] > 160:
+        return None
+    st = prepare(case, seed)
+    _, new = _lengths(case)
+    if case["op"] == "rope":
+        return _turn(st["q"], st["table"][st["pos"].long()], st["layout"])
+    if case["op"] == "append":
+        return _exact_append(st, new)
+    if case["op"] == "fwd":
+        return _exact_rows(st, new, True, False)[:2]
+    if case["op"] == "weights":
+        return _exact_rows(st, new, False, True)[2]
+    return _exact_evict(st)
