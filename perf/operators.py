@@ -107,11 +107,16 @@ def _lengths(case):
     return lens, new
 
 
+def _pow2(e):
+    """2^e in 64 bits for whole e (exp2 and log2 may be off by a rounding)."""
+    return ((e.long() + 1023) << 52).view(torch.float64)
+
+
 def _quantise(x):
     """[..., page, d] in 32 bits -> E4M3 codes and bytes, one scale per block."""
     f, t = torch.frexp(x.abs().amax((-2, -1)))
     e = (t - 9 + (f > 0.875).int()).clamp_(min=-127)
-    return (x * torch.exp2(-e.float())[..., None, None]).to(E4M3), (e + 127).to(torch.uint8)
+    return (x * _pow2(-e).float()[..., None, None]).to(E4M3), (e + 127).to(torch.uint8)
 
 
 def _make_table(n_pos, rot, device):
@@ -200,7 +205,7 @@ def prepare(case, seed):
 def _e4m3_64(y):
     """64-bit values to the nearest E4M3 value, ties to even, saturating at 448."""
     _, e = torch.frexp(y)
-    step = torch.exp2(((e - 1).clamp_(min=-6) - 3).double())
+    step = _pow2((e - 1).clamp_(min=-6) - 3)
     return (torch.round(y / step) * step).clamp_(-448.0, 448.0)
 
 
@@ -253,9 +258,9 @@ def _plain_append(st):
         e = (t - 9 + (f > 0.875).int()).clamp_(min=-127)
         was = s[pid].int() - 127
         e = torch.where(any_old, torch.maximum(e, was), e)
-        here = c[pid].double() * torch.exp2(was.double())[..., None, None]
+        here = c[pid].double() * _pow2(was)[..., None, None]
         y = torch.where(is_old[:, None, :, None], here, y)
-        code = _e4m3_64(y * torch.exp2(-e.double())[..., None, None]).float().to(E4M3)
+        code = _e4m3_64(y * _pow2(-e)[..., None, None]).float().to(E4M3)
         keep = (is_old | is_new)[:, None, :, None]
         c.view(torch.uint8)[pid] = torch.where(keep, code.view(torch.uint8), c.view(torch.uint8)[pid])
         s[pid] = (e + 127).to(torch.uint8)
@@ -266,7 +271,7 @@ def _plain_append(st):
 def _gathered(st, code, byte):
     """[B][Hkv][W * page][d] in 32 bits: a sequence's blocks side by side."""
     pid = st["pages"].clamp(min=0).long()
-    x = code[pid].float() * torch.exp2(byte[pid].float() - 127.0)[..., None, None]
+    x = code[pid].float() * _pow2(byte[pid].int() - 127).float()[..., None, None]
     B, W, Hkv, page, d = x.shape
     return x.transpose(1, 2).reshape(B, Hkv, W * page, d)
 
@@ -312,7 +317,7 @@ def _plain_fwd(st, want_out=True):
     mg = torch.ceil(x.amax(-1, keepdim=True))
     mg = torch.where(mg == -math.inf, m[..., None], mg)
     p = torch.exp2(x.sub_(mg))
-    lift = torch.exp2(mg - m[..., None])
+    lift = _pow2((mg - m[..., None]).clamp(min=-900)).float()
     ell = (p.sum(-1, keepdim=True) * lift).sum((-2, -1))
     p = p.mul_(256.0).to(E4M3).float().mul_(lift)
     o = torch.matmul(p.view(B, Hkv, nq * G, n), _gathered(st, vc, vs)).view(B, Hkv, nq, G, -1)
@@ -357,11 +362,11 @@ def _plain_evict(st):
     h = torch.arange(Hkv, device=dev)[None, :, None]
     ok = torch.nn.functional.pad(there, (0, pad)).view(B, Hkv, nb, page)
     for c, s, nc, ns in ((kc, ks, nk, nks), (vc, vs, nv, nvs)):
-        y = c[pid, h, src % page].float() * torch.exp2(s[pid, h].float() - 127.0)[..., None]
+        y = c[pid, h, src % page].float() * _pow2(s[pid, h].int() - 127).float()[..., None]
         y = torch.nn.functional.pad(torch.where(there[..., None], y, 0.0), (0, 0, 0, pad)).view(B, Hkv, nb, page, -1)
         f, tt = torch.frexp(y.abs().amax((-2, -1)))
         e = (tt - 9 + (f > 0.875).int()).clamp_(min=-127)
-        code = (y * torch.exp2(-e.float())[..., None, None]).to(E4M3).view(torch.uint8).transpose(1, 2)
+        code = (y * _pow2(-e).float()[..., None, None]).to(E4M3).view(torch.uint8).transpose(1, 2)
         full = ok.any(-1).transpose(1, 2)
         nc.view(torch.uint8)[dst] = torch.where(ok.transpose(1, 2)[..., None], code, nc.view(torch.uint8)[dst])
         ns[dst] = torch.where(full, (e + 127).to(torch.uint8).transpose(1, 2), ns[dst])
@@ -434,7 +439,7 @@ def work(case):
 
 def _unit(b):
     """2^(byte - 127) in 64 bits."""
-    return torch.ldexp(torch.ones((), dtype=torch.float64, device=b.device), b.int() - 127)
+    return _pow2(b.int() - 127)
 
 
 def _turn(x, cs, layout):
@@ -449,18 +454,17 @@ def _turn(x, cs, layout):
 
 
 def _block(y):
-    """Codes (as values) and byte of one block of true values [Hkv][tokens][d]."""
+    """The scales' exponents of one block of true values [Hkv][tokens][d]."""
     top = y.abs().flatten(1).amax(1)
     e = torch.where(top > 0, torch.ceil(torch.log2(top / 448.0)), -127.0)
     # (log2 next to an integer may be off by one either way)
-    e = torch.where(top > 448.0 * torch.exp2(e), e + 1, e)
-    e = torch.where(top <= 448.0 * torch.exp2(e - 1), e - 1, e).clamp(min=-127)
-    return e
+    e = torch.where(top > 448.0 * _pow2(e), e + 1, e)
+    return torch.where(top <= 448.0 * _pow2(e - 1), e - 1, e).clamp(min=-127)
 
 
 def _codes(y, e):
-    z = y * torch.exp2(-e)[:, None, None]
-    quantum = torch.exp2(torch.floor(torch.log2(z.abs().clamp(min=2.0 ** -6))).clamp(min=-6) - 3)
+    z = y * _pow2(-e)[:, None, None]
+    quantum = _pow2((torch.frexp(z).exponent - 1).clamp(min=-6) - 3)
     return (torch.round(z / quantum) * quantum).clamp(-448, 448)
 
 
@@ -485,7 +489,7 @@ def _exact_append(st, new):
                 if o:
                     was = s[p].double() - 127
                     e = torch.maximum(e, was)
-                    t = torch.cat((c[p, :, :o].double() * torch.exp2(was)[:, None, None], t), 1)
+                    t = torch.cat((c[p, :, :o].double() * _pow2(was)[:, None, None], t), 1)
                 out[name][p, :, :z - j * page] = _codes(t, e).float().to(E4M3)
                 out[sname][p] = (e + 127).to(torch.uint8)
         at += new[b]
@@ -523,7 +527,7 @@ def _exact_rows(st, new, want_out, want_w):
                     x = torch.nn.functional.pad(z * math.log2(math.e), (0, -n % 32), value=-math.inf).view(z.shape[0], -1, 32)
                     top = torch.ceil(x.amax(2, keepdim=True)).clamp(min=-1e300)
                     y = 256 * torch.exp2(x - top)
-                    quantum = torch.exp2(torch.floor(torch.log2(y.clamp(min=2.0 ** -6))) - 3)
+                    quantum = _pow2((torch.frexp(y).exponent - 1).clamp(min=-6) - 3)
                     y = torch.round(y / quantum) * quantum / 256 * torch.exp2(top - (s * math.log2(math.e))[:, None, None])
                     out[at + i0:at + i1, h * G:(h + 1) * G] = (y.flatten(1)[:, :n] @ v).view(-1, G, d)
         at += new[b]
