@@ -3,14 +3,17 @@
 The C entry points are exposed under their C names; ``fwd`` and
 ``p_underflow_count`` are thin conveniences that take torch tensors on the GPU,
 check their dtypes and shapes, allocate outputs with torch and pass the
-current torch stream.  Every step of the computation runs in the HIP kernels;
-there is no fallback.  If the shared library is missing the import fails.
+current torch stream; ``rope``, ``cache_append``, ``cache_fwd``, ``cache_weights``
+and ``cache_evict`` do the same for the KV cache.  Every step of the computation
+runs in the HIP kernels; there is no fallback.  If the shared library is missing the import fails.
 """
 from __future__ import annotations
 
 import ctypes
 import functools
+import math
 import os
+from typing import NamedTuple
 
 import torch
 
@@ -144,6 +147,61 @@ def attn_fp8_strerror(status: int) -> str:
 
 def attn_fp8_version() -> int:
     return _lib.attn_fp8_version()
+
+
+# ---- the KV cache (include/attn_fp8_cache.h): structures and C entry points ----
+
+ATTN_TYPE_F32, ATTN_TYPE_BF16, ATTN_TYPE_F16, ATTN_TYPE_E4M3 = 0, 1, 2, 3
+ATTN_ROPE_HALF, ATTN_ROPE_INTERLEAVED = 0, 1
+
+LAYOUTS = {"half": ATTN_ROPE_HALF, "interleaved": ATTN_ROPE_INTERLEAVED}
+
+
+class attn_fp8_cache(ctypes.Structure):
+    _fields_ = [("k", _P), ("v", _P), ("k_scale", _P), ("v_scale", _P), ("n_pages", _I), ("Hkv", _I),
+                ("page", _I), ("d", _I)]
+
+
+class attn_fp8_batch(ctypes.Structure):
+    _fields_ = [("pages", _P), ("lens", _P), ("cu", _P), ("B", _I), ("W", _I), ("T", _I), ("max_q", _I)]
+
+
+class attn_fp8_heads(ctypes.Structure):
+    _fields_ = [("data", _P), ("stride_t", ctypes.c_int64), ("stride_h", ctypes.c_int64), ("type", _I)]
+
+
+class attn_fp8_rotation(ctypes.Structure):
+    _fields_ = [("table", _P), ("positions", _P), ("n_pos", _I), ("rot", _I), ("layout", _I)]
+
+
+_L = ctypes.c_int64
+_PC, _PB, _PH, _PR = (ctypes.POINTER(t) for t in (attn_fp8_cache, attn_fp8_batch, attn_fp8_heads,
+                                                  attn_fp8_rotation))
+_lib.attn_fp8_rope.argtypes = [_PH, _PH, _I, _I, _I, _PR, _P]
+_lib.attn_fp8_rope.restype = _I
+_lib.attn_fp8_cache_append.argtypes = [_PC, _PB, _PH, _PH, _PR, _PH, _PH, _I, _P]
+_lib.attn_fp8_cache_append.restype = _I
+_lib.attn_fp8_cache_fwd.argtypes = [_PC, _PB, _PH, _I, _P, _I, _P, _I, _F, _F, _I, _P, _Z, _P]
+_lib.attn_fp8_cache_fwd.restype = _I
+_lib.attn_fp8_cache_workspace_bytes.argtypes = [_PC, _PB, _I, _I, ctypes.POINTER(_Z)]
+_lib.attn_fp8_cache_workspace_bytes.restype = _I
+_lib.attn_fp8_cache_weights.argtypes = [_PC, _PB, _PH, _I, _P, _I, _F, _F, _I, _P, _L, _L, _P]
+_lib.attn_fp8_cache_weights.restype = _I
+_lib.attn_fp8_cache_evict.argtypes = [_PC, _PB, _PC, _P, _P, _L, _L, _I, _I, _I, _P, _P, _P, _P]
+_lib.attn_fp8_cache_evict.restype = _I
+
+attn_fp8_rope = _lib.attn_fp8_rope
+attn_fp8_cache_append = _lib.attn_fp8_cache_append
+attn_fp8_cache_fwd = _lib.attn_fp8_cache_fwd
+attn_fp8_cache_weights = _lib.attn_fp8_cache_weights
+attn_fp8_cache_evict = _lib.attn_fp8_cache_evict
+
+
+def attn_fp8_cache_workspace_bytes(cache, batch, Hq, max_len):
+    """Returns (status, bytes)."""
+    n = _Z(0)
+    st = _lib.attn_fp8_cache_workspace_bytes(cache, batch, Hq, max_len, ctypes.byref(n))
+    return st, n.value
 
 
 # ---- torch conveniences ----
@@ -282,3 +340,301 @@ def block_gap_diag(q, k, v, *, S: float = 256.0, order: str = "reverse", causal:
     if st != ATTN_OK:
         raise AttnError(st)
     return hist, bz, counts
+
+
+# ---- the KV cache: torch conveniences ----
+
+_TYPES = {torch.float32: ATTN_TYPE_F32, torch.bfloat16: ATTN_TYPE_BF16, torch.float16: ATTN_TYPE_F16,
+          torch.float8_e4m3fn: ATTN_TYPE_E4M3}
+
+
+class KVCache(NamedTuple):
+    """An E4M3 cache in pages: k, v [pages, Hkv, page, d] float8_e4m3fn (or uint8),
+    k_scale, v_scale [pages, Hkv] uint8; a code stands for code * 2^(byte - 127)."""
+    k: torch.Tensor
+    v: torch.Tensor
+    k_scale: torch.Tensor
+    v_scale: torch.Tensor
+
+
+def kv_cache(n_pages, Hkv, d, *, page: int = 128, device="cuda"):
+    """A KVCache of empty (zero) pages."""
+    def codes():
+        return torch.zeros((n_pages, Hkv, page, d), dtype=torch.uint8, device=device).view(torch.float8_e4m3fn)
+
+    def scales():
+        return torch.zeros((n_pages, Hkv), dtype=torch.uint8, device=device)
+
+    return KVCache(codes(), codes(), scales(), scales())
+
+
+def _device(t):
+    if not t.is_cuda:
+        raise ValueError("tensors must be on the GPU")
+    if t.device.index != torch.cuda.current_device():
+        raise ValueError(f"tensors are on {t.device}, the current device is cuda:{torch.cuda.current_device()}")
+    return t.device
+
+
+def _ints(t, shape, name, device):
+    if t.dtype != torch.int32 or tuple(t.shape) != shape or not t.is_contiguous() or t.device != device:
+        raise ValueError(f"{name} must be a contiguous int32 tensor {list(shape)} on {device}")
+    return t.data_ptr()
+
+
+def _cache(cache, device):
+    k, v, ks, vs = cache
+    shape = k.shape
+    if len(shape) != 4 or v.shape != shape or ks.shape != shape[:2] or vs.shape != shape[:2]:
+        raise ValueError("a cache has k, v [pages, Hkv, page, d] and k_scale, v_scale [pages, Hkv]")
+    if k.dtype not in _FAST_V or v.dtype not in _FAST_V or ks.dtype != torch.uint8 or vs.dtype != torch.uint8:
+        raise TypeError("a cache has float8_e4m3fn (or uint8) codes and uint8 scales")
+    for t in cache:
+        if t.device != device or not t.is_contiguous():
+            raise ValueError("a cache's tensors must be contiguous and on the inputs' device")
+    return attn_fp8_cache(k.data_ptr(), v.data_ptr(), ks.data_ptr(), vs.data_ptr(), shape[0], shape[1],
+                          shape[2], shape[3])
+
+
+def _batch(pages, lens, cu, T, max_q, device):
+    if pages.dim() != 2:
+        raise ValueError("pages must be [B, W]")
+    B, W = pages.shape
+    if cu is None:
+        n = T // B if B else 0
+        if B * n != T:
+            raise ValueError(f"{T} tokens of {B} sequences: give cu")
+        max_q = n if max_q is None else max_q
+        if max_q < n:
+            raise ValueError(f"max_q = {max_q}, but each sequence has {n} new tokens")
+    elif max_q is None:
+        raise ValueError("cu needs max_q, the most new tokens of a sequence")
+    return attn_fp8_batch(_ints(pages, (B, W), "pages", device), _ints(lens, (B,), "lens", device),
+                          None if cu is None else _ints(cu, (B + 1,), "cu", device), B, W, T, max(int(max_q), 1))
+
+
+def _heads(t, name, device, types):
+    if t.dim() != 3 or t.dtype not in types or t.device != device or (t.shape[2] > 1 and t.stride(2) != 1):
+        raise ValueError(f"{name} must be [T, H, d] with contiguous channels on {device}, of a type in "
+                         f"{[str(x) for x in types]}")
+    return attn_fp8_heads(t.data_ptr(), t.stride(0), t.stride(1), _TYPES[t.dtype])
+
+
+def _empty(shape, dtype, device, stream):
+    """Memory that belongs to the stream the call runs on."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    if not isinstance(stream, torch.cuda.Stream):
+        stream = torch.cuda.ExternalStream(stream.cuda_stream, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
+def _rotation(table, positions, T, layout, device):
+    if (table.dim() != 3 or table.shape[2] != 2 or table.dtype != torch.float32 or not table.is_contiguous()
+            or table.device != device):
+        raise ValueError(f"table must be a contiguous float32 tensor [positions, rot / 2, 2] on {device}")
+    p = None if positions is None else _ints(positions, (T,), "positions", device)
+    return attn_fp8_rotation(table.data_ptr(), p, table.shape[0], 2 * table.shape[1], LAYOUTS[layout])
+
+
+_INPUTS = (torch.float32, torch.bfloat16, torch.float16)
+_QUERIES = (torch.bfloat16, torch.float8_e4m3fn)
+
+
+def rope_table(n_pos, rot, *, base: float = 10000.0, scaling: str = "none", factor: float = 1.0,
+               original: int = 0, ramp=(1.0, 32.0), device="cuda"):
+    """cos and sin of the rotations, float32 [n_pos, rot / 2, 2], computed in 64 bits
+    and rounded once: pair i turns by p * base^(-2 i / rot) at position p.  Scaled
+    for contexts `factor` times longer than the model was trained on:
+      "linear"  positions are divided by factor;
+      "base"    the base grows to base * factor^(rot / (rot - 2)), which divides the
+                slowest pair's angle by factor and leaves the fastest one's;
+      "ramp"    a pair that makes fewer than ramp[0] turns over the `original`
+                positions is divided by factor, one of more than ramp[1] turns is
+                left, those between are blended linearly in the number of turns."""
+    if rot < 2 or rot % 2 or n_pos < 1 or factor <= 0 or base <= 0:
+        raise ValueError("rope_table needs n_pos >= 1, an even rot >= 2, and positive base and factor")
+    i = torch.arange(rot // 2, dtype=torch.float64, device=device)
+    if scaling == "base":
+        if rot < 4:
+            raise ValueError("scaling by the base needs rot >= 4")
+        base = base * factor ** (rot / (rot - 2))
+    freq = base ** (-2.0 * i / rot)
+    if scaling == "linear":
+        freq = freq / factor
+    elif scaling == "ramp":
+        lo, hi = ramp
+        if original < 1 or not 0 <= lo < hi:
+            raise ValueError("scaling by a ramp needs original >= 1 and 0 <= ramp[0] < ramp[1]")
+        keep = ((original * freq / (2 * math.pi) - lo) / (hi - lo)).clamp(0.0, 1.0)
+        freq = freq * keep + freq / factor * (1 - keep)
+    elif scaling not in ("none", "base"):
+        raise ValueError(f"unknown scaling {scaling!r}")
+    angle = torch.arange(n_pos, dtype=torch.float64, device=device)[:, None] * freq
+    return torch.stack((torch.cos(angle), torch.sin(angle)), -1).float().contiguous()
+
+
+def rope(x, table, positions, *, layout: str = "half", out=None, stream=None):
+    """Rotary positions: x [T, H, d] (float32, bfloat16 or float16, any strides of tokens
+    and heads that are multiples of 16 bytes) with its first rot channels rotated by
+    row positions[t] of the table (rope_table); layout "half" pairs channel i with
+    i + rot / 2, "interleaved" 2 i with 2 i + 1.  out may be x."""
+    dev = _device(x)
+    T, H, d = x.shape if x.dim() == 3 else (0, 0, 0)
+    hx = _heads(x, "x", dev, _INPUTS)
+    r = _rotation(table, positions, T, layout, dev)
+    if out is None:
+        out = _empty((T, H, d), x.dtype, dev, stream)
+    elif out.shape != x.shape:
+        raise ValueError("out must have x's shape")
+    st = _lib.attn_fp8_rope(hx, _heads(out, "out", dev, (x.dtype,)), T, H, d, r, _stream(stream))
+    if st != ATTN_OK:
+        raise AttnError(st)
+    return out
+
+
+def cache_append(cache, k, v, pages, lens, *, cu=None, max_q=None, table=None, positions=None,
+                 layout: str = "half", q=None, q_out=None, stream=None):
+    """Writes new tokens k, v [T, Hkv, d] into the pages of their sequences: k rotated
+    (with a table), both rounded to E4M3 on the scale of their block.  pages int32
+    [B, W], lens int32 [B] (the new tokens included), cu int32 [B + 1] with max_q (None:
+    T / B tokens each).  positions None: the tokens' places in their sequences.  With
+    q [T, Hq, d] its rotation is done in the same launch and returned."""
+    dev = _device(k)
+    c = _cache(cache, dev)
+    hk, hv = _heads(k, "k", dev, _INPUTS), _heads(v, "v", dev, (k.dtype,))
+    T = k.shape[0]
+    if k.shape != v.shape or k.shape[1] != c.Hkv or k.shape[2] != c.d:
+        raise ValueError(f"k, v must be [T, {c.Hkv}, {c.d}]")
+    bt = _batch(pages, lens, cu, T, max_q, dev)
+    r = None if table is None else _rotation(table, positions, T, layout, dev)
+    hq = ho = None
+    Hq = 0
+    if q is not None:
+        if r is None:
+            raise ValueError("q is rotated along: that needs a table")
+        hq, Hq = _heads(q, "q", dev, (k.dtype,)), q.shape[1]
+        if q.shape[0] != T or q.shape[2] != c.d:
+            raise ValueError(f"q must be [{T}, Hq, {c.d}]")
+        if q_out is None:
+            q_out = _empty(tuple(q.shape), q.dtype, dev, stream)
+        elif q_out.shape != q.shape:
+            raise ValueError("q_out must have q's shape")
+        ho = _heads(q_out, "q_out", dev, (k.dtype,))
+    st = _lib.attn_fp8_cache_append(c, bt, hk, hv, r, hq, ho, Hq, _stream(stream))
+    if st != ATTN_OK:
+        raise AttnError(st)
+    return q_out
+
+
+@functools.lru_cache(maxsize=4096)
+def _cache_workspace_bytes(device_index, n_pages, Hkv, page, d, B, W, T, max_q, Hq, max_len):
+    """The size depends on these sizes and on the device's CU count alone."""
+    st, n = attn_fp8_cache_workspace_bytes(attn_fp8_cache(None, None, None, None, n_pages, Hkv, page, d),
+                                           attn_fp8_batch(None, None, None, B, W, T, max_q), Hq, max_len)
+    if st != ATTN_OK:
+        raise AttnError(st)
+    return n
+
+
+def _queries(q, cache, pages, lens, cu, max_q, sm_scale):
+    dev = _device(q)
+    c = _cache(cache, dev)
+    hq = _heads(q, "q", dev, _QUERIES)
+    T, Hq, d = q.shape
+    if d != c.d or Hq % c.Hkv:
+        raise ValueError(f"q must be [T, Hq, {c.d}] with Hq a multiple of {c.Hkv}")
+    bt = _batch(pages, lens, cu, T, max_q, dev)
+    return dev, c, hq, T, Hq, d, bt, 1.0 / math.sqrt(d) if sm_scale is None else float(sm_scale)
+
+
+def cache_fwd(q, cache, pages, lens, *, cu=None, max_q=None, causal: bool = True, sm_scale=None,
+              q_descale: float = 1.0, max_len: int = 0, out=None, out_dtype=torch.bfloat16, lse=None,
+              want_lse: bool = True, stream=None):
+    """Attention of new tokens q [T, Hq, d] (bfloat16 or float8_e4m3fn) over their
+    sequences' cached ones, the new ones included; returns (out [T, Hq, d] of out_dtype
+    (bfloat16 or float32), lse [T, Hq] float32 or None).  Token i of a sequence's n is
+    at position lens[b] - n + i and sees the keys up to it (causal=False: all).
+    pages, lens, cu, max_q as for cache_append.  sm_scale None: 1 / sqrt(d).
+    max_len: no sequence is longer (0: as long as pages allows)."""
+    dev, c, hq, T, Hq, d, bt, sm = _queries(q, cache, pages, lens, cu, max_q, sm_scale)
+    if out is None:
+        out = _empty((T, Hq, d), out_dtype, dev, stream)
+    elif out.shape != q.shape or not out.is_contiguous() or out.device != dev:
+        raise ValueError("out must be a contiguous tensor of q's shape on its device")
+    if out.dtype not in (torch.bfloat16, torch.float32):
+        raise TypeError("out is bfloat16 or float32")
+    if lse is None:
+        lse = _empty((T, Hq), torch.float32, dev, stream) if want_lse else None
+    elif lse.shape != (T, Hq) or lse.dtype != torch.float32 or not lse.is_contiguous() or lse.device != dev:
+        raise ValueError(f"lse must be a contiguous float32 tensor [{T}, {Hq}]")
+    n = _cache_workspace_bytes(dev.index, c.n_pages, c.Hkv, c.page, d, bt.B, bt.W, T, bt.max_q, Hq, int(max_len))
+    ws = _empty((n,), torch.uint8, dev, stream) if n else None
+    st = _lib.attn_fp8_cache_fwd(c, bt, hq, Hq, out.data_ptr(), _TYPES[out.dtype], _ptr(lse), int(bool(causal)), sm,
+                                 float(q_descale), int(max_len), _ptr(ws), n, _stream(stream))
+    if st != ATTN_OK:
+        raise AttnError(st)
+    return out, lse
+
+
+def _weights(weights, B, Hkv, least, device):
+    if (weights.dim() != 3 or weights.shape[:2] != (B, Hkv) or weights.shape[2] < least
+            or weights.dtype != torch.float32 or weights.device != device
+            or (weights.shape[2] > 1 and weights.stride(2) != 1)
+            or (Hkv > 1 and weights.stride(1) < weights.shape[2])
+            or (B > 1 and weights.stride(0) < (Hkv - 1) * weights.stride(1) + weights.shape[2])):
+        raise ValueError(f"weights must be float32 [{B}, {Hkv}, at least {least}] with contiguous rows that do not "
+                         f"overlap, on {device}")
+    return weights.data_ptr(), weights.stride(0), max(weights.stride(1), weights.shape[2])
+
+
+def cache_weights(q, lse, cache, pages, lens, weights, *, cu=None, max_q=None, causal: bool = True, sm_scale=None,
+                  q_descale: float = 1.0, max_len: int = 0, stream=None):
+    """Adds to weights [B, Hkv, n] (float32, in place; n at least the longest sequence,
+    max_len or W * page) the attention weight that each cached token receives from the
+    new tokens q and the query heads of its group; lse is cache_fwd's for the same call."""
+    dev, c, hq, T, Hq, d, bt, sm = _queries(q, cache, pages, lens, cu, max_q, sm_scale)
+    if lse.shape != (T, Hq) or lse.dtype != torch.float32 or not lse.is_contiguous() or lse.device != dev:
+        raise ValueError(f"lse must be a contiguous float32 tensor [{T}, {Hq}]")
+    most = bt.W * c.page
+    most = min(most, int(max_len)) if max_len else most
+    p, sb, sh = _weights(weights, bt.B, c.Hkv, most, dev)
+    st = _lib.attn_fp8_cache_weights(c, bt, hq, Hq, lse.data_ptr(), int(bool(causal)), sm, float(q_descale),
+                                     int(max_len), p, sb, sh, _stream(stream))
+    if st != ATTN_OK:
+        raise AttnError(st)
+    return weights
+
+
+def cache_evict(cache, pages, lens, weights, to, new_pages, budget, *, n_sink: int = 4, n_recent: int = 0,
+                kept=None, new_lens=None, new_weights=None, stream=None):
+    """Moves the `budget` tokens of every sequence and KV head that matter most into the
+    pages new_pages int32 [B, ceil(budget / page)] of the cache `to` (which may be
+    `cache`, then pages that hold none of these sequences): the first n_sink, the last
+    n_recent, and the ones of the largest weights [B, Hkv, n] (equal ones: the earlier).
+    Returns (kept [B, Hkv, budget] int32: where each was, then -1; new_lens [B] int32;
+    new_weights [B, Hkv, budget] float32: theirs, then 0)."""
+    dev = _device(lens)
+    c, ct = _cache(cache, dev), _cache(to, dev)
+    if pages.dim() != 2:
+        raise ValueError("pages must be [B, W]")
+    B, W = pages.shape
+    if (ct.Hkv, ct.page, ct.d) != (c.Hkv, c.page, c.d) or budget < 1:
+        raise ValueError("both caches have the same heads, page and d, and budget is at least 1")
+    bt = attn_fp8_batch(_ints(pages, (B, W), "pages", dev), _ints(lens, (B,), "lens", dev), None, B, W, 0, 1)
+    np_ = _ints(new_pages, (B, -(-budget // c.page)), "new_pages", dev)
+    p, sb, sh = _weights(weights, B, c.Hkv, W * c.page, dev)
+    shape = (B, c.Hkv, budget)
+    kept = _empty(shape, torch.int32, dev, stream) if kept is None else kept
+    new_lens = _empty((B,), torch.int32, dev, stream) if new_lens is None else new_lens
+    new_weights = _empty(shape, torch.float32, dev, stream) if new_weights is None else new_weights
+    if (new_weights.dtype != torch.float32 or tuple(new_weights.shape) != shape or not new_weights.is_contiguous()
+            or new_weights.device != dev):
+        raise ValueError(f"new_weights must be a contiguous float32 tensor {list(shape)}")
+    st = _lib.attn_fp8_cache_evict(c, bt, ct, np_, p, sb, sh, int(budget), int(n_sink), int(n_recent),
+                                   _ints(kept, shape, "kept", dev), _ints(new_lens, (B,), "new_lens", dev),
+                                   new_weights.data_ptr(), _stream(stream))
+    if st != ATTN_OK:
+        raise AttnError(st)
+    return kept, new_lens, new_weights

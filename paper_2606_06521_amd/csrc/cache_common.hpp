@@ -1,0 +1,217 @@
+// The KV cache's kernels: launch parameters, the sequences and pages of a batch,
+// element types.
+#pragma once
+
+#include "attn_common.hpp"
+
+namespace attn {
+
+// element types (the values of ATTN_TYPE_*)
+constexpr int kTypeF32 = 0, kTypeBf16 = 1, kTypeF16 = 2, kTypeE4m3 = 3;
+
+// Keys per group of P with a scale of its own: what one scale of an E4M3 MFMA
+// operand covers.  Keys per visit of the attention kernels.
+constexpr int kGroup = 32, kVisit = 128;
+
+// The batch, as the device reads it.  Nothing in lens, cu or pages is trusted:
+// whatever they hold, no access leaves the arrays.
+struct Batch {
+    const int32_t* pages;   // [B][W]
+    const int32_t* lens;    // [B]
+    const int32_t* cu;      // [B + 1], or null: `uniform` tokens each
+    int B, W, T, max_q, uniform;
+};
+
+struct Cache {
+    uint8_t* k;
+    uint8_t* v;
+    uint8_t* ks;
+    uint8_t* vs;
+    int n_pages, Hkv;
+};
+
+// Packed heads [T][H][d]: element strides.
+struct Heads {
+    void* data;
+    int64_t st, sh;
+};
+
+struct Rotation {
+    const float* table;          // [n_pos][rot / 2][2], null: no rotation
+    const int32_t* positions;    // null: the position in the sequence
+    int n_pos, rot, layout;      // layout 0: halves, 1: interleaved
+};
+
+// Sequence b: its length (at most max_len), its new tokens [first, first + n) of
+// the call (at most max_q, inside [0, T)), the position of the first of them.
+struct Seq {
+    int len, first, n, pos0;
+};
+
+__device__ inline Seq sequence(const Batch& bt, int b, int max_len)
+{
+    Seq s;
+    s.len = min(max(bt.lens[b], 0), max_len);
+    int n;
+    if (bt.cu) {
+        const int c0 = bt.cu[b], c1 = bt.cu[b + 1];
+        s.first = min(max(c0, 0), bt.T);
+        n = min(max(c1, s.first), bt.T) - s.first;
+    } else {
+        s.first = b * bt.uniform;
+        n = bt.uniform;
+    }
+    // (position of the first new token, which may lie before token 0 or, past the
+    // first max_q, leave tokens out at the end)
+    s.pos0 = s.len - n;
+    s.n = min(n, bt.max_q);
+    return s;
+}
+
+// The same in scalar registers, for a sequence that all lanes share.
+__device__ inline Seq uniform(const Seq& s)
+{
+    return {__builtin_amdgcn_readfirstlane(s.len), __builtin_amdgcn_readfirstlane(s.first), __builtin_amdgcn_readfirstlane(s.n),
+            __builtin_amdgcn_readfirstlane(s.pos0)};
+}
+
+// Page of a sequence's block, -1 if there is none.
+__device__ inline int page_of(const Batch& bt, int n_pages, int b, int block)
+{
+    const int p = block < bt.W ? bt.pages[(size_t)b * bt.W + block] : -1;
+    return (uint32_t)p < (uint32_t)n_pages ? p : -1;
+}
+
+// ---- E4M3 blocks ----
+
+// Least e >= -127 with amax <= 448 * 2^e (amax finite, >= 0).
+__device__ inline int block_exponent(float amax)
+{
+    if (amax == 0.f)
+        return -127;
+    const int t = __builtin_amdgcn_frexp_expf(amax);
+    const float f = __builtin_amdgcn_frexp_mantf(amax);   // [0.5, 1): 448 = 0.875 * 2^9
+    return max(t - 9 + (f > 0.875f ? 1 : 0), -127);
+}
+
+// Four values to E4M3 bytes (round to nearest even; |x| <= 448 or NaN).
+__device__ inline uint32_t to_e4m3(float a, float b, float c, float d)
+{
+    const int w = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, w, true);
+}
+
+__device__ inline void from_e4m3(uint32_t w, float* x)
+{
+    x[0] = __builtin_amdgcn_cvt_f32_fp8((int)w, 0);
+    x[1] = __builtin_amdgcn_cvt_f32_fp8((int)w, 1);
+    x[2] = __builtin_amdgcn_cvt_f32_fp8((int)w, 2);
+    x[3] = __builtin_amdgcn_cvt_f32_fp8((int)w, 3);
+}
+
+// ---- eight consecutive values of an element type ----
+
+template <int TYPE>
+__device__ inline void load8(const void* base, int64_t i, float* x)
+{
+    if constexpr (TYPE == kTypeF32) {
+        const f32x4* p = reinterpret_cast<const f32x4*>(static_cast<const float*>(base) + i);
+        const f32x4 a = p[0], b = p[1];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            x[j] = a[j];
+            x[4 + j] = b[j];
+        }
+    } else {
+        const i32x4 w = *reinterpret_cast<const i32x4*>(static_cast<const uint16_t*>(base) + i);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const uint32_t u = (uint32_t)w[j];
+            if constexpr (TYPE == kTypeBf16) {
+                x[2 * j] = __uint_as_float(u << 16);
+                x[2 * j + 1] = __uint_as_float(u & 0xFFFF0000u);
+            } else {
+                x[2 * j] = (float)__builtin_bit_cast(_Float16, (uint16_t)u);
+                x[2 * j + 1] = (float)__builtin_bit_cast(_Float16, (uint16_t)(u >> 16));
+            }
+        }
+    }
+}
+
+template <int TYPE>
+__device__ inline void store8(void* base, int64_t i, const float* x)
+{
+    if constexpr (TYPE == kTypeF32) {
+        f32x4* p = reinterpret_cast<f32x4*>(static_cast<float*>(base) + i);
+        p[0] = f32x4{x[0], x[1], x[2], x[3]};
+        p[1] = f32x4{x[4], x[5], x[6], x[7]};
+    } else {
+        i32x4 w;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            if constexpr (TYPE == kTypeBf16)
+                w[j] = (int)((uint32_t)__builtin_bit_cast(uint16_t, (__bf16)x[2 * j]) |
+                             (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)x[2 * j + 1]) << 16);
+            else
+                w[j] = (int)((uint32_t)__builtin_bit_cast(uint16_t, (_Float16)x[2 * j]) |
+                             (uint32_t)__builtin_bit_cast(uint16_t, (_Float16)x[2 * j + 1]) << 16);
+        }
+        *reinterpret_cast<i32x4*>(static_cast<uint16_t*>(base) + i) = w;
+    }
+}
+
+// ---- host side ----
+
+struct FwdParams {
+    Batch bt;
+    Cache cache;
+    Heads q;
+    void* out;
+    float* lse;             // nullable
+    float* ws;              // partial results of split tiles
+    int out_bf16, Hq, G;    // G = Hq / Hkv
+    int causal, max_len;
+    float c;                // log2(e) sm_scale q_descale
+    int tiles, chunk, ranges;   // row tiles per (sequence, KV head); visits per range; most ranges
+};
+
+struct WeightParams {
+    Batch bt;
+    Cache cache;
+    Heads q;
+    const float* lse;
+    float* w;
+    int64_t sb, sh;
+    int Hq, G, causal, max_len;
+    float c;
+};
+
+struct EvictParams {
+    Batch bt;
+    Cache from, to;
+    const int32_t* new_pages;   // [B][nb]
+    const float* w;
+    int64_t sb, sh;
+    int budget, n_sink, n_recent, nb;
+    int32_t* kept;
+    int32_t* new_lens;
+    float* new_w;               // nullable
+};
+
+// How a call of the attention is cut (host code; see cache_fwd.hip).
+struct FwdPlan {
+    int rows;               // query rows per tile
+    int tiles;              // tiles per (sequence, KV head)
+    int chunk, ranges;      // visits per range, ranges per tile (1: no split)
+    size_t bytes;           // workspace
+};
+FwdPlan cache_fwd_plan(int B, int Hkv, int G, int max_q, int max_len, int d, int n_cu);
+
+hipError_t launch_rope(const Heads& x, const Heads& out, int T, int H, int d, int type, const Rotation& r, hipStream_t s);
+hipError_t launch_append(const Batch& bt, const Cache& c, int d, int page, const Heads& k, const Heads& v, int type,
+                         const Rotation& r, const Heads& q, const Heads& q_out, int Hq, hipStream_t s);
+hipError_t launch_cache_fwd(FwdParams p, const FwdPlan& plan, int d, int page, bool e4m3, hipStream_t s);
+hipError_t launch_cache_weights(const WeightParams& p, int d, int page, bool e4m3, hipStream_t s);
+hipError_t launch_cache_evict(const EvictParams& p, int d, int page, hipStream_t s);
+
+}  // namespace attn

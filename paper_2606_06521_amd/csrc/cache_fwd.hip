@@ -1,0 +1,118 @@
+// Attention of new tokens over the cache: plan, launch, merge.
+#include "cache_fwd_kernel.hpp"
+
+#include <algorithm>
+#include <type_traits>
+
+namespace attn {
+
+namespace {
+
+// Merge of a split tile: a workgroup per query row, thread (piece, part) takes
+// one 16-byte piece of the row from every PARTS-th range; the parts are added
+// through LDS in a fixed order.  Ranges stand at their own power of two; the
+// row's is the largest.
+template <int D>
+__global__ void __launch_bounds__(256) cache_merge(FwdParams p, int tile_rows)
+{
+    constexpr int PIECES = D / 4, PARTS = 256 / PIECES;
+    __shared__ f32x4 osh[PARTS][PIECES];
+    __shared__ float lsh[PARTS];
+    const int hk = (int)(blockIdx.x % p.cache.Hkv);
+    int64_t rest = blockIdx.x / p.cache.Hkv;
+    const int per_seq = p.bt.max_q * p.G;
+    const int b = (int)(rest / per_seq), R = (int)(rest - (int64_t)b * per_seq);
+    const Seq s = sequence(p.bt, b, p.max_len);
+    if (R >= s.n * p.G)
+        return;
+    const int tile = R / tile_rows;
+    const int visits = tile_visits(p, s, tile, tile_rows);
+    const int n = (visits + p.chunk - 1) / p.chunk;
+    if (n <= 1)
+        return;                                  // (the range wrote the row itself)
+    const int rr = R - tile * tile_rows;
+    const size_t stride = (size_t)tile_rows * (D + 2);
+    const float* base = p.ws + (((size_t)b * p.cache.Hkv + hk) * p.tiles + tile) * p.ranges * stride;
+    const int piece = threadIdx.x % PIECES, part = threadIdx.x / PIECES;
+    float m = -INFINITY;
+    for (int c = 0; c < n; ++c)
+        m = fmax_f(m, base[c * stride + tile_rows * (D + 1) + rr]);
+    f32x4 acc = {};
+    float l = 0.f;
+    for (int c = part; c < n; c += PARTS) {
+        const float* at = base + c * stride;
+        const float mc = at[tile_rows * (D + 1) + rr];
+        const float f = mc == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mc - m);
+        const f32x4 x = *reinterpret_cast<const f32x4*>(at + rr * D + 4 * piece);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            acc[e] += x[e] * f;
+        l += at[tile_rows * D + rr] * f;
+    }
+    osh[part][piece] = acc;
+    if (piece == 0)
+        lsh[part] = l;
+    __syncthreads();
+    if (part != 0)
+        return;
+#pragma unroll
+    for (int v = 1; v < PARTS; ++v) {
+        const f32x4 t = osh[v][piece];
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            acc[e] += t[e];
+        l += lsh[v];
+    }
+    write_row<D>(p, s, hk, R, piece, acc, l, m);
+}
+
+template <int D, int PAGE>
+hipError_t fwd_go(const FwdParams& p, bool e4m3, int64_t grid, hipStream_t s)
+{
+    auto go = [&](auto kern) {
+        hipLaunchKernelGGL(kern, dim3((unsigned)grid), dim3(256), 0, s, p);
+        return hipGetLastError();
+    };
+    return e4m3 ? go(cache_fwd_kernel<D, PAGE, true>) : go(cache_fwd_kernel<D, PAGE, false>);
+}
+
+}  // namespace
+
+FwdPlan cache_fwd_plan(int B, int Hkv, int G, int max_q, int max_len, int d, int n_cu)
+{
+    FwdPlan pl;
+    pl.rows = 16;
+    pl.tiles = (int)(((int64_t)max_q * G + pl.rows - 1) / pl.rows);
+    const int64_t units = (int64_t)B * Hkv * pl.tiles;
+    const int visits = (max_len + kVisit - 1) / kVisit;
+    // enough ranges to fill the GPU, none shorter than two visits of its four waves
+    const int64_t want = std::max<int64_t>(1, n_cu / std::max<int64_t>(units, 1));
+    pl.chunk = (int)std::max<int64_t>(8, (visits + want - 1) / want);
+    pl.chunk = std::min(pl.chunk, kMaxChunk);
+    pl.ranges = std::max(1, (visits + pl.chunk - 1) / pl.chunk);
+    pl.bytes = pl.ranges > 1 ? (size_t)units * pl.ranges * pl.rows * (d + 2) * sizeof(float) : 0;
+    return pl;
+}
+
+hipError_t launch_cache_fwd(FwdParams p, const FwdPlan& pl, int d, int page, bool e4m3, hipStream_t s)
+{
+    p.tiles = pl.tiles;
+    p.chunk = pl.chunk;
+    p.ranges = pl.ranges;
+    const int64_t units = (int64_t)p.bt.B * p.cache.Hkv * pl.tiles;
+    const int64_t grid = units * pl.ranges, rows = (int64_t)p.bt.B * p.cache.Hkv * p.bt.max_q * p.G;
+    if (grid > 1 << 30 || rows > 1 << 30)
+        return hipErrorInvalidValue;
+    hipError_t e = d == 64 ? (page == 64 ? fwd_go<64, 64>(p, e4m3, grid, s) : fwd_go<64, 128>(p, e4m3, grid, s))
+                           : (page == 64 ? fwd_go<128, 64>(p, e4m3, grid, s) : fwd_go<128, 128>(p, e4m3, grid, s));
+    if (e == hipSuccess && pl.ranges > 1) {
+        if (d == 64)
+            hipLaunchKernelGGL(cache_merge<64>, dim3((unsigned)rows), dim3(256), 0, s, p, pl.rows);
+        else
+            hipLaunchKernelGGL(cache_merge<128>, dim3((unsigned)rows), dim3(256), 0, s, p, pl.rows);
+        e = hipGetLastError();
+    }
+    return e;
+}
+
+}  // namespace attn
