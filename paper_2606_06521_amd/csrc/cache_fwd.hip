@@ -1,5 +1,5 @@
 // Attention of new tokens over the cache: plan, launch, merge.
-#include "cache_fwd_kernel.hpp"
+#include "cache_fwd_tile.hpp"
 
 #include <algorithm>
 #include <type_traits>
@@ -63,32 +63,41 @@ __global__ void __launch_bounds__(256) cache_merge(FwdParams p, int tile_rows)
             acc[e] += t[e];
         l += lsh[v];
     }
-    write_row<D>(p, s, hk, R, piece, acc, l, m);
+    write_row<D>(p, s, hk, R, piece, acc, l, 1.f / l, m);
 }
 
 template <int D, int PAGE>
-hipError_t fwd_go(const FwdParams& p, bool e4m3, int64_t grid, hipStream_t s)
+hipError_t fwd_go(const FwdParams& p, int rows, bool e4m3, int64_t grid, hipStream_t s)
 {
     auto go = [&](auto kern) {
         hipLaunchKernelGGL(kern, dim3((unsigned)grid), dim3(256), 0, s, p);
         return hipGetLastError();
     };
+    if (rows == kTileRows)
+        return e4m3 ? go(cache_fwd_tile_kernel<D, PAGE, true>) : go(cache_fwd_tile_kernel<D, PAGE, false>);
     return e4m3 ? go(cache_fwd_kernel<D, PAGE, true>) : go(cache_fwd_kernel<D, PAGE, false>);
 }
+
+// Query rows of a (sequence, KV head) beyond which tiles of 128 rows take less time
+// than tiles of 16, each of which streams K and V by itself.
+constexpr int kTallFrom = 32;
 
 }  // namespace
 
 FwdPlan cache_fwd_plan(int B, int Hkv, int G, int max_q, int max_len, int d, int n_cu)
 {
     FwdPlan pl;
-    pl.rows = 16;
-    pl.tiles = (int)(((int64_t)max_q * G + pl.rows - 1) / pl.rows);
+    const int64_t run = (int64_t)max_q * G;             // rows of a (sequence, KV head)
+    const bool tall = run > kTallFrom;
+    pl.rows = tall ? kTileRows : 16;
+    pl.tiles = (int)((run + pl.rows - 1) / pl.rows);
     const int64_t units = (int64_t)B * Hkv * pl.tiles;
     const int visits = (max_len + kVisit - 1) / kVisit;
-    // enough ranges to fill the GPU, none shorter than two visits of its four waves
-    const int64_t want = std::max<int64_t>(1, n_cu / std::max<int64_t>(units, 1));
+    // enough ranges to fill the GPU (two workgroups of tall tiles fit a CU), none
+    // shorter than two visits of a workgroup's four waves, or eight of a tall tile's
+    const int64_t want = std::max<int64_t>(1, (tall ? 2 : 1) * n_cu / std::max<int64_t>(units, 1));
     pl.chunk = (int)std::max<int64_t>(8, (visits + want - 1) / want);
-    pl.chunk = std::min(pl.chunk, kMaxChunk);
+    pl.chunk = std::min(pl.chunk, tall ? kTileChunk : kMaxChunk);
     pl.ranges = std::max(1, (visits + pl.chunk - 1) / pl.chunk);
     pl.bytes = pl.ranges > 1 ? (size_t)units * pl.ranges * pl.rows * (d + 2) * sizeof(float) : 0;
     return pl;
@@ -100,11 +109,12 @@ hipError_t launch_cache_fwd(FwdParams p, const FwdPlan& pl, int d, int page, boo
     p.chunk = pl.chunk;
     p.ranges = pl.ranges;
     const int64_t units = (int64_t)p.bt.B * p.cache.Hkv * pl.tiles;
-    const int64_t grid = units * pl.ranges, rows = (int64_t)p.bt.B * p.cache.Hkv * p.bt.max_q * p.G;
+    // (whole rounds of the XCDs)
+    const int64_t grid = (units * pl.ranges + kNumXcd - 1) / kNumXcd * kNumXcd, rows = (int64_t)p.bt.B * p.cache.Hkv * p.bt.max_q * p.G;
     if (grid > 1 << 30 || rows > 1 << 30)
         return hipErrorInvalidValue;
-    hipError_t e = d == 64 ? (page == 64 ? fwd_go<64, 64>(p, e4m3, grid, s) : fwd_go<64, 128>(p, e4m3, grid, s))
-                           : (page == 64 ? fwd_go<128, 64>(p, e4m3, grid, s) : fwd_go<128, 128>(p, e4m3, grid, s));
+    hipError_t e = d == 64 ? (page == 64 ? fwd_go<64, 64>(p, pl.rows, e4m3, grid, s) : fwd_go<64, 128>(p, pl.rows, e4m3, grid, s))
+                           : (page == 64 ? fwd_go<128, 64>(p, pl.rows, e4m3, grid, s) : fwd_go<128, 128>(p, pl.rows, e4m3, grid, s));
     if (e == hipSuccess && pl.ranges > 1) {
         if (d == 64)
             hipLaunchKernelGGL(cache_merge<64>, dim3((unsigned)rows), dim3(256), 0, s, p, pl.rows);

@@ -39,17 +39,16 @@ __device__ inline int tile_visits(const FwdParams& p, const Seq& s, int tile, in
     return (seen + kVisit - 1) / kVisit;
 }
 
-// One 16-byte piece of a row's result.
+// Four channels of a row's result: acc / l (inv = 1 / l), in units of 2^m.
 template <int D>
-__device__ inline void write_row(const FwdParams& p, const Seq& s, int hk, int R, int piece, f32x4 acc, float l, float m)
+__device__ inline void write_row(const FwdParams& p, const Seq& s, int hk, int R, int piece, f32x4 acc, float l, float inv, float m)
 {
     const int i = R / p.G;
     const int64_t row = (int64_t)(s.first + i) * p.Hq + hk * p.G + (R - i * p.G);
     // (no key seen: l = 0, m = -inf)
-    const float inv = m == -INFINITY ? 0.f : 1.f / l;
 #pragma unroll
     for (int e = 0; e < 4; ++e)
-        acc[e] *= inv;
+        acc[e] = m == -INFINITY ? 0.f : acc[e] * inv;
     if (p.out_bf16) {
         const uint32_t lo = (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)acc[0]) |
                             (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)acc[1]) << 16;
@@ -138,6 +137,8 @@ __global__ void __launch_bounds__(256, 1) cache_fwd_kernel(FwdParams p)
 
     const int range = (int)(blockIdx.x % p.ranges);
     int rest = (int)(blockIdx.x / p.ranges);
+    if (rest >= p.bt.B * p.cache.Hkv * p.tiles)
+        return;
     const int tile = p.tiles - 1 - rest % p.tiles;      // (causal: the longest first)
     rest /= p.tiles;
     const int hk = rest % p.cache.Hkv, b = rest / p.cache.Hkv;
@@ -412,7 +413,7 @@ __global__ void __launch_bounds__(256, 1) cache_fwd_kernel(FwdParams p)
                 acc[c] += t[c];
         }
         if (whole) {
-            write_row<D>(p, s, hk, row0 + rr, piece, acc, l, mm);
+            write_row<D>(p, s, hk, row0 + rr, piece, acc, l, 1.f / l, mm);
         } else {
             *reinterpret_cast<f32x4*>(part + rr * D + 4 * piece) = acc;
             if (piece == 0) {
