@@ -116,7 +116,8 @@ int attn_fp8_cache_append(const attn_fp8_cache *cache, const attn_fp8_batch *bat
  *   out = sum_g 2^(M_g - 8) sum_t code_t v_t / l,  l = sum_t 2^(x_t) before the cast,
  * sums in FP32 relative to a power of two per row; lse = ln l.  A query that
  * sees no key gets out = 0 and lse = -inf.
- *   q          [T][Hq][d], BF16 or E4M3.
+ *   q          [T][Hq][d], BF16 or E4M3; Hq / Hkv at most 256, times max_q at most 2^24
+ *              (beyond: ATTN_ERR_UNSUPPORTED).
  *   out        contiguous [T][Hq][d], BF16 or F32 by out_type, 16-byte aligned.
  *   lse        FP32 [T][Hq], or NULL.
  *   sm_scale, q_descale   finite and > 0.

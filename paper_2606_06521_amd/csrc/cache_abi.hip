@@ -109,8 +109,9 @@ int check_attention(const attn_fp8_cache* c, const attn_fp8_batch* bt, int Hq, i
     if (Hq < 1 || Hq % c->Hkv != 0 || max_len < 0 || (causal != 0 && causal != 1) || !(sm_scale > 0.f) || !isfinite(sm_scale) ||
         !(q_descale > 0.f) || !isfinite(q_descale))
         return ATTN_ERR_INVALID_ARG;
-    // row numbers of a (sequence, KV head) stay inside int
-    return (int64_t)(Hq / c->Hkv) * bt->max_q > 1 << 28 ? ATTN_ERR_UNSUPPORTED : ATTN_OK;
+    // (the row numbers of a sequence and KV head times the group stay below 2^32)
+    const int G = Hq / c->Hkv;
+    return G > 256 || (int64_t)G * bt->max_q > 1 << 24 ? ATTN_ERR_UNSUPPORTED : ATTN_OK;
 }
 
 int longest(const attn_fp8_cache* c, const attn_fp8_batch* bt, int max_len)
@@ -227,11 +228,11 @@ int attn_fp8_cache_fwd(const attn_fp8_cache* cache, const attn_fp8_batch* batch,
     p.ws = static_cast<float*>(workspace);
     p.out_bf16 = out_type == ATTN_TYPE_BF16;
     p.Hq = Hq;
-    p.G = Hq / cache->Hkv;
+    p.gr = attn::group_of(Hq / cache->Hkv);
     p.causal = causal;
     p.max_len = longest(cache, batch, max_len);
     p.c = (float)(1.4426950408889634074 * (double)sm_scale * (double)q_descale);
-    const attn::FwdPlan pl = attn::cache_fwd_plan(batch->B, cache->Hkv, p.G, batch->max_q, p.max_len, cache->d, n_cu);
+    const attn::FwdPlan pl = attn::cache_fwd_plan(batch->B, cache->Hkv, p.gr.G, batch->max_q, p.max_len, cache->d, n_cu);
     if (pl.bytes > 0 && (!workspace || workspace_bytes < pl.bytes))
         return ATTN_ERR_INVALID_ARG;
     return status(attn::launch_cache_fwd(p, pl, cache->d, cache->page, q->type == ATTN_TYPE_E4M3, static_cast<hipStream_t>(stream)));
@@ -263,11 +264,14 @@ int attn_fp8_cache_weights(const attn_fp8_cache* cache, const attn_fp8_batch* ba
     p.sb = stride_b;
     p.sh = stride_h;
     p.Hq = Hq;
-    p.G = Hq / cache->Hkv;
+    p.gr = attn::group_of(Hq / cache->Hkv);
     p.causal = causal;
     p.max_len = most;
     p.c = (float)(1.4426950408889634074 * (double)sm_scale * (double)q_descale);
-    return status(attn::launch_cache_weights(p, cache->d, cache->page, q->type == ATTN_TYPE_E4M3, static_cast<hipStream_t>(stream)));
+    int n_cu = 0;
+    if ((st = device_cus(n_cu)) != ATTN_OK)
+        return st;
+    return status(attn::launch_cache_weights(p, cache->d, cache->page, q->type == ATTN_TYPE_E4M3, n_cu, static_cast<hipStream_t>(stream)));
 }
 
 int attn_fp8_cache_evict(const attn_fp8_cache* from, const attn_fp8_batch* batch, const attn_fp8_cache* to,

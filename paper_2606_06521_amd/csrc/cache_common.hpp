@@ -75,6 +75,15 @@ __device__ inline Seq uniform(const Seq& s)
             __builtin_amdgcn_readfirstlane(s.pos0)};
 }
 
+// Query rows of a (sequence, KV head): row R is head R % G of token R / G.
+struct Group {
+    int G;
+    uint32_t mul;           // ceil(2^32 / G) (G = 1: 0): exact for R G < 2^32
+    __device__ inline int token(int R) const { return mul ? (int)__umulhi((uint32_t)R, mul) : R; }
+};
+
+inline Group group_of(int G) { return {G, G == 1 ? 0u : (uint32_t)((((uint64_t)1 << 32) + G - 1) / G)}; }
+
 // Page of a sequence's block, -1 if there is none.
 __device__ inline int page_of(const Batch& bt, int n_pages, int b, int block)
 {
@@ -160,6 +169,68 @@ __device__ inline void store8(void* base, int64_t i, const float* x)
     }
 }
 
+namespace {
+
+// Buffer over `bytes` bytes at a uniform address (what lies behind them reads as
+// 0), as the instruction takes it.
+__device__ inline i32x4 bytes_buffer(const uint8_t* base, int bytes)
+{
+    const uint64_t a = (uint64_t)(uintptr_t)base;
+    return i32x4{__builtin_amdgcn_readfirstlane((int)(uint32_t)a), __builtin_amdgcn_readfirstlane((int)(uint32_t)(a >> 32) & 0xFFFF),
+                 __builtin_amdgcn_readfirstlane(bytes), 0x00027000};
+}
+
+// 16 bytes per lane from a buffer straight into LDS: lane i's to dst + 16 i.  As
+// inline assembly, so that the compiler does not make every LDS read wait for the
+// loads in flight (it cannot tell the stages apart); the kernel waits by vmcnt.
+__device__ inline void load_lds16(i32x4 buf, uint32_t voff, uint32_t soff, const uint8_t* dst)
+{
+    const uint32_t at = (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) uint8_t*)dst;
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds"
+                 :
+                 : "s"(__builtin_amdgcn_readfirstlane(at)), "v"(voff), "s"(buf),
+                   "s"(__builtin_amdgcn_readfirstlane(soff))
+                 : "memory");
+}
+
+// The same from an address per lane.
+__device__ inline void load_lds16(const uint8_t* src, const uint8_t* dst)
+{
+    const uint32_t at = (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) uint8_t*)dst;
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off"
+                 :
+                 : "s"(__builtin_amdgcn_readfirstlane(at)), "v"(src)
+                 : "memory");
+}
+
+__device__ inline i32x2 read_tr8(const uint8_t* p)
+{
+    return __builtin_amdgcn_ds_read_tr8_b64_v2i32((__attribute__((address_space(3))) i32x2*)(p));
+}
+
+// Eight E4M3 codes as bf16 (exact).
+__device__ inline bf16x8 widen(uint32_t a, uint32_t b)
+{
+    typedef __bf16 bf2 __attribute__((ext_vector_type(2)));
+    const bf2 x0 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, 1.0f, false), x1 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, 1.0f, true);
+    const bf2 x2 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, 1.0f, false), x3 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, 1.0f, true);
+    return bf16x8{x0[0], x0[1], x1[0], x1[1], x2[0], x2[1], x3[0], x3[1]};
+}
+
+// Eight channels of a query row as bf16.
+template <bool E4M3>
+__device__ inline bf16x8 load_q8(const void* q, int64_t at)
+{
+    if constexpr (E4M3) {
+        const i32x2 w = *reinterpret_cast<const i32x2*>(static_cast<const uint8_t*>(q) + at);
+        return widen((uint32_t)w[0], (uint32_t)w[1]);
+    } else {
+        return __builtin_bit_cast(bf16x8, *reinterpret_cast<const i32x4*>(static_cast<const uint16_t*>(q) + at));
+    }
+}
+
+}  // namespace
+
 // ---- host side ----
 
 struct FwdParams {
@@ -169,7 +240,8 @@ struct FwdParams {
     void* out;
     float* lse;             // nullable
     float* ws;              // partial results of split tiles
-    int out_bf16, Hq, G;    // G = Hq / Hkv
+    int out_bf16, Hq;
+    Group gr;               // G = Hq / Hkv
     int causal, max_len;
     float c;                // log2(e) sm_scale q_descale
     int tiles, chunk, ranges;   // row tiles per (sequence, KV head); visits per range; most ranges
@@ -182,7 +254,9 @@ struct WeightParams {
     const float* lse;
     float* w;
     int64_t sb, sh;
-    int Hq, G, causal, max_len;
+    int Hq;
+    Group gr;
+    int causal, max_len;
     float c;
 };
 
@@ -211,7 +285,7 @@ hipError_t launch_rope(const Heads& x, const Heads& out, int T, int H, int d, in
 hipError_t launch_append(const Batch& bt, const Cache& c, int d, int page, const Heads& k, const Heads& v, int type,
                          const Rotation& r, const Heads& q, const Heads& q_out, int Hq, hipStream_t s);
 hipError_t launch_cache_fwd(FwdParams p, const FwdPlan& plan, int d, int page, bool e4m3, hipStream_t s);
-hipError_t launch_cache_weights(const WeightParams& p, int d, int page, bool e4m3, hipStream_t s);
+hipError_t launch_cache_weights(const WeightParams& p, int d, int page, bool e4m3, int n_cu, hipStream_t s);
 hipError_t launch_cache_evict(const EvictParams& p, int d, int page, hipStream_t s);
 
 }  // namespace attn

@@ -20,10 +20,10 @@ __global__ void __launch_bounds__(256) cache_merge(FwdParams p, int tile_rows)
     __shared__ float lsh[PARTS];
     const int hk = (int)(blockIdx.x % p.cache.Hkv);
     int64_t rest = blockIdx.x / p.cache.Hkv;
-    const int per_seq = p.bt.max_q * p.G;
+    const int per_seq = p.bt.max_q * p.gr.G;
     const int b = (int)(rest / per_seq), R = (int)(rest - (int64_t)b * per_seq);
     const Seq s = sequence(p.bt, b, p.max_len);
-    if (R >= s.n * p.G)
+    if (R >= s.n * p.gr.G)
         return;
     const int tile = R / tile_rows;
     const int visits = tile_visits(p, s, tile, tile_rows);
@@ -110,7 +110,7 @@ hipError_t launch_cache_fwd(FwdParams p, const FwdPlan& pl, int d, int page, boo
     p.ranges = pl.ranges;
     const int64_t units = (int64_t)p.bt.B * p.cache.Hkv * pl.tiles;
     // (whole rounds of the XCDs)
-    const int64_t grid = (units * pl.ranges + kNumXcd - 1) / kNumXcd * kNumXcd, rows = (int64_t)p.bt.B * p.cache.Hkv * p.bt.max_q * p.G;
+    const int64_t grid = (units * pl.ranges + kNumXcd - 1) / kNumXcd * kNumXcd, rows = (int64_t)p.bt.B * p.cache.Hkv * p.bt.max_q * p.gr.G;
     if (grid > 1 << 30 || rows > 1 << 30)
         return hipErrorInvalidValue;
     hipError_t e = d == 64 ? (page == 64 ? fwd_go<64, 64>(p, pl.rows, e4m3, grid, s) : fwd_go<64, 128>(p, pl.rows, e4m3, grid, s))

@@ -34,8 +34,8 @@ constexpr float kSlack = 16.f;      // how far (log2) a group's maximum may exce
 // Visits of a tile: those that hold a key that its last row sees.
 __device__ inline int tile_visits(const FwdParams& p, const Seq& s, int tile, int tile_rows)
 {
-    const int last = min((tile + 1) * tile_rows, s.n * p.G) - 1;       // last row
-    const int seen = p.causal ? min(max(s.pos0 + last / p.G + 1, 0), s.len) : s.len;
+    const int last = min((tile + 1) * tile_rows, s.n * p.gr.G) - 1;       // last row
+    const int seen = p.causal ? min(max(s.pos0 + p.gr.token(last) + 1, 0), s.len) : s.len;
     return (seen + kVisit - 1) / kVisit;
 }
 
@@ -43,8 +43,8 @@ __device__ inline int tile_visits(const FwdParams& p, const Seq& s, int tile, in
 template <int D>
 __device__ inline void write_row(const FwdParams& p, const Seq& s, int hk, int R, int piece, f32x4 acc, float l, float inv, float m)
 {
-    const int i = R / p.G;
-    const int64_t row = (int64_t)(s.first + i) * p.Hq + hk * p.G + (R - i * p.G);
+    const int i = p.gr.token(R);
+    const int64_t row = (int64_t)(s.first + i) * p.Hq + hk * p.gr.G + (R - i * p.gr.G);
     // (no key seen: l = 0, m = -inf)
 #pragma unroll
     for (int e = 0; e < 4; ++e)
@@ -61,58 +61,6 @@ __device__ inline void write_row(const FwdParams& p, const Seq& s, int hk, int R
     if (p.lse && piece == 0)
         p.lse[row] = m == -INFINITY ? -INFINITY : (m + __builtin_log2f(l)) * 0.6931471805599453f;
 }
-
-namespace {
-
-// Buffer over `bytes` bytes at a uniform address (what lies behind them reads as
-// 0), as the instruction takes it.
-__device__ inline i32x4 bytes_buffer(const uint8_t* base, int bytes)
-{
-    const uint64_t a = (uint64_t)(uintptr_t)base;
-    return i32x4{__builtin_amdgcn_readfirstlane((int)(uint32_t)a), __builtin_amdgcn_readfirstlane((int)(uint32_t)(a >> 32) & 0xFFFF),
-                 __builtin_amdgcn_readfirstlane(bytes), 0x00027000};
-}
-
-// 16 bytes per lane from a buffer straight into LDS: lane i's to dst + 16 i.  As
-// inline assembly, so that the compiler does not make every LDS read wait for the
-// loads in flight (it cannot tell the stages apart); the kernel waits by vmcnt.
-__device__ inline void load_lds16(i32x4 buf, uint32_t voff, uint32_t soff, const uint8_t* dst)
-{
-    const uint32_t at = (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) uint8_t*)dst;
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds"
-                 :
-                 : "s"(__builtin_amdgcn_readfirstlane(at)), "v"(voff), "s"(buf),
-                   "s"(__builtin_amdgcn_readfirstlane(soff))
-                 : "memory");
-}
-
-__device__ inline i32x2 read_tr8(const uint8_t* p)
-{
-    return __builtin_amdgcn_ds_read_tr8_b64_v2i32((__attribute__((address_space(3))) i32x2*)(p));
-}
-
-// Eight E4M3 codes as bf16 (exact).
-__device__ inline bf16x8 widen(uint32_t a, uint32_t b)
-{
-    typedef __bf16 bf2 __attribute__((ext_vector_type(2)));
-    const bf2 x0 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, 1.0f, false), x1 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, 1.0f, true);
-    const bf2 x2 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, 1.0f, false), x3 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, 1.0f, true);
-    return bf16x8{x0[0], x0[1], x1[0], x1[1], x2[0], x2[1], x3[0], x3[1]};
-}
-
-// Eight channels of a query row as bf16.
-template <bool E4M3>
-__device__ inline bf16x8 load_q8(const void* q, int64_t at)
-{
-    if constexpr (E4M3) {
-        const i32x2 w = *reinterpret_cast<const i32x2*>(static_cast<const uint8_t*>(q) + at);
-        return widen((uint32_t)w[0], (uint32_t)w[1]);
-    } else {
-        return __builtin_bit_cast(bf16x8, *reinterpret_cast<const i32x4*>(static_cast<const uint16_t*>(q) + at));
-    }
-}
-
-}  // namespace
 
 template <int D, int PAGE, bool E4M3>
 __global__ void __launch_bounds__(256, 1) cache_fwd_kernel(FwdParams p)
@@ -143,7 +91,7 @@ __global__ void __launch_bounds__(256, 1) cache_fwd_kernel(FwdParams p)
     rest /= p.tiles;
     const int hk = rest % p.cache.Hkv, b = rest / p.cache.Hkv;
     const Seq s = uniform(sequence(p.bt, b, p.max_len));
-    const int rows = s.n * p.G;
+    const int rows = s.n * p.gr.G;
     const int row0 = tile * TR;
     if (row0 >= rows)
         return;
@@ -157,9 +105,9 @@ __global__ void __launch_bounds__(256, 1) cache_fwd_kernel(FwdParams p)
     const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int n = lane & 15, g = lane >> 4;
     const int row = row0 + n;
-    const int pos = row < rows ? (p.causal ? s.pos0 + row / p.G : s.len - 1) : -1;   // the last key the row sees
-    const int pos_min = p.causal ? s.pos0 + row0 / p.G : s.len - 1;
-    const int seen = p.causal ? min(max(s.pos0 + (min(row0 + TR, rows) - 1) / p.G + 1, 0), s.len) : s.len;
+    const int pos = row < rows ? (p.causal ? s.pos0 + p.gr.token(row) : s.len - 1) : -1;   // the last key the row sees
+    const int pos_min = p.causal ? s.pos0 + p.gr.token(row0) : s.len - 1;
+    const int seen = p.causal ? min(max(s.pos0 + p.gr.token(min(row0 + TR, rows) - 1) + 1, 0), s.len) : s.len;
 
     // the range's page numbers, then their scales
     const int np = max(v1 - v0, 0) * PPV;
@@ -223,8 +171,8 @@ __global__ void __launch_bounds__(256, 1) cache_fwd_kernel(FwdParams p)
     // Q^T fragments: k-step 2 i + e of lane (n, g): channels 64 i + 16 g + 8 e on
     bf16x8 qf[2 * KP];
     {
-        const int i = row / p.G;
-        const int64_t at = (int64_t)(s.first + i) * p.q.st + (int64_t)(hk * p.G + (row - i * p.G)) * p.q.sh;
+        const int i = p.gr.token(row);
+        const int64_t at = (int64_t)(s.first + i) * p.q.st + (int64_t)(hk * p.gr.G + (row - i * p.gr.G)) * p.q.sh;
 #pragma unroll
         for (int j = 0; j < 2 * KP; ++j)
             qf[j] = row < rows ? load_q8<E4M3>(p.q.data, at + 64 * (j / 2) + 16 * g + 8 * (j % 2)) : bf16x8{};

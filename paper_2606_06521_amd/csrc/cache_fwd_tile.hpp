@@ -53,7 +53,7 @@ __global__ void __launch_bounds__(256, 2) cache_fwd_tile_kernel(FwdParams p)
     rest /= p.ranges;
     const int hk = rest % p.cache.Hkv, b = rest / p.cache.Hkv;
     const Seq s = uniform(sequence(p.bt, b, p.max_len));
-    const int rows = s.n * p.G;
+    const int rows = s.n * p.gr.G;
     const int row0 = tile * TR;
     if (row0 >= rows)
         return;
@@ -68,9 +68,9 @@ __global__ void __launch_bounds__(256, 2) cache_fwd_tile_kernel(FwdParams p)
     const int n = lane & 31, h = lane >> 5;
     const int wrow0 = row0 + 32 * w;                    // the wave's first row
     const int row = wrow0 + n;
-    const int pos = row < rows ? (p.causal ? s.pos0 + row / p.G : s.len - 1) : -1;
-    const int pos_min = p.causal ? s.pos0 + wrow0 / p.G : s.len - 1;
-    const int seen = p.causal ? min(max(s.pos0 + (min(row0 + TR, rows) - 1) / p.G + 1, 0), s.len) : s.len;
+    const int pos = row < rows ? (p.causal ? s.pos0 + p.gr.token(row) : s.len - 1) : -1;
+    const int pos_min = p.causal ? s.pos0 + p.gr.token(wrow0) : s.len - 1;
+    const int seen = p.causal ? min(max(s.pos0 + p.gr.token(min(row0 + TR, rows) - 1) + 1, 0), s.len) : s.len;
 
     const int np = max(v1 - v0, 0) * PPV;
     for (int i = tid; i < np; i += 256) {
@@ -82,8 +82,8 @@ __global__ void __launch_bounds__(256, 2) cache_fwd_tile_kernel(FwdParams p)
     }
     bf16x8 qf[2 * KP];
     {
-        const int i = row / p.G;
-        const int64_t at = (int64_t)(s.first + i) * p.q.st + (int64_t)(hk * p.G + (row - i * p.G)) * p.q.sh;
+        const int i = p.gr.token(row);
+        const int64_t at = (int64_t)(s.first + i) * p.q.st + (int64_t)(hk * p.gr.G + (row - i * p.gr.G)) * p.q.sh;
 #pragma unroll
         for (int j = 0; j < 2 * KP; ++j)
             qf[j] = row < rows ? load_q8<E4M3>(p.q.data, at + 32 * (j / 2) + 16 * h + 8 * (j % 2)) : bf16x8{};

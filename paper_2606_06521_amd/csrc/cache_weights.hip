@@ -3,147 +3,377 @@
 //
 // D = Q K^T on the bf16 MFMA with the keys as columns: lane (n, g) holds rows
 // 4 g .. 4 g + 3 of a 16-row tile for key n, so the sum over rows stays in the
-// lane until the last row, and a key is owned by one wave: no atomics, one order
-// of sums.  A wave takes the 128 keys of a visit; their codes lie in its LDS
-// stage, widened to bf16 registers once for all row tiles.  With few rows it is
-// bound by the stream of K, with many by the exp2 of every (row, key).
+// lane until the last row, and a key is owned by one workgroup: no atomics, one
+// order of sums.
+//
+// Up to 64 rows (decode) the kernel streams K: a workgroup takes a range of
+// visits of 128 keys, each of its eight waves every eighth one; a visit's codes go
+// from their LDS stage to registers at once, so that the wave's next visit is on
+// its way while this one is computed with Q in registers (two waves on a SIMD: one
+// hides the other's latencies); the sums wait in LDS for one update of the weights
+// at the end.  What bounds it is the stream of K.  With more rows (chunks) a workgroup
+// takes one visit, widens its keys to bf16 registers once (64 keys a wave) and
+// runs over the rows 64 at a time, the next 64 on their way into the other of two
+// LDS stages, each wave two 16-row tiles of them; what bounds that is the exp2 of
+// every (row, key).
 #include "cache_common.hpp"
 
+#include <algorithm>
 #include <type_traits>
 
 namespace attn {
 
 namespace {
 
-__device__ inline bf16x8 widen_w(uint32_t a, uint32_t b)
+constexpr int kStreamChunk = 32;     // visits of a range
+constexpr int kStreamRows = 64;      // rows up to which K is streamed
+
+// Row R of a (sequence, KV head): its lse in units of log2 (none: +inf, whose
+// weights are 0) and the last key it sees (rows past the last: none).
+__device__ inline void row_of(const WeightParams& p, const Seq& s, int hk, int R, int rows, float& lse2, int& last)
 {
-    typedef __bf16 bf2 __attribute__((ext_vector_type(2)));
-    const bf2 x0 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, 1.0f, false), x1 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, 1.0f, true);
-    const bf2 x2 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, 1.0f, false), x3 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, 1.0f, true);
-    return bf16x8{x0[0], x0[1], x1[0], x1[1], x2[0], x2[1], x3[0], x3[1]};
+    const int at = min(R, rows - 1), i = p.gr.token(at);
+    const float x = p.lse[(int64_t)(s.first + i) * p.Hq + hk * p.gr.G + (at - i * p.gr.G)];
+    lse2 = x == -INFINITY ? INFINITY : x * 1.4426950408889634f;
+    last = R >= rows ? -1 : p.causal ? s.pos0 + i : s.len - 1;
 }
 
-template <int D, int PAGE, bool E4M3>
-__global__ void __launch_bounds__(256) cache_weights_kernel(WeightParams p, int visits)
+// Q operand of row R (past the last: any row): k-step 2 i + e of lane group g:
+// channels 64 i + 16 g + 8 e on.
+template <int KP, bool E4M3>
+__device__ inline void q_rows(const WeightParams& p, const Seq& s, int hk, int R, int rows, int g, bf16x8* qf)
 {
-    constexpr int NW = 4;
-    constexpr int KT = kVisit / 16, KP = D / 64;
-    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
-    const int n = lane & 15, g = lane >> 4;
-    const int groups = (visits + NW - 1) / NW;
-    const int v = (int)(blockIdx.x % groups) * NW + w;
-    const int rest = (int)(blockIdx.x / groups);
+    R = min(R, rows - 1);
+    const int i = p.gr.token(R);
+    const int64_t at = (int64_t)(s.first + i) * p.q.st + (int64_t)(hk * p.gr.G + (R - i * p.gr.G)) * p.q.sh;
+#pragma unroll
+    for (int j = 0; j < 2 * KP; ++j)
+        qf[j] = load_q8<E4M3>(p.q.data, at + 64 * (j / 2) + 16 * g + 8 * (j % 2));
+}
+
+__device__ inline float over_groups(float x)
+{
+    x += __shfl_xor(x, 16, 64);
+    return halves_sum(x);
+}
+
+// x[g]
+__device__ inline float of_group(int g, const float* x)
+{
+    const float lo = g & 1 ? x[1] : x[0], hi = g & 1 ? x[3] : x[2];
+    return g & 2 ? hi : lo;
+}
+
+// K stage: row r's chunk c at chunk c ^ swz(r): 16 rows in a row are read without bank conflicts.
+template <int D>
+__device__ inline int stage_swz(int r)
+{
+    return D == 128 ? r & 7 : (r >> 1) & 3;
+}
+
+template <int D, int PAGE, bool E4M3, int RT>
+__global__ void __launch_bounds__(512, 1) weights_stream_kernel(WeightParams p, int chunk, int ranges)
+{
+    constexpr int NW = 8, PPV = kVisit / PAGE, KT = kVisit / 16, KP = D / 64, CPR = D / 16;
+    constexpr int STAGE = kVisit * D, NI = STAGE / 1024, RPI = 1024 / D, IPP = NI / PPV;
+    __shared__ __attribute__((aligned(1024))) uint8_t lds[NW * STAGE];
+    __shared__ float acc_w[kStreamChunk * kVisit];
+    __shared__ int pids[kStreamChunk * PPV];
+    __shared__ uint8_t kbyte[kStreamChunk * PPV];
+
+    const int range = (int)(blockIdx.x % ranges);
+    const int rest = (int)(blockIdx.x / ranges);
     const int hk = rest % p.cache.Hkv, b = rest / p.cache.Hkv;
-    const Seq s = sequence(p.bt, b, p.max_len);
-    const int t0 = v * kVisit;
-    if (t0 >= s.len || s.n <= 0)
+    const Seq s = uniform(sequence(p.bt, b, p.max_len));
+    const int visits = (s.len + kVisit - 1) / kVisit;
+    const int v0 = range * chunk, v1 = min(v0 + chunk, visits);
+    if (v0 >= v1 || s.n <= 0)
         return;
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int n = lane & 15, g = lane >> 4;
+    const int rows = s.n * p.gr.G;
+    const int np = (v1 - v0) * PPV;
+    if (tid < np)
+        pids[tid] = page_of(p.bt, p.cache.n_pages, b, v0 * PPV + tid);
+    __syncthreads();
 
-    // K operand: key 16 kt + n, channels 64 i + 16 g on (two k-steps)
-    bf16x8 kf[KT][2 * KP];
-    float c[KT], sum[KT];
+    const int lr = lane / CPR, lc = lane % CPR;
+    const int k_off = lr * D + 16 * (lc ^ stage_swz<D>(lr));
+    uint8_t* const st = lds + w * STAGE;
+    auto issue = [&](int v) __attribute__((always_inline)) {
 #pragma unroll
-    for (int kt = 0; kt < KT; ++kt) {
-        const int t = t0 + 16 * kt + n;
-        const int pid = t < s.len ? page_of(p.bt, p.cache.n_pages, b, t / PAGE) : -1;
-        const size_t block = (size_t)(pid < 0 ? 0 : pid) * p.cache.Hkv + hk;
-        const uint8_t* row = p.cache.k + block * (PAGE * D) + (t % PAGE) * D;
-        // (no key: a scale of NaN marks it)
-        c[kt] = pid < 0 ? __builtin_nanf("") : __builtin_amdgcn_ldexpf(p.c, (int)p.cache.ks[block] - 127);
-        sum[kt] = 0.f;
+        for (int sub = 0; sub < PPV; ++sub) {
+            const int pid = v < v1 ? __builtin_amdgcn_readfirstlane(pids[(v - v0) * PPV + sub]) : -1;
+            const int left = pid < 0 ? 0 : min(max(s.len - (v * kVisit + sub * PAGE), 0), PAGE) * D;
+            const i32x4 kb = bytes_buffer(p.cache.k + ((size_t)(pid < 0 ? 0 : pid) * p.cache.Hkv + hk) * (PAGE * D), left);
 #pragma unroll
-        for (int i = 0; i < KP; ++i) {
-            const i32x4 x = pid < 0 ? i32x4{} : *reinterpret_cast<const i32x4*>(row + 64 * i + 16 * g);
-            kf[kt][2 * i] = widen_w((uint32_t)x[0], (uint32_t)x[1]);
-            kf[kt][2 * i + 1] = widen_w((uint32_t)x[2], (uint32_t)x[3]);
+            for (int j = 0; j < IPP; ++j)
+                load_lds16(kb, k_off, 1024 * j, st + 1024 * (sub * IPP + j));
         }
-    }
-
-    const int rows = s.n * p.G;
-    // (causal: the rows before the first that sees key t0 add nothing)
-    const int first = p.causal ? max(t0 - s.pos0, 0) * p.G / 16 : 0;
-    for (int tile = first; 16 * tile < rows; ++tile) {
-        const int row = 16 * tile + n;
-        bf16x8 qf[2 * KP];
-        {
-            const int i = row / p.G;
-            const int64_t at = (int64_t)(s.first + i) * p.q.st + (int64_t)(hk * p.G + (row - i * p.G)) * p.q.sh;
+    };
+    issue(v0 + w);
+    // (these loads are younger: they wait for the first visit too)
+    if (tid < np)
+        kbyte[tid] = pids[tid] < 0 ? 127 : p.cache.ks[(size_t)pids[tid] * p.cache.Hkv + hk];
+    bf16x8 qf[RT][2 * KP];
+    float lse2[RT][4];
+    int last[RT][4];
 #pragma unroll
-            for (int j = 0; j < 2 * KP; ++j) {
-                const int64_t e = at + 64 * (j / 2) + 16 * g + 8 * (j % 2);
-                if (row >= rows) {
-                    qf[j] = bf16x8{};
-                } else if constexpr (E4M3) {
-                    const i32x2 x = *reinterpret_cast<const i32x2*>(static_cast<const uint8_t*>(p.q.data) + e);
-                    qf[j] = widen_w((uint32_t)x[0], (uint32_t)x[1]);
-                } else {
-                    qf[j] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const i32x4*>(static_cast<const uint16_t*>(p.q.data) + e));
+    for (int t = 0; t < RT; ++t) {
+        q_rows<KP, E4M3>(p, s, hk, 16 * t + n, rows, g, qf[t]);
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+            row_of(p, s, hk, 16 * t + 4 * g + r, rows, lse2[t][r], last[t][r]);
+    }
+    // (used here, so that their wait is here and not in the loop)
+#pragma unroll
+    for (int t = 0; t < RT; ++t) {
+#pragma unroll
+        for (int j = 0; j < 2 * KP; ++j) {
+            i32x4 x = __builtin_bit_cast(i32x4, qf[t][j]);
+            asm volatile("" : "+v"(x));
+            qf[t][j] = __builtin_bit_cast(bf16x8, x);
+        }
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+            asm volatile("" : "+v"(lse2[t][r]));
+    }
+    __syncthreads();
+
+    for (int v = v0 + w; v < v1; v += NW) {
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        i32x4 raw[KT][KP];
+#pragma unroll
+        for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+            for (int i = 0; i < KP; ++i)
+                raw[kt][i] = *reinterpret_cast<const i32x4*>(st + (16 * kt + n) * D + 16 * ((4 * i + g) ^ stage_swz<D>(n)));
+        // (all in registers: the stage takes the next visit)
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        issue(v + NW);
+        float sum[KT];
+#pragma unroll
+        for (int kt = 0; kt < KT; ++kt) {
+            const float c = __builtin_amdgcn_ldexpf(p.c, (int)kbyte[(v - v0) * PPV + 16 * kt / PAGE] - 127);
+            bf16x8 kf[2 * KP];
+#pragma unroll
+            for (int i = 0; i < KP; ++i) {
+                kf[2 * i] = widen((uint32_t)raw[kt][i][0], (uint32_t)raw[kt][i][1]);
+                kf[2 * i + 1] = widen((uint32_t)raw[kt][i][2], (uint32_t)raw[kt][i][3]);
+            }
+            const int t = v * kVisit + 16 * kt + n;
+            sum[kt] = 0.f;
+#pragma unroll
+            for (int q = 0; q < RT; ++q) {
+                if (RT > 1 && 16 * q >= rows)
+                    break;
+                f32x4 acc = {};
+#pragma unroll
+                for (int j = 0; j < 2 * KP; ++j)
+                    acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(qf[q][j], kf[j], acc, 0, 0, 0);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(acc[r], c, -lse2[q][r]));
+                    sum[kt] += t <= last[q][r] ? x : 0.f;
                 }
             }
         }
-        // of the lane's four rows: lse in units of log2 (none: +inf, whose weights are 0), last key seen
-        float lse2[4];
-        int last[4];
+        // lane (n, g) keeps key n of tiles g and 4 + g: keys lane and 64 + lane
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const int R = 16 * tile + 4 * g + r, i = R / p.G;
-            lse2[r] = INFINITY;
-            last[r] = -1;
-            if (R < rows) {
-                const float x = p.lse[(int64_t)(s.first + i) * p.Hq + hk * p.G + (R - i * p.G)];
-                lse2[r] = x == -INFINITY ? INFINITY : x * 1.4426950408889634f;
-                last[r] = p.causal ? s.pos0 + i : s.len - 1;
-            }
-        }
+        for (int kt = 0; kt < KT; ++kt)
+            sum[kt] = over_groups(sum[kt]);
 #pragma unroll
-        for (int kt = 0; kt < KT; ++kt) {
-            f32x4 acc = {};
-#pragma unroll
-            for (int j = 0; j < 2 * KP; ++j)
-                acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(qf[j], kf[kt][j], acc, 0, 0, 0);
-            const int t = t0 + 16 * kt + n;
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(acc[r], c[kt], -lse2[r]));
-                sum[kt] += t <= last[r] ? x : 0.f;
-            }
-        }
+        for (int hf = 0; hf < 2; ++hf)
+            acc_w[(v - v0) * kVisit + 64 * hf + lane] = of_group(g, sum + 4 * hf);
     }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
     float* const out = p.w + (int64_t)b * p.sb + (int64_t)hk * p.sh;
+    for (int i = tid; i < (v1 - v0) * kVisit; i += 64 * NW) {
+        const int t = v0 * kVisit + i;
+        if (t < s.len && pids[i / PAGE] >= 0)
+            out[t] += acc_w[i];
+    }
+}
+
+template <int D, int PAGE, bool E4M3>
+__global__ void __launch_bounds__(256, 2) weights_tall_kernel(WeightParams p, int visits)
+{
+    constexpr int KT = 4, KP = D / 64, CPR = D / 16, PPV = kVisit / PAGE;
+    constexpr int STAGE = kVisit * D, LPW = STAGE / 1024 / 4;
+    constexpr int SEG = 64;                         // rows of a segment
+    constexpr int QROW = E4M3 ? D : 2 * D;          // bytes of a query row
+    constexpr int QC = QROW / 16, QRPI = 1024 / QROW, QLPW = 16 * QROW / 1024;   // chunks of a row, rows per load, loads of 16 rows
+    __shared__ __attribute__((aligned(1024))) uint8_t lds[STAGE];
+    __shared__ __attribute__((aligned(1024))) uint8_t qst[2][SEG * QROW];
+    __shared__ __attribute__((aligned(16))) float lse_s[2][SEG];
+    __shared__ __attribute__((aligned(16))) int last_s[2][SEG];
+    __shared__ float half_w[kVisit];
+    const int v = (int)(blockIdx.x % visits);       // (causal: the first keys have the most rows)
+    const int rest = (int)(blockIdx.x / visits);
+    const int hk = rest % p.cache.Hkv, b = rest / p.cache.Hkv;
+    const Seq s = uniform(sequence(p.bt, b, p.max_len));
+    const int t0 = v * kVisit;
+    if (t0 >= s.len || s.n <= 0)
+        return;
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int n = lane & 15, g = lane >> 4;
+    // the wave's keys: a half of the visit; its row tiles: two of a segment's four
+    const int kh = w & 1, rh = w >> 1;
+    const int rows = s.n * p.gr.G;
+    const int segs = (rows + SEG - 1) / SEG;
+    // (causal: the rows before the first that sees key t0 add nothing)
+    const int first = p.causal ? min(max(t0 - s.pos0, 0), s.n) * p.gr.G / SEG : 0;
+
+    // a wave loads 16 rows of a segment, row r's chunk c at chunk c ^ qswz(r)
+    auto qswz = [](int r) __attribute__((always_inline)) { return QROW >= 128 ? r & 7 : (r >> 1) & 3; };
+    auto issue_q = [&](int seg, int buf) __attribute__((always_inline)) {
+#pragma unroll
+        for (int j = 0; j < QLPW; ++j) {
+            const int r = 16 * w + QRPI * j + lane / QC;
+            // (rows past the last: any row, its weights are taken as 0)
+            const int R = min(SEG * seg + r, rows - 1), i = p.gr.token(R);
+            const int64_t at = (int64_t)(s.first + i) * p.q.st + (int64_t)(hk * p.gr.G + (R - i * p.gr.G)) * p.q.sh;
+            load_lds16(static_cast<const uint8_t*>(p.q.data) + at * (E4M3 ? 1 : 2) + 16 * ((lane % QC) ^ qswz(r)),
+                       qst[buf] + 16 * w * QROW + 1024 * j);
+        }
+    };
+    if (first < segs)
+        issue_q(first, 0);
+    // and 32 rows of K
+    const int lr = lane / CPR, lc = lane % CPR;
+    const int sub = PPV == 2 ? w >> 1 : 0;
+    const int lpid = __builtin_amdgcn_readfirstlane(page_of(p.bt, p.cache.n_pages, b, v * PPV + sub));
+    {
+        const int left = lpid < 0 ? 0 : min(max(s.len - (t0 + sub * PAGE), 0), PAGE) * D;
+        const i32x4 kb = bytes_buffer(p.cache.k + ((size_t)(lpid < 0 ? 0 : lpid) * p.cache.Hkv + hk) * (PAGE * D), left);
+        const int src = (32 * w - sub * PAGE) * D;
+#pragma unroll
+        for (int j = 0; j < LPW; ++j)
+            load_lds16(kb, lr * D + 16 * (lc ^ stage_swz<D>(lr)), src + 1024 * j, lds + w * (32 * D) + 1024 * j);
+    }
+    const int pid = __builtin_amdgcn_readfirstlane(page_of(p.bt, p.cache.n_pages, b, v * PPV + (PPV == 2 ? kh : 0)));
+    const float c = pid < 0 ? 0.f : __builtin_amdgcn_ldexpf(p.c, (int)p.cache.ks[(size_t)pid * p.cache.Hkv + hk] - 127);
+    float lse2 = 0.f;
+    int last = -1;
+    if (tid < SEG) {
+        row_of(p, s, hk, SEG * first + tid, rows, lse2, last);
+        lse_s[0][tid] = lse2;
+        last_s[0][tid] = last;
+    }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    bf16x8 kf[KT][2 * KP];
+    float sum[KT];
 #pragma unroll
     for (int kt = 0; kt < KT; ++kt) {
-        float x = sum[kt];
-        x += __shfl_xor(x, 16, 64);
-        x += __shfl_xor(x, 32, 64);
-        const int t = t0 + 16 * kt + n;
-        // (c = NaN: no page)
-        if (g == 0 && t < s.len && c[kt] == c[kt])
-            out[t] += x;
+        const int r = 64 * kh + 16 * kt + n;
+        sum[kt] = 0.f;
+#pragma unroll
+        for (int i = 0; i < KP; ++i) {
+            const i32x4 x = *reinterpret_cast<const i32x4*>(lds + r * D + 16 * ((4 * i + g) ^ stage_swz<D>(r)));
+            kf[kt][2 * i] = widen((uint32_t)x[0], (uint32_t)x[1]);
+            kf[kt][2 * i + 1] = widen((uint32_t)x[2], (uint32_t)x[3]);
+        }
     }
+    int buf = 0;
+    for (int seg = first; seg < segs; ++seg, buf ^= 1) {
+        if (seg + 1 < segs) {
+            if (tid < SEG)
+                row_of(p, s, hk, SEG * (seg + 1) + tid, rows, lse2, last);
+            issue_q(seg + 1, buf ^ 1);
+        }
+        // every row of the segment sees every key of the visit
+        const bool all = SEG * (seg + 1) <= rows && (!p.causal || s.pos0 + p.gr.token(SEG * seg) >= t0 + kVisit - 1) && t0 + kVisit <= s.len;
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+            const int r0 = 32 * rh + 16 * q;
+            bf16x8 qf[2 * KP];
+#pragma unroll
+            for (int i = 0; i < KP; ++i) {
+                const uint8_t* const at = qst[buf] + (r0 + n) * QROW;
+                if constexpr (E4M3) {
+                    const i32x4 x = *reinterpret_cast<const i32x4*>(at + 16 * ((4 * i + g) ^ qswz(n)));
+                    qf[2 * i] = widen((uint32_t)x[0], (uint32_t)x[1]);
+                    qf[2 * i + 1] = widen((uint32_t)x[2], (uint32_t)x[3]);
+                } else {
+                    qf[2 * i] = *reinterpret_cast<const bf16x8*>(at + 16 * ((8 * i + 2 * g) ^ qswz(n)));
+                    qf[2 * i + 1] = *reinterpret_cast<const bf16x8*>(at + 16 * ((8 * i + 2 * g + 1) ^ qswz(n)));
+                }
+            }
+            const f32x4 l4 = *reinterpret_cast<const f32x4*>(&lse_s[buf][r0 + 4 * g]);
+            const i32x4 e4 = *reinterpret_cast<const i32x4*>(&last_s[buf][r0 + 4 * g]);
+#pragma unroll
+            for (int kt = 0; kt < KT; ++kt) {
+                f32x4 acc = {};
+#pragma unroll
+                for (int j = 0; j < 2 * KP; ++j)
+                    acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(qf[j], kf[kt][j], acc, 0, 0, 0);
+                const int t = t0 + 64 * kh + 16 * kt + n;
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(acc[r], c, -l4[r]));
+                    sum[kt] += all || t <= e4[r] ? x : 0.f;
+                }
+            }
+        }
+        // the next segment is there, and everyone is done with this one
+        if (tid < SEG) {
+            lse_s[buf ^ 1][tid] = lse2;
+            last_s[buf ^ 1][tid] = last;
+        }
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        lds_barrier();
+    }
+#pragma unroll
+    for (int kt = 0; kt < KT; ++kt)
+        sum[kt] = over_groups(sum[kt]);
+    const float x = of_group(g, sum);
+    if (rh == 1)
+        half_w[64 * kh + lane] = x;
+    __syncthreads();
+    const int t = t0 + 64 * kh + lane;
+    if (rh == 0 && t < s.len && pid >= 0)
+        p.w[(int64_t)b * p.sb + (int64_t)hk * p.sh + t] += x + half_w[64 * kh + lane];
 }
 
 }  // namespace
 
-hipError_t launch_cache_weights(const WeightParams& p, int d, int page, bool e4m3, hipStream_t s)
+hipError_t launch_cache_weights(const WeightParams& p, int d, int page, bool e4m3, int n_cu, hipStream_t s)
 {
     const int visits = (p.max_len + kVisit - 1) / kVisit;
-    const int64_t grid = (int64_t)((visits + 3) / 4) * p.bt.B * p.cache.Hkv;
+    const int64_t heads = (int64_t)p.bt.B * p.cache.Hkv, rows = (int64_t)p.bt.max_q * p.gr.G;
+    const bool tall = rows > kStreamRows;
+    // ranges that fill the GPU, of at least a visit per wave
+    const int64_t want = std::max<int64_t>(1, n_cu / heads);
+    const int chunk = (int)std::min<int64_t>(std::max<int64_t>(8, (visits + want - 1) / want), kStreamChunk);
+    const int ranges = (visits + chunk - 1) / chunk;
+    const int64_t grid = heads * (tall ? visits : ranges);
     if (grid > 1 << 30)
         return hipErrorInvalidValue;
-    auto go = [&](auto kern) {
-        hipLaunchKernelGGL(kern, dim3((unsigned)grid), dim3(256), 0, s, p, visits);
+    auto by_type = [&](auto dc, auto pc, auto ec) {
+        constexpr int D = decltype(dc)::value, PAGE = decltype(pc)::value;
+        constexpr bool E = decltype(ec)::value;
+        if (tall)
+            hipLaunchKernelGGL((weights_tall_kernel<D, PAGE, E>), dim3((unsigned)grid), dim3(256), 0, s, p, visits);
+        else if (rows <= 16)
+            hipLaunchKernelGGL((weights_stream_kernel<D, PAGE, E, 1>), dim3((unsigned)grid), dim3(512), 0, s, p, chunk, ranges);
+        else
+            hipLaunchKernelGGL((weights_stream_kernel<D, PAGE, E, kStreamRows / 16>), dim3((unsigned)grid), dim3(512), 0, s, p, chunk,
+                               ranges);
         return hipGetLastError();
     };
-    auto by_type = [&](auto dc, auto pc) {
-        constexpr int D = decltype(dc)::value, PAGE = decltype(pc)::value;
-        return e4m3 ? go(cache_weights_kernel<D, PAGE, true>) : go(cache_weights_kernel<D, PAGE, false>);
-    };
     using std::integral_constant;
-    if (d == 64)
-        return page == 64 ? by_type(integral_constant<int, 64>{}, integral_constant<int, 64>{})
-                          : by_type(integral_constant<int, 64>{}, integral_constant<int, 128>{});
-    return page == 64 ? by_type(integral_constant<int, 128>{}, integral_constant<int, 64>{})
-                      : by_type(integral_constant<int, 128>{}, integral_constant<int, 128>{});
+    auto by_size = [&](auto ec) {
+        if (d == 64)
+            return page == 64 ? by_type(integral_constant<int, 64>{}, integral_constant<int, 64>{}, ec)
+                              : by_type(integral_constant<int, 64>{}, integral_constant<int, 128>{}, ec);
+        return page == 64 ? by_type(integral_constant<int, 128>{}, integral_constant<int, 64>{}, ec)
+                          : by_type(integral_constant<int, 128>{}, integral_constant<int, 128>{}, ec);
+    };
+    return e4m3 ? by_size(std::true_type{}) : by_size(std::false_type{});
 }
 
 }  // namespace attn
