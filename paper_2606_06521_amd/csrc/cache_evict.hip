@@ -1,11 +1,10 @@
 // Eviction: the tokens to keep of every (sequence, KV head), and their move into
 // new pages.
 //
-// Choice: the k-th largest weight by its bits, eight at a time (a histogram of
-// the weights that agree so far, in LDS), then one ordered pass that numbers the
-// kept tokens.  One workgroup per (sequence, head): the passes read 4 bytes per
-// token from L2 and are bound by their chain (four histograms, the ordered pass),
-// not by memory.  Move: one workgroup per new block, head, and K or V gathers the
+// Choice: the k-th largest weight by its bits, eleven at a time (a histogram of
+// the weights that agree so far, in LDS), then the kept tokens are numbered in
+// their order.  One workgroup per (sequence, head), which keeps up to 16384
+// weights in registers: bound by the chain of rounds, not by memory.  Move: one workgroup per new block, head, and K or V gathers the
 // block's rows into registers, takes their largest value and writes the codes.
 #include "cache_common.hpp"
 
@@ -16,6 +15,7 @@ namespace attn {
 namespace {
 
 constexpr int kPick = 1024;      // threads of a choosing workgroup
+constexpr int kDigit = 11;       // bits per round of the choice: 11, 11, 10
 
 // Order of the weights as unsigned numbers: NaN lowest, -0 equal to 0.
 __device__ inline uint32_t weight_key(float w)
@@ -26,20 +26,42 @@ __device__ inline uint32_t weight_key(float w)
     return (u >> 31) ? ~u : u | 0x80000000u;
 }
 
+// Inclusive sum over the lanes of a wave.
+__device__ inline uint32_t wave_scan(uint32_t x, int lane)
+{
+#pragma unroll
+    for (int off = 1; off < 64; off <<= 1) {
+        const uint32_t t = (uint32_t)__shfl_up((int)x, off, 64);
+        x += lane >= off ? t : 0u;
+    }
+    return x;
+}
+
+// E > 0: a thread keeps its E keys in registers (up to 1024 E tokens); E = 0: any
+// number, read again in every round.
+template <int E>
 __global__ void __launch_bounds__(kPick) evict_pick(EvictParams p, int max_len)
 {
-    constexpr int NW = kPick / 64;
-    __shared__ uint32_t hist[256];
-    __shared__ uint32_t wsum[2][NW];
-    __shared__ uint32_t found[2];
+    constexpr int NW = kPick / 64, BINS = 1 << kDigit, CAP = E > 0 ? E : 1;
+    __shared__ uint32_t hist[BINS];
+    __shared__ uint32_t wsum[NW], found[2];
+    __shared__ uint32_t tally[CAP * NW];
     const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
     const int hk = (int)(blockIdx.x % p.from.Hkv), b = (int)(blockIdx.x / p.from.Hkv);
+    const float* const w = p.w + (int64_t)b * p.sb + (int64_t)hk * p.sh;
     const int len = min(max(p.bt.lens[b], 0), max_len);
     const int m = min(len, p.budget);
-    const float* const w = p.w + (int64_t)b * p.sb + (int64_t)hk * p.sh;
     const size_t row = ((size_t)b * p.from.Hkv + hk) * p.budget;
     int32_t* const kept = p.kept + row;
     float* const nw = p.new_w ? p.new_w + row : nullptr;
+    float x[CAP];
+    if constexpr (E > 0) {
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            const int t = e * kPick + tid;
+            x[e] = t < len ? w[t] : 0.f;
+        }
+    }
     if (hk == 0 && tid == 0)
         p.new_lens[b] = m;
     for (int i = m + tid; i < p.budget; i += kPick) {
@@ -56,86 +78,140 @@ __global__ void __launch_bounds__(kPick) evict_pick(EvictParams p, int max_len)
         want = p.budget - lo - recent;
     }
     // the key of the last one kept, and how many equal to it
-    uint32_t key = 0;
-    uint32_t left = (uint32_t)want;
+    uint32_t key = 0, left = (uint32_t)want;
     if (want > 0) {
-        for (int shift = 24; shift >= 0; shift -= 8) {
-            if (tid < 256)
-                hist[tid] = 0u;
+#pragma unroll
+        for (int round = 0; round < 3; ++round) {
+            const int shift = round == 0 ? 21 : round == 1 ? 10 : 0, above = round == 1 ? 21 : 10;
+            const uint32_t mask = round == 2 ? 1023u : BINS - 1;
+            hist[tid] = 0u;
+            hist[tid + kPick] = 0u;
             __syncthreads();
-            for (int t = lo + tid; t < hi; t += kPick) {
-                const uint32_t k = weight_key(w[t]);
-                if (shift == 24 || (k >> (shift + 8)) == (key >> (shift + 8)))
-                    atomicAdd(&hist[(k >> shift) & 255], 1u);
+            auto count = [&](int t, float xt) __attribute__((always_inline)) {
+                const uint32_t k = weight_key(xt);
+                if (t >= lo && t < hi && (round == 0 || (k >> above) == (key >> above)))
+                    atomicAdd(&hist[(k >> shift) & mask], 1u);
+            };
+            if constexpr (E > 0) {
+#pragma unroll
+                for (int e = 0; e < E; ++e)
+                    count(e * kPick + tid, x[e]);
+            } else {
+                for (int t = lo + tid; t < hi; t += kPick)
+                    count(t, w[t]);
             }
             __syncthreads();
-            // from the top: the digit at which `left` are reached
-            if (tid < 64) {
-                uint32_t c[4], mine = 0;
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    c[j] = hist[255 - (4 * lane + j)];
-                    mine += c[j];
-                }
-                uint32_t before = mine;
-#pragma unroll
-                for (int off = 1; off < 64; off <<= 1) {
-                    const uint32_t t = (uint32_t)__shfl_up((int)before, off, 64);
-                    if (lane >= off)
-                        before += t;
-                }
-                before -= mine;
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    if (before < left && before + c[j] >= left) {
-                        found[0] = 255u - (4 * lane + j);
-                        found[1] = left - before;
-                    }
-                    before += c[j];
-                }
+            // from the top: the digit at which `left` are reached (two digits a thread)
+            const int top = BINS - 1 - 2 * tid;
+            const uint32_t c0 = hist[top], c1 = hist[top - 1];
+            uint32_t sum = wave_scan(c0 + c1, lane);
+            if (lane == 63)
+                wsum[wv] = sum;
+            __syncthreads();
+            uint32_t before = sum - (c0 + c1);
+            for (int i = 0; i < wv; ++i)
+                before += wsum[i];
+            if (before < left && before + c0 + c1 >= left) {
+                const bool second = before + c0 < left;
+                found[0] = (uint32_t)(second ? top - 1 : top);
+                found[1] = left - before - (second ? c0 : 0u);
             }
             __syncthreads();
             key |= found[0] << shift;
             left = found[1];
-            __syncthreads();
         }
     }
-    // number the kept ones in order
-    uint32_t base = 0, equal = 0;
-    for (int t0 = 0; t0 < len; t0 += kPick) {
-        const int t = t0 + tid;
-        const bool in = t < len, middle = in && t >= lo && t < hi;
-        const float x = in ? w[t] : 0.f;
-        const uint32_t k = weight_key(x);
-        const bool eq = middle && want > 0 && k == key;
-        const uint64_t eqs = __ballot(eq);
-        if (lane == 0)
-            wsum[0][wv] = (uint32_t)__popcll(eqs);
-        __syncthreads();
-        uint32_t eb = equal;
-        for (int i = 0; i < NW; ++i) {
-            const uint32_t c = wsum[0][i];
-            eb += i < wv ? c : 0u;
-            equal += c;
-        }
-        const uint64_t below = (1ull << lane) - 1;
-        const uint32_t erank = eb + (uint32_t)__popcll(eqs & below);
-        const bool keep = in && (!middle || (want > 0 && (k > key || (eq && erank < left))));
-        const uint64_t ks = __ballot(keep);
-        if (lane == 0)
-            wsum[1][wv] = (uint32_t)__popcll(ks);
-        __syncthreads();
-        uint32_t kb = base;
-        for (int i = 0; i < NW; ++i) {
-            const uint32_t c = wsum[1][i];
-            kb += i < wv ? c : 0u;
-            base += c;
-        }
-        const uint32_t at = kb + (uint32_t)__popcll(ks & below);
-        if (keep && at < (uint32_t)m) {
+    const uint64_t below = (1ull << lane) - 1;
+    auto put = [&](int t, float xt, uint32_t at) __attribute__((always_inline)) {
+        if (at < (uint32_t)m) {
             kept[at] = t;
             if (nw)
-                nw[at] = x;
+                nw[at] = xt;
+        }
+    };
+    if constexpr (E > 0) {
+        // per run of 64 tokens (e, wave) the number of equal ones, then of kept ones;
+        // their sums over the runs before it
+        auto scan = [&]() __attribute__((always_inline)) {
+            __syncthreads();
+            if (wv == 0) {
+                uint32_t base = 0;
+#pragma unroll
+                for (int i = 0; i < E * NW; i += 64) {
+                    const uint32_t c = i + lane < E * NW ? tally[i + lane] : 0u;
+                    const uint32_t s = wave_scan(c, lane);
+                    if (i + lane < E * NW)
+                        tally[i + lane] = base + s - c;
+                    base += (uint32_t)__shfl((int)s, 63, 64);
+                }
+            }
+            __syncthreads();
+        };
+        uint64_t eqs[E];
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            const int t = e * kPick + tid;
+            eqs[e] = __ballot(want > 0 && t >= lo && t < hi && weight_key(x[e]) == key);
+            if (lane == 0)
+                tally[e * NW + wv] = (uint32_t)__popcll(eqs[e]);
+        }
+        scan();
+        uint32_t keep = 0;
+        uint32_t mine[E];
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            const int t = e * kPick + tid;
+            const bool middle = t >= lo && t < hi, eq = (eqs[e] >> lane) & 1;
+            const uint32_t rank = tally[e * NW + wv] + (uint32_t)__popcll(eqs[e] & below);
+            const bool k = t < len && (!middle || (want > 0 && (weight_key(x[e]) > key || (eq && rank < left))));
+            keep |= (uint32_t)k << e;
+            const uint64_t ks = __ballot(k);
+            mine[e] = (uint32_t)__popcll(ks & below);
+            eqs[e] = ks;
+        }
+        __syncthreads();
+        if (lane == 0) {
+#pragma unroll
+            for (int e = 0; e < E; ++e)
+                tally[e * NW + wv] = (uint32_t)__popcll(eqs[e]);
+        }
+        scan();
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+            if ((keep >> e) & 1)
+                put(e * kPick + tid, x[e], tally[e * NW + wv] + mine[e]);
+    } else {
+        __shared__ uint32_t wcount[2][NW];
+        uint32_t base = 0, equal = 0;
+        for (int t0 = 0; t0 < len; t0 += kPick) {
+            const int t = t0 + tid;
+            const bool in = t < len, middle = in && t >= lo && t < hi;
+            const float xt = in ? w[t] : 0.f;
+            const uint32_t k = weight_key(xt);
+            const bool eq = middle && want > 0 && k == key;
+            const uint64_t eqs = __ballot(eq);
+            if (lane == 0)
+                wcount[0][wv] = (uint32_t)__popcll(eqs);
+            __syncthreads();
+            uint32_t rank = equal + (uint32_t)__popcll(eqs & below);
+            for (int i = 0; i < NW; ++i) {
+                const uint32_t c = wcount[0][i];
+                rank += i < wv ? c : 0u;
+                equal += c;
+            }
+            const bool keep = in && (!middle || (want > 0 && (k > key || (eq && rank < left))));
+            const uint64_t ks = __ballot(keep);
+            if (lane == 0)
+                wcount[1][wv] = (uint32_t)__popcll(ks);
+            __syncthreads();
+            uint32_t at = base + (uint32_t)__popcll(ks & below);
+            for (int i = 0; i < NW; ++i) {
+                const uint32_t c = wcount[1][i];
+                at += i < wv ? c : 0u;
+                base += c;
+            }
+            if (keep)
+                put(t, xt, at);
         }
     }
 }
@@ -161,23 +237,28 @@ __global__ void __launch_bounds__(256) evict_move(EvictParams p)
     const uint8_t* const src = is_v ? p.from.v : p.from.k;
     const uint8_t* const src_scale = is_v ? p.from.vs : p.from.ks;
     const int u = threadIdx.x % UPT, tk = threadIdx.x / UPT;
+    // (all rows' loads of a step at once: the chain is paid once, not per row)
     i32x4 code[NP];
-    int ex[NP];
+    int ex[NP], from[NP], tok[NP];
     float amax = 0.f;
 #pragma unroll
+    for (int q = 0; q < NP; ++q)
+        tok[q] = kept[min(q * TPP + tk, z - 1)];
+#pragma unroll
+    for (int q = 0; q < NP; ++q)
+        from[q] = page_of(p.bt, p.from.n_pages, b, max(tok[q], 0) / PAGE);
+#pragma unroll
     for (int q = 0; q < NP; ++q) {
-        const int slot = q * TPP + tk;
-        code[q] = i32x4{};
-        ex[q] = 0;
-        if (slot >= z)
-            continue;
-        const int t = kept[slot];
-        const int from = t < 0 ? -1 : page_of(p.bt, p.from.n_pages, b, t / PAGE);
-        if (from < 0)
-            continue;                               // (no page: zeros)
-        const size_t at = (size_t)from * p.from.Hkv + hk;
-        code[q] = *reinterpret_cast<const i32x4*>(src + at * (PAGE * D) + (t % PAGE) * D + 16 * u);
+        const size_t at = (size_t)max(from[q], 0) * p.from.Hkv + hk;
+        code[q] = *reinterpret_cast<const i32x4*>(src + at * (PAGE * D) + (max(tok[q], 0) % PAGE) * D + 16 * u);
         ex[q] = (int)src_scale[at] - 127;
+    }
+#pragma unroll
+    for (int q = 0; q < NP; ++q) {
+        if (from[q] < 0) {                          // (no page: zeros)
+            code[q] = i32x4{};
+            ex[q] = 0;
+        }
         float top = 0.f;
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
@@ -187,7 +268,7 @@ __global__ void __launch_bounds__(256) evict_move(EvictParams p)
             for (int e = 0; e < 4; ++e)
                 top = fmax_f(top, __builtin_fabsf(y[e]));   // (a NaN code does not count)
         }
-        amax = fmax_f(amax, __builtin_amdgcn_ldexpf(top, ex[q]));
+        amax = fmax_f(amax, q * TPP + tk < z ? __builtin_amdgcn_ldexpf(top, ex[q]) : 0.f);
     }
 #pragma unroll
     for (int off = 32; off > 0; off >>= 1)
@@ -230,7 +311,16 @@ hipError_t launch_cache_evict(const EvictParams& p, int d, int page, hipStream_t
     const int64_t heads = (int64_t)p.bt.B * p.from.Hkv, moves = heads * p.nb * 2;
     if (moves > 1 << 30)
         return hipErrorInvalidValue;
-    hipLaunchKernelGGL(evict_pick, dim3((unsigned)heads), dim3(kPick), 0, s, p, p.bt.W * page);
+    const int most = p.bt.W * page;
+    auto pick = [&](auto kern) { hipLaunchKernelGGL(kern, dim3((unsigned)heads), dim3(kPick), 0, s, p, most); };
+    if (most <= 4 * kPick)
+        pick(evict_pick<4>);
+    else if (most <= 8 * kPick)
+        pick(evict_pick<8>);
+    else if (most <= 16 * kPick)
+        pick(evict_pick<16>);
+    else
+        pick(evict_pick<0>);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess)
         return e;

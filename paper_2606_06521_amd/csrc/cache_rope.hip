@@ -18,22 +18,17 @@ __device__ inline void unit_at(const Rotation& r, bool rotates, int u, int& o1, 
     o2 = half ? 8 * u + r.rot / 2 : 16 * u + 8;
 }
 
-// cos and sin of the unit's eight pairs.
+// cos and sin of the unit's eight pairs (a position outside the table: NaN).
 __device__ inline void unit_table(const Rotation& r, int pos, int u, float* cs)
 {
-    if ((uint32_t)pos >= (uint32_t)r.n_pos) {
-#pragma unroll
-        for (int j = 0; j < 16; ++j)
-            cs[j] = __builtin_nanf("");
-        return;
-    }
-    const f32x4* t = reinterpret_cast<const f32x4*>(r.table + (int64_t)pos * r.rot + 16 * u);
+    const bool in = (uint32_t)pos < (uint32_t)r.n_pos;
+    const f32x4* t = reinterpret_cast<const f32x4*>(r.table + (int64_t)(in ? pos : 0) * r.rot + 16 * u);
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
         const f32x4 v = t[j];
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-            cs[4 * j + e] = v[e];
+            cs[4 * j + e] = in ? v[e] : __builtin_nanf("");
     }
 }
 
@@ -155,32 +150,38 @@ __global__ void __launch_bounds__(256) append_kernel(Batch bt, Cache cache, Head
     const bool rotates = !is_v && r.table && 16 * u < r.rot;
     int o1, o2;
     unit_at(r, rotates, u, o1, o2);
-    float val[NP][16];
-    float amax = 0.f;
+    // (all loads of a step at once: the chain is paid once, not per token; slots past
+    // the last new one read that one again)
+    float val[NP][16], cs[NP][16];
+    int pos[NP];
+    const int was = a > 0 ? (int)*scale - 127 : -128;
 #pragma unroll
     for (int p = 0; p < NP; ++p) {
-        const int slot = a + p * TPP + tk;
-        if (slot >= z)
-            continue;
+        const int slot = min(a + p * TPP + tk, z - 1);
         const int t = t0 + slot - s.pos0 + s.first;     // the packed token
         const int64_t at = (int64_t)t * x.st + (int64_t)h * x.sh;
+        pos[p] = rotates && r.positions ? r.positions[t] : t0 + slot;
         load8<TYPE>(x.data, at + o1, val[p]);
         load8<TYPE>(x.data, at + o2, val[p] + 8);
-        if (rotates) {
-            float cs[16];
-            unit_table(r, r.positions ? r.positions[t] : t0 + slot, u, cs);
-            rotate64(r, val[p], cs);
-        }
+    }
+    if (rotates) {
+#pragma unroll
+        for (int p = 0; p < NP; ++p)
+            unit_table(r, pos[p], u, cs[p]);
+#pragma unroll
+        for (int p = 0; p < NP; ++p)
+            rotate64(r, val[p], cs[p]);
+    }
+    float amax = 0.f;
+#pragma unroll
+    for (int p = 0; p < NP; ++p)
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
             const float m = __builtin_fabsf(val[p][e]);
-            if (m < __builtin_inff())
-                amax = fmax_f(amax, m);
-            else
-                val[p][e] = __builtin_nanf("");
+            const bool finite = m < __builtin_inff();
+            amax = fmax_f(amax, finite ? m : 0.f);
+            val[p][e] = finite ? val[p][e] : __builtin_nanf("");
         }
-    }
-    const int was = a > 0 ? (int)*scale - 127 : -128;
 #pragma unroll
     for (int off = 32; off > 0; off >>= 1)
         amax = fmax_f(amax, __shfl_xor(amax, off, 64));
