@@ -152,11 +152,13 @@ __global__ void __launch_bounds__(256) append_kernel(Batch bt, Cache cache, Head
     unit_at(r, rotates, u, o1, o2);
     // (all loads of a step at once: the chain is paid once, not per token; slots past
     // the last new one read that one again)
-    float val[NP][16], cs[NP][16];
+    float val[NP][16];
     int pos[NP];
     const int was = a > 0 ? (int)*scale - 127 : -128;
 #pragma unroll
     for (int p = 0; p < NP; ++p) {
+        if (p * TPP >= z - a)
+            break;
         const int slot = min(a + p * TPP + tk, z - 1);
         const int t = t0 + slot - s.pos0 + s.first;     // the packed token
         const int64_t at = (int64_t)t * x.st + (int64_t)h * x.sh;
@@ -166,15 +168,19 @@ __global__ void __launch_bounds__(256) append_kernel(Batch bt, Cache cache, Head
     }
     if (rotates) {
 #pragma unroll
-        for (int p = 0; p < NP; ++p)
-            unit_table(r, pos[p], u, cs[p]);
-#pragma unroll
-        for (int p = 0; p < NP; ++p)
-            rotate64(r, val[p], cs[p]);
+        for (int p = 0; p < NP; ++p) {
+            if (p * TPP >= z - a)
+                break;
+            float cs[16];
+            unit_table(r, pos[p], u, cs);
+            rotate64(r, val[p], cs);
+        }
     }
     float amax = 0.f;
 #pragma unroll
-    for (int p = 0; p < NP; ++p)
+    for (int p = 0; p < NP; ++p) {
+        if (p * TPP >= z - a)
+            break;
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
             const float m = __builtin_fabsf(val[p][e]);
@@ -182,6 +188,7 @@ __global__ void __launch_bounds__(256) append_kernel(Batch bt, Cache cache, Head
             amax = fmax_f(amax, finite ? m : 0.f);
             val[p][e] = finite ? val[p][e] : __builtin_nanf("");
         }
+    }
 #pragma unroll
     for (int off = 32; off > 0; off >>= 1)
         amax = fmax_f(amax, __shfl_xor(amax, off, 64));
