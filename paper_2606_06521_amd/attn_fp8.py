@@ -368,38 +368,47 @@ def kv_cache(n_pages, Hkv, d, *, page: int = 128, device="cuda"):
     return KVCache(codes(), codes(), scales(), scales())
 
 
+# (a short call is host time: one attribute of a tensor costs 0.05 to 0.2 us, and a
+# device as a number a third of a device as an object)
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+
+
 def _device(t):
-    if not t.is_cuda:
+    """The current device's number, which has to be the tensor's."""
+    i = t.get_device()
+    if i < 0:
         raise ValueError("tensors must be on the GPU")
-    if t.device.index != torch.cuda.current_device():
+    if i != _current_device():
         raise ValueError(f"tensors are on {t.device}, the current device is cuda:{torch.cuda.current_device()}")
-    return t.device
+    return i
 
 
 def _ints(t, shape, name, device):
-    if t.dtype != torch.int32 or tuple(t.shape) != shape or not t.is_contiguous() or t.device != device:
-        raise ValueError(f"{name} must be a contiguous int32 tensor {list(shape)} on {device}")
+    if t.dtype is not torch.int32 or t.shape != shape or not t.is_contiguous() or t.get_device() != device:
+        raise ValueError(f"{name} must be a contiguous int32 tensor {list(shape)} on cuda:{device}")
     return t.data_ptr()
 
 
 def _cache(cache, device):
     k, v, ks, vs = cache
-    shape = k.shape
-    if len(shape) != 4 or v.shape != shape or ks.shape != shape[:2] or vs.shape != shape[:2]:
+    shape, scales = k.shape, ks.shape
+    if (len(shape) != 4 or v.shape != shape or len(scales) != 2 or vs.shape != scales or scales[0] != shape[0]
+            or scales[1] != shape[1]):
         raise ValueError("a cache has k, v [pages, Hkv, page, d] and k_scale, v_scale [pages, Hkv]")
-    if k.dtype not in _FAST_V or v.dtype not in _FAST_V or ks.dtype != torch.uint8 or vs.dtype != torch.uint8:
+    if (k.dtype not in _FAST_V or v.dtype not in _FAST_V or ks.dtype is not torch.uint8
+            or vs.dtype is not torch.uint8):
         raise TypeError("a cache has float8_e4m3fn (or uint8) codes and uint8 scales")
-    for t in cache:
-        if t.device != device or not t.is_contiguous():
-            raise ValueError("a cache's tensors must be contiguous and on the inputs' device")
-    return attn_fp8_cache(k.data_ptr(), v.data_ptr(), ks.data_ptr(), vs.data_ptr(), shape[0], shape[1],
-                          shape[2], shape[3])
+    if not (k.get_device() == v.get_device() == ks.get_device() == vs.get_device() == device and k.is_contiguous()
+            and v.is_contiguous() and ks.is_contiguous() and vs.is_contiguous()):
+        raise ValueError("a cache's tensors must be contiguous and on the inputs' device")
+    return attn_fp8_cache(k.data_ptr(), v.data_ptr(), ks.data_ptr(), vs.data_ptr(), *shape)
 
 
 def _batch(pages, lens, cu, T, max_q, device):
-    if pages.dim() != 2:
+    shape = pages.shape
+    if len(shape) != 2:
         raise ValueError("pages must be [B, W]")
-    B, W = pages.shape
+    B, W = shape
     if cu is None:
         n = T // B if B else 0
         if B * n != T:
@@ -409,15 +418,16 @@ def _batch(pages, lens, cu, T, max_q, device):
             raise ValueError(f"max_q = {max_q}, but each sequence has {n} new tokens")
     elif max_q is None:
         raise ValueError("cu needs max_q, the most new tokens of a sequence")
-    return attn_fp8_batch(_ints(pages, (B, W), "pages", device), _ints(lens, (B,), "lens", device),
+    return attn_fp8_batch(_ints(pages, shape, "pages", device), _ints(lens, (B,), "lens", device),
                           None if cu is None else _ints(cu, (B + 1,), "cu", device), B, W, T, max(int(max_q), 1))
 
 
 def _heads(t, name, device, types):
-    if t.dim() != 3 or t.dtype not in types or t.device != device or (t.shape[2] > 1 and t.stride(2) != 1):
-        raise ValueError(f"{name} must be [T, H, d] with contiguous channels on {device}, of a type in "
+    shape, strides, dtype = t.shape, t.stride(), t.dtype
+    if len(shape) != 3 or dtype not in types or t.get_device() != device or (strides[2] != 1 and shape[2] > 1):
+        raise ValueError(f"{name} must be [T, H, d] with contiguous channels on cuda:{device}, of a type in "
                          f"{[str(x) for x in types]}")
-    return attn_fp8_heads(t.data_ptr(), t.stride(0), t.stride(1), _TYPES[t.dtype])
+    return attn_fp8_heads(t.data_ptr(), strides[0], strides[1], _TYPES[dtype])
 
 
 def _empty(shape, dtype, device, stream):
@@ -431,11 +441,12 @@ def _empty(shape, dtype, device, stream):
 
 
 def _rotation(table, positions, T, layout, device):
-    if (table.dim() != 3 or table.shape[2] != 2 or table.dtype != torch.float32 or not table.is_contiguous()
-            or table.device != device):
-        raise ValueError(f"table must be a contiguous float32 tensor [positions, rot / 2, 2] on {device}")
+    shape = table.shape
+    if (len(shape) != 3 or shape[2] != 2 or table.dtype is not torch.float32 or not table.is_contiguous()
+            or table.get_device() != device):
+        raise ValueError(f"table must be a contiguous float32 tensor [positions, rot / 2, 2] on cuda:{device}")
     p = None if positions is None else _ints(positions, (T,), "positions", device)
-    return attn_fp8_rotation(table.data_ptr(), p, table.shape[0], 2 * table.shape[1], LAYOUTS[layout])
+    return attn_fp8_rotation(table.data_ptr(), p, shape[0], 2 * shape[1], LAYOUTS[layout])
 
 
 _INPUTS = (torch.float32, torch.bfloat16, torch.float16)
@@ -481,8 +492,8 @@ def rope(x, table, positions, *, layout: str = "half", out=None, stream=None):
     row positions[t] of the table (rope_table); layout "half" pairs channel i with
     i + rot / 2, "interleaved" 2 i with 2 i + 1.  out may be x."""
     dev = _device(x)
-    T, H, d = x.shape if x.dim() == 3 else (0, 0, 0)
     hx = _heads(x, "x", dev, _INPUTS)
+    T, H, d = x.shape
     r = _rotation(table, positions, T, layout, dev)
     if out is None:
         out = _empty((T, H, d), x.dtype, dev, stream)
@@ -561,15 +572,15 @@ def cache_fwd(q, cache, pages, lens, *, cu=None, max_q=None, causal: bool = True
     dev, c, hq, T, Hq, d, bt, sm = _queries(q, cache, pages, lens, cu, max_q, sm_scale)
     if out is None:
         out = _empty((T, Hq, d), out_dtype, dev, stream)
-    elif out.shape != q.shape or not out.is_contiguous() or out.device != dev:
+    elif out.shape != q.shape or not out.is_contiguous() or out.get_device() != dev:
         raise ValueError("out must be a contiguous tensor of q's shape on its device")
     if out.dtype not in (torch.bfloat16, torch.float32):
         raise TypeError("out is bfloat16 or float32")
     if lse is None:
         lse = _empty((T, Hq), torch.float32, dev, stream) if want_lse else None
-    elif lse.shape != (T, Hq) or lse.dtype != torch.float32 or not lse.is_contiguous() or lse.device != dev:
+    elif lse.shape != (T, Hq) or lse.dtype != torch.float32 or not lse.is_contiguous() or lse.get_device() != dev:
         raise ValueError(f"lse must be a contiguous float32 tensor [{T}, {Hq}]")
-    n = _cache_workspace_bytes(dev.index, c.n_pages, c.Hkv, c.page, d, bt.B, bt.W, T, bt.max_q, Hq, int(max_len))
+    n = _cache_workspace_bytes(dev, c.n_pages, c.Hkv, c.page, d, bt.B, bt.W, T, bt.max_q, Hq, int(max_len))
     ws = _empty((n,), torch.uint8, dev, stream) if n else None
     st = _lib.attn_fp8_cache_fwd(c, bt, hq, Hq, out.data_ptr(), _TYPES[out.dtype], _ptr(lse), int(bool(causal)), sm,
                                  float(q_descale), int(max_len), _ptr(ws), n, _stream(stream))
@@ -579,13 +590,13 @@ def cache_fwd(q, cache, pages, lens, *, cu=None, max_q=None, causal: bool = True
 
 
 def _weights(weights, B, Hkv, least, device):
-    if (weights.dim() != 3 or weights.shape[:2] != (B, Hkv) or weights.shape[2] < least
-            or weights.dtype != torch.float32 or weights.device != device
+    if (weights.dim() != 3 or weights.shape[0] != B or weights.shape[1] != Hkv or weights.shape[2] < least
+            or weights.dtype != torch.float32 or weights.get_device() != device
             or (weights.shape[2] > 1 and weights.stride(2) != 1)
             or (Hkv > 1 and weights.stride(1) < weights.shape[2])
             or (B > 1 and weights.stride(0) < (Hkv - 1) * weights.stride(1) + weights.shape[2])):
         raise ValueError(f"weights must be float32 [{B}, {Hkv}, at least {least}] with contiguous rows that do not "
-                         f"overlap, on {device}")
+                         f"overlap, on cuda:{device}")
     return weights.data_ptr(), weights.stride(0), max(weights.stride(1), weights.shape[2])
 
 
@@ -595,7 +606,7 @@ def cache_weights(q, lse, cache, pages, lens, weights, *, cu=None, max_q=None, c
     max_len or W * page) the attention weight that each cached token receives from the
     new tokens q and the query heads of its group; lse is cache_fwd's for the same call."""
     dev, c, hq, T, Hq, d, bt, sm = _queries(q, cache, pages, lens, cu, max_q, sm_scale)
-    if lse.shape != (T, Hq) or lse.dtype != torch.float32 or not lse.is_contiguous() or lse.device != dev:
+    if lse.shape != (T, Hq) or lse.dtype != torch.float32 or not lse.is_contiguous() or lse.get_device() != dev:
         raise ValueError(f"lse must be a contiguous float32 tensor [{T}, {Hq}]")
     most = bt.W * c.page
     most = min(most, int(max_len)) if max_len else most
@@ -630,7 +641,7 @@ def cache_evict(cache, pages, lens, weights, to, new_pages, budget, *, n_sink: i
     new_lens = _empty((B,), torch.int32, dev, stream) if new_lens is None else new_lens
     new_weights = _empty(shape, torch.float32, dev, stream) if new_weights is None else new_weights
     if (new_weights.dtype != torch.float32 or tuple(new_weights.shape) != shape or not new_weights.is_contiguous()
-            or new_weights.device != dev):
+            or new_weights.get_device() != dev):
         raise ValueError(f"new_weights must be a contiguous float32 tensor {list(shape)}")
     st = _lib.attn_fp8_cache_evict(c, bt, ct, np_, p, sb, sh, int(budget), int(n_sink), int(n_recent),
                                    _ints(kept, shape, "kept", dev), _ints(new_lens, (B,), "new_lens", dev),
