@@ -21,7 +21,8 @@
  * of sequence b from cu[b] to cu[b + 1]: they are its last ones, token i of n is
  * position lens[b] - n + i.  cu = NULL: T / B tokens of each sequence.
  * lens, pages and cu are read on the device, so a captured call follows them:
- *   - lens[b] above W * page counts as W * page, below 0 as 0;
+ *   - lens[b] above W * page (at most 2^26, else ATTN_ERR_UNSUPPORTED) counts as
+ *     W * page, below 0 as 0;
  *   - a page number outside 0 .. n_pages - 1 is no page: its tokens are not
  *     written, and no query sees them;
  *   - a sequence has at most max_q new tokens; those beyond are left out (not

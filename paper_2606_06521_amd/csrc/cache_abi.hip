@@ -41,8 +41,8 @@ int check_sizes(const attn_fp8_cache* c, const attn_fp8_batch* bt)
         return ATTN_ERR_UNSUPPORTED;
     if (c->page != 64 && c->page != 128)
         return ATTN_ERR_UNSUPPORTED;
-    // token positions plus a visit stay inside int, element counts of a grid too
-    if ((int64_t)bt->W * c->page > 1 << 30 || c->Hkv > 1 << 16 || bt->max_q > 1 << 26)
+    // (the merge of a split call holds at most 4096 ranges)
+    if ((int64_t)bt->W * c->page > 1 << 26 || c->Hkv > 1 << 16 || bt->max_q > 1 << 26)
         return ATTN_ERR_UNSUPPORTED;
     return ATTN_OK;
 }

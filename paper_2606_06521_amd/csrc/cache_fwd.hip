@@ -8,6 +8,10 @@ namespace attn {
 
 namespace {
 
+// Ranges of a tile at most: 2^26 keys in ranges of kMaxChunk visits.
+constexpr int kMergeRanges = 4096;
+static_assert((1 << 26) / kVisit / kMaxChunk <= kMergeRanges && kTileChunk >= kMaxChunk);
+
 // Merge of a split tile: a workgroup per query row, thread (piece, part) takes
 // one 16-byte piece of the row from every PARTS-th range; the parts are added
 // through LDS in a fixed order.  Ranges stand at their own power of two; the
@@ -17,7 +21,7 @@ __global__ void __launch_bounds__(256) cache_merge(FwdParams p, int tile_rows)
 {
     constexpr int PIECES = D / 4, PARTS = 256 / PIECES;
     __shared__ f32x4 osh[PARTS][PIECES];
-    __shared__ float lsh[PARTS];
+    __shared__ float lsh[PARTS], msh[kMergeRanges], wave_max[4];
     const int hk = (int)(blockIdx.x % p.cache.Hkv);
     int64_t rest = blockIdx.x / p.cache.Hkv;
     const int per_seq = p.bt.max_q * p.gr.G;
@@ -34,20 +38,33 @@ __global__ void __launch_bounds__(256) cache_merge(FwdParams p, int tile_rows)
     const size_t stride = (size_t)tile_rows * (D + 2);
     const float* base = p.ws + (((size_t)b * p.cache.Hkv + hk) * p.tiles + tile) * p.ranges * stride;
     const int piece = threadIdx.x % PIECES, part = threadIdx.x / PIECES;
+    // the ranges' references, all loaded at once
     float m = -INFINITY;
-    for (int c = 0; c < n; ++c)
-        m = fmax_f(m, base[c * stride + tile_rows * (D + 1) + rr]);
+    for (int c = threadIdx.x; c < n; c += 256) {
+        const float x = base[c * stride + tile_rows * (D + 1) + rr];
+        msh[c] = x;
+        m = fmax_f(m, x);
+    }
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1)
+        m = fmax_f(m, __shfl_xor(m, off, 64));
+    m = halves_max(m);
+    if ((threadIdx.x & 63) == 0)
+        wave_max[threadIdx.x >> 6] = m;
+    __syncthreads();
+    m = fmax_f(fmax_f(wave_max[0], wave_max[1]), fmax_f(wave_max[2], wave_max[3]));
     f32x4 acc = {};
     float l = 0.f;
+#pragma unroll 4
     for (int c = part; c < n; c += PARTS) {
         const float* at = base + c * stride;
-        const float mc = at[tile_rows * (D + 1) + rr];
-        const float f = mc == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mc - m);
         const f32x4 x = *reinterpret_cast<const f32x4*>(at + rr * D + 4 * piece);
+        const float lc = at[tile_rows * D + rr], mc = msh[c];
+        const float f = mc == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mc - m);
 #pragma unroll
         for (int e = 0; e < 4; ++e)
             acc[e] += x[e] * f;
-        l += at[tile_rows * D + rr] * f;
+        l += lc * f;
     }
     osh[part][piece] = acc;
     if (piece == 0)
@@ -95,7 +112,7 @@ FwdPlan cache_fwd_plan(int B, int Hkv, int G, int max_q, int max_len, int d, int
     const int visits = (max_len + kVisit - 1) / kVisit;
     // enough ranges to fill the GPU (two workgroups of tall tiles fit a CU), none
     // shorter than two visits of a workgroup's four waves, or eight of a tall tile's
-    const int64_t want = std::max<int64_t>(1, (tall ? 2 : 1) * n_cu / std::max<int64_t>(units, 1));
+    const int64_t want = std::min<int64_t>(std::max<int64_t>(1, (tall ? 2 : 1) * n_cu / std::max<int64_t>(units, 1)), kMergeRanges);
     pl.chunk = (int)std::max<int64_t>(8, (visits + want - 1) / want);
     pl.chunk = std::min(pl.chunk, tall ? kTileChunk : kMaxChunk);
     pl.ranges = std::max(1, (visits + pl.chunk - 1) / pl.chunk);

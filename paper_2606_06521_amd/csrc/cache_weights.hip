@@ -203,7 +203,7 @@ __global__ void __launch_bounds__(256, 2) weights_tall_kernel(WeightParams p, in
     constexpr int KT = 4, KP = D / 64, CPR = D / 16, PPV = kVisit / PAGE;
     constexpr int STAGE = kVisit * D, LPW = STAGE / 1024 / 4;
     constexpr int SEG = 64;                         // rows of a segment
-    constexpr int QROW = E4M3 ? D : 2 * D;          // bytes of a query row
+    constexpr int QB = E4M3 ? 1 : 2, QROW = QB * D; // bytes of a query's element and row
     constexpr int QC = QROW / 16, QRPI = 1024 / QROW, QLPW = 16 * QROW / 1024;   // chunks of a row, rows per load, loads of 16 rows
     __shared__ __attribute__((aligned(1024))) uint8_t lds[STAGE];
     __shared__ __attribute__((aligned(1024))) uint8_t qst[2][SEG * QROW];
@@ -229,15 +229,30 @@ __global__ void __launch_bounds__(256, 2) weights_tall_kernel(WeightParams p, in
 
     // a wave loads 16 rows of a segment, row r's chunk c at chunk c ^ qswz(r)
     auto qswz = [](int r) __attribute__((always_inline)) { return QROW >= 128 ? r & 7 : (r >> 1) & 3; };
+    // (address and head of the lane's rows; from segment to segment they move on by 64
+    // rows without a division; rows past the last read row 0, their weights are 0)
+    const uint8_t* const q0 = static_cast<const uint8_t*>(p.q.data) + ((int64_t)s.first * p.q.st + (int64_t)hk * p.gr.G * p.q.sh) * QB;
+    const int step_i = p.gr.token(SEG), step_h = SEG - step_i * p.gr.G;
+    const int64_t step = (step_i * p.q.st + step_h * p.q.sh) * QB, carry = (p.q.st - p.gr.G * p.q.sh) * QB;
+    int64_t q_at[QLPW];
+    int q_head[QLPW];
+#pragma unroll
+    for (int j = 0; j < QLPW; ++j) {
+        const int r = 16 * w + QRPI * j + lane / QC, R = SEG * first + r, i = p.gr.token(R);
+        q_head[j] = R - i * p.gr.G;
+        q_at[j] = (i * p.q.st + q_head[j] * p.q.sh) * QB + 16 * ((lane % QC) ^ qswz(r));
+    }
     auto issue_q = [&](int seg, int buf) __attribute__((always_inline)) {
 #pragma unroll
         for (int j = 0; j < QLPW; ++j) {
-            const int r = 16 * w + QRPI * j + lane / QC;
-            // (rows past the last: any row, its weights are taken as 0)
-            const int R = min(SEG * seg + r, rows - 1), i = p.gr.token(R);
-            const int64_t at = (int64_t)(s.first + i) * p.q.st + (int64_t)(hk * p.gr.G + (R - i * p.gr.G)) * p.q.sh;
-            load_lds16(static_cast<const uint8_t*>(p.q.data) + at * (E4M3 ? 1 : 2) + 16 * ((lane % QC) ^ qswz(r)),
-                       qst[buf] + 16 * w * QROW + 1024 * j);
+            const bool in = SEG * seg + 16 * w + QRPI * j + lane / QC < rows;
+            load_lds16(q0 + (in ? q_at[j] : 0), qst[buf] + 16 * w * QROW + 1024 * j);
+            q_at[j] += step;
+            q_head[j] += step_h;
+            if (q_head[j] >= p.gr.G) {
+                q_head[j] -= p.gr.G;
+                q_at[j] += carry;
+            }
         }
     };
     if (first < segs)
@@ -287,38 +302,44 @@ __global__ void __launch_bounds__(256, 2) weights_tall_kernel(WeightParams p, in
         }
         // every row of the segment sees every key of the visit
         const bool all = SEG * (seg + 1) <= rows && (!p.causal || s.pos0 + p.gr.token(SEG * seg) >= t0 + kVisit - 1) && t0 + kVisit <= s.len;
+        auto tiles = [&](auto masked) __attribute__((always_inline)) {
 #pragma unroll
-        for (int q = 0; q < 2; ++q) {
-            const int r0 = 32 * rh + 16 * q;
-            bf16x8 qf[2 * KP];
+            for (int q = 0; q < 2; ++q) {
+                const int r0 = 32 * rh + 16 * q;
+                bf16x8 qf[2 * KP];
 #pragma unroll
-            for (int i = 0; i < KP; ++i) {
-                const uint8_t* const at = qst[buf] + (r0 + n) * QROW;
-                if constexpr (E4M3) {
-                    const i32x4 x = *reinterpret_cast<const i32x4*>(at + 16 * ((4 * i + g) ^ qswz(n)));
-                    qf[2 * i] = widen((uint32_t)x[0], (uint32_t)x[1]);
-                    qf[2 * i + 1] = widen((uint32_t)x[2], (uint32_t)x[3]);
-                } else {
-                    qf[2 * i] = *reinterpret_cast<const bf16x8*>(at + 16 * ((8 * i + 2 * g) ^ qswz(n)));
-                    qf[2 * i + 1] = *reinterpret_cast<const bf16x8*>(at + 16 * ((8 * i + 2 * g + 1) ^ qswz(n)));
+                for (int i = 0; i < KP; ++i) {
+                    const uint8_t* const at = qst[buf] + (r0 + n) * QROW;
+                    if constexpr (E4M3) {
+                        const i32x4 x = *reinterpret_cast<const i32x4*>(at + 16 * ((4 * i + g) ^ qswz(n)));
+                        qf[2 * i] = widen((uint32_t)x[0], (uint32_t)x[1]);
+                        qf[2 * i + 1] = widen((uint32_t)x[2], (uint32_t)x[3]);
+                    } else {
+                        qf[2 * i] = *reinterpret_cast<const bf16x8*>(at + 16 * ((8 * i + 2 * g) ^ qswz(n)));
+                        qf[2 * i + 1] = *reinterpret_cast<const bf16x8*>(at + 16 * ((8 * i + 2 * g + 1) ^ qswz(n)));
+                    }
+                }
+                const f32x4 l4 = *reinterpret_cast<const f32x4*>(&lse_s[buf][r0 + 4 * g]);
+                const i32x4 e4 = *reinterpret_cast<const i32x4*>(&last_s[buf][r0 + 4 * g]);
+#pragma unroll
+                for (int kt = 0; kt < KT; ++kt) {
+                    f32x4 acc = {};
+#pragma unroll
+                    for (int j = 0; j < 2 * KP; ++j)
+                        acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(qf[j], kf[kt][j], acc, 0, 0, 0);
+                    const int t = t0 + 64 * kh + 16 * kt + n;
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(acc[r], c, -l4[r]));
+                        sum[kt] += !decltype(masked)::value || t <= e4[r] ? x : 0.f;
+                    }
                 }
             }
-            const f32x4 l4 = *reinterpret_cast<const f32x4*>(&lse_s[buf][r0 + 4 * g]);
-            const i32x4 e4 = *reinterpret_cast<const i32x4*>(&last_s[buf][r0 + 4 * g]);
-#pragma unroll
-            for (int kt = 0; kt < KT; ++kt) {
-                f32x4 acc = {};
-#pragma unroll
-                for (int j = 0; j < 2 * KP; ++j)
-                    acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(qf[j], kf[kt][j], acc, 0, 0, 0);
-                const int t = t0 + 64 * kh + 16 * kt + n;
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(acc[r], c, -l4[r]));
-                    sum[kt] += all || t <= e4[r] ? x : 0.f;
-                }
-            }
-        }
+        };
+        if (all)
+            tiles(std::false_type{});
+        else
+            tiles(std::true_type{});
         // the next segment is there, and everyone is done with this one
         if (tid < SEG) {
             lse_s[buf ^ 1][tid] = lse2;

@@ -87,7 +87,7 @@ def rotation(A, **kw):
 # what every call of a cache and a batch refuses (kind, change, status)
 SIZES = [("c", dict(d=96), -2), ("c", dict(page=32), -2), ("c", dict(page=0), -1), ("c", dict(d=0), -1), ("c", dict(Hkv=0), -1),
          ("c", dict(n_pages=-1), -1), ("b", dict(B=-1), -1), ("b", dict(W=-1), -1), ("b", dict(T=-1), -1), ("b", dict(max_q=0), -1),
-         ("b", dict(W=1 << 24), -2), ("c", dict(k=None), -1), ("c", dict(v=None), -1), ("c", dict(ks=None), -1),
+         ("b", dict(W=1 << 24), -2), ("b", dict(W=(1 << 19) + 1), -2), ("c", dict(k=None), -1), ("c", dict(v=None), -1), ("c", dict(ks=None), -1),
          ("c", dict(vs=None), -1), ("c", dict(k=FAKE + 8), -1), ("c", dict(v=FAKE + 1), -1), ("b", dict(pages=None), -1),
          ("b", dict(lens=None), -1), ("b", dict(lens=FAKE + 2), -1), ("b", dict(pages=FAKE + 1), -1)]
 # and of the new tokens
