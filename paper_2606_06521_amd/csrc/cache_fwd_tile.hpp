@@ -141,6 +141,7 @@ __global__ void __launch_bounds__(256, 2) cache_fwd_tile_kernel(FwdParams p)
         const int sa[2] = {vbyte[pi], vbyte[pi + PPV - 1]};
         const bool there[2] = {pids[pi] >= 0, pids[pi + PPV - 1] >= 0};
         f32x16 sc[KT];
+        __builtin_amdgcn_s_setprio(1);
 #pragma unroll
         for (int kt = 0; kt < KT; ++kt) {
             const int r = krow + 32 * kt;
@@ -153,6 +154,7 @@ __global__ void __launch_bounds__(256, 2) cache_fwd_tile_kernel(FwdParams p)
             }
             sc[kt] = acc;
         }
+        __builtin_amdgcn_s_setprio(0);
         // ---- keys the row does not see ----
         const int t0 = v * kVisit;
         if (t0 + kVisit - 1 > pos_min || !there[0] || !there[1]) {
@@ -211,6 +213,7 @@ __global__ void __launch_bounds__(256, 2) cache_fwd_tile_kernel(FwdParams p)
             sb[kt] = max(127 - 8 + up, 0);
         }
         // ---- O^T += V^T P^T ----
+        __builtin_amdgcn_s_setprio(1);
 #pragma unroll
         for (int js = 0; js < KT / 2; ++js) {
             // the first group's scale from the lower half, the second's from the upper
@@ -231,6 +234,7 @@ __global__ void __launch_bounds__(256, 2) cache_fwd_tile_kernel(FwdParams p)
                 o[dt] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(av, bop, o[dt], 0, 0, 0, sa[js], 0, scale_b);
             }
         }
+        __builtin_amdgcn_s_setprio(0);
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     if (row >= rows)
