@@ -231,6 +231,51 @@ __device__ inline bf16x8 load_q8(const void* q, int64_t at)
 
 }  // namespace
 
+// The NaN codes of a word of four: 0x80 in their bytes.
+__device__ inline uint32_t nan_bytes(uint32_t w)
+{
+    return ((w & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u;
+}
+
+// Whether `bytes` (a multiple of 1024) of LDS hold a NaN code; the wave looks at all of them.
+__device__ inline bool holds_nan(const uint8_t* p, int bytes, int lane)
+{
+    uint32_t any = 0;
+    for (int i = 16 * lane; i < bytes; i += 1024) {
+        const i32x4 x = *reinterpret_cast<const i32x4*>(p + i);
+        any |= nan_bytes(x[0]) | nan_bytes(x[1]) | nan_bytes(x[2]) | nan_bytes(x[3]);
+    }
+    return __ballot(any != 0) != 0;
+}
+
+// Sets the NaN codes of `bytes` bytes of LDS to 0.
+__device__ inline void clear_nans(uint8_t* p, int bytes, int lane)
+{
+    for (int i = 16 * lane; i < bytes; i += 1024) {
+        i32x4 x = *reinterpret_cast<const i32x4*>(p + i);
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            x[j] &= (int)~((nan_bytes(x[j]) >> 7) * 255u);
+        *reinterpret_cast<i32x4*>(p + i) = x;
+    }
+}
+
+// An operand of E4M3 ones where `av` has NaN codes.
+__device__ inline i32x8 nan_ones(const i32x8& av)
+{
+    i32x8 x;
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        x[i] = (int)((nan_bytes(av[i]) >> 7) * 0x38u);
+    return x;
+}
+
+// Four E4M3 ones, the first `count` (at most 4) of them.
+__device__ inline int ones(int count)
+{
+    return (int)(0x38383838u & (uint32_t)((1ull << (8 * min(max(count, 0), 4))) - 1));
+}
+
 // ---- host side ----
 
 struct FwdParams {

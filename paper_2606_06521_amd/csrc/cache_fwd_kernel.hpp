@@ -296,8 +296,7 @@ __global__ void __launch_bounds__(256, 1) cache_fwd_kernel(FwdParams p)
         const int scale_b = (int)(g & 1 ? sw[1] : sw[0]);
         // ---- O^T += V^T P^T (this visit's V is older than the next one's K) ----
         asm volatile("s_waitcnt vmcnt(%0)" :: "n"(NI) : "memory");
-#pragma unroll
-        for (int dt = 0; dt < DT; ++dt) {
+        auto v_read = [&](int dt) __attribute__((always_inline)) {
             i32x8 av;
 #pragma unroll
             for (int u = 0; u < 4; ++u) {
@@ -305,6 +304,28 @@ __global__ void __launch_bounds__(256, 1) cache_fwd_kernel(FwdParams p)
                 av[2 * u] = t[0];
                 av[2 * u + 1] = t[1];
             }
+            return av;
+        };
+        // Where some rows see keys that others do not, a NaN of V must not reach the others
+        // by way of 0 times NaN: it makes NaN of the sums of the rows that see it, and goes.
+        if (t0 + kVisit - 1 > pos_min && pos_min + 1 < seen && holds_nan(vst, STAGE, lane)) {
+            i32x8 see;
+#pragma unroll
+            for (int kt = 0; kt < KT; ++kt)
+                see[kt] = ones(pos - t0 - 64 * (kt / 4) - 16 * g - 4 * (kt % 4) + 1);
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt) {
+                const f32x4 hits = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(nan_ones(v_read(dt)), see, f32x4{}, 0, 0, 0, 127, 0, 127);
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    o[dt][r] = hits[r] > 0.f ? __builtin_nanf("") : o[dt][r];
+            }
+            clear_nans(vst, STAGE, lane);
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        }
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) {
+            const i32x8 av = v_read(dt);
             o[dt] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(av, pk, o[dt], 0, 0, 0, sa, 0, scale_b);
         }
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");

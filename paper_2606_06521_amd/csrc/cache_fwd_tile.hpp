@@ -70,6 +70,7 @@ __global__ void __launch_bounds__(256, 2) cache_fwd_tile_kernel(FwdParams p)
     const int row = wrow0 + n;
     const int pos = row < rows ? (p.causal ? s.pos0 + p.gr.token(row) : s.len - 1) : -1;
     const int pos_min = p.causal ? s.pos0 + p.gr.token(wrow0) : s.len - 1;
+    const int tile_pos_min = p.causal ? s.pos0 + p.gr.token(row0) : s.len - 1;
     const int seen = p.causal ? min(max(s.pos0 + p.gr.token(min(row0 + TR, rows) - 1) + 1, 0), s.len) : s.len;
 
     const int np = max(v1 - v0, 0) * PPV;
@@ -131,10 +132,43 @@ __global__ void __launch_bounds__(256, 2) cache_fwd_tile_kernel(FwdParams p)
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         lds_barrier();
         issue(v + 1);
+        uint8_t* const kst = lds + (v & 1) * 2 * STAGE;
+        uint8_t* const vst = kst + STAGE;
+        const int t0 = v * kVisit;
+        auto v_read = [&](int js, int dt) __attribute__((always_inline)) {
+            i32x8 av;
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const i32x2 t = read_tr8(vst + (v_lane ^ (uint32_t)(dt << 5)) + (64 * js + 32 * (u / 2) + 8 * (u % 2)) * D);
+                av[2 * u] = t[0];
+                av[2 * u + 1] = t[1];
+            }
+            return av;
+        };
+        // Where some rows see keys that others do not, a NaN of V must not reach the others
+        // by way of 0 times NaN: it makes NaN of the sums of the rows that see it, and goes
+        // (every wave looks at the whole stage, so all take the same way).
+        if (t0 + kVisit - 1 > tile_pos_min && holds_nan(vst, STAGE, lane)) {
+#pragma unroll
+            for (int js = 0; js < KT / 2; ++js) {
+                i32x8 see;
+#pragma unroll
+                for (int q = 0; q < 8; ++q)
+                    see[q] = ones(pos - t0 - 64 * js - 32 * (q / 4) - 16 * h - 4 * (q % 4) + 1);
+#pragma unroll
+                for (int dt = 0; dt < DT; ++dt) {
+                    const f32x16 hits = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(nan_ones(v_read(js, dt)), see, f32x16{}, 0, 0, 0, 127, 0, 127);
+#pragma unroll
+                    for (int r = 0; r < 16; ++r)
+                        o[dt][r] = hits[r] > 0.f ? __builtin_nanf("") : o[dt][r];
+                }
+            }
+            lds_barrier();
+            clear_nans(vst + w * (32 * D), 32 * D, lane);
+            lds_barrier();
+        }
         if (wrow0 >= rows)
             continue;
-        const uint8_t* const kst = lds + (v & 1) * 2 * STAGE;
-        const uint8_t* const vst = kst + STAGE;
         const int pi = (v - v0) * PPV;
         const float c[2] = {__builtin_amdgcn_ldexpf(p.c, (int)kbyte[pi] - 127),
                             __builtin_amdgcn_ldexpf(p.c, (int)kbyte[pi + PPV - 1] - 127)};
@@ -156,7 +190,6 @@ __global__ void __launch_bounds__(256, 2) cache_fwd_tile_kernel(FwdParams p)
         }
         __builtin_amdgcn_s_setprio(0);
         // ---- keys the row does not see ----
-        const int t0 = v * kVisit;
         if (t0 + kVisit - 1 > pos_min || !there[0] || !there[1]) {
 #pragma unroll
             for (int kt = 0; kt < KT; ++kt) {
@@ -224,13 +257,7 @@ __global__ void __launch_bounds__(256, 2) cache_fwd_tile_kernel(FwdParams p)
                 bop[q] = pk[8 * js + q];
 #pragma unroll
             for (int dt = 0; dt < DT; ++dt) {
-                i32x8 av;
-#pragma unroll
-                for (int u = 0; u < 4; ++u) {
-                    const i32x2 t = read_tr8(vst + (v_lane ^ (uint32_t)(dt << 5)) + (64 * js + 32 * (u / 2) + 8 * (u % 2)) * D);
-                    av[2 * u] = t[0];
-                    av[2 * u + 1] = t[1];
-                }
+                const i32x8 av = v_read(js, dt);
                 o[dt] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(av, bop, o[dt], 0, 0, 0, sa[js], 0, scale_b);
             }
         }

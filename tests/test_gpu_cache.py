@@ -478,3 +478,52 @@ def test_calls_on_another_stream(A):
     out, lse = A.cache_fwd(q, gc, pages, lens, stream=s)
     s.synchronize()
     assert torch.equal(out, want) and torch.equal(lse, wl)
+
+
+# ---- values that are not finite ----
+
+@pytest.mark.parametrize("d,page,G,new", [(64, 64, 2, 6), (128, 128, 4, 20), (128, 64, 1, 130), (64, 128, 8, 40)])
+def test_fwd_nan_values_reach_the_rows_that_see_them(A, d, page, G, new):
+    """NaN codes of K and V in a chunk: rows before them are as without, rows from them on are NaN (V: in
+    the NaN's channel alone)."""
+    rng = np.random.default_rng(d + new)
+    n = 150 + new
+    c = R.make_cache(rng, 1, 1, page, d, [n])
+    q = R.make_queries(rng, new, G, d)
+    want, wl, bound, lb = R.attention(c, q, G)
+    t = n - new // 2                                   # a key that the first half of the rows does not see
+    pid, slot = int(c.pages[0, t // page]), t % page
+    log(f"nan d={d} page={page} G={G} new={new}")
+    first = t - (n - new)                              # the first row that sees it
+    c.v[pid, 0, slot, 5] = 0x7F
+    c.v[pid, 0, slot, d - 1] = 0xFF
+    out, lse, _ = run_fwd(A, c, q, G, "bf16", check=False)
+    o, l = out.cpu().double().numpy(), lse.cpu().double().numpy()
+    hit = np.zeros(o.shape, dtype=bool)
+    hit[first:, :, [5, d - 1]] = True
+    assert np.array_equal(np.isnan(o), hit)
+    within(np.where(hit, 0, o), np.where(hit, 0, want), bound)
+    within(l, wl, lb)
+    # a NaN in K: the rows that see it have a NaN score
+    c.k[pid, 0, slot, 3] = 0x7F
+    out, lse, _ = run_fwd(A, c, q, G, "bf16", check=False)
+    o, l = out.cpu().double().numpy(), lse.cpu().double().numpy()
+    assert np.isnan(o[first:]).all() and np.isnan(l[first:]).all()
+    within(o[:first], want[:first], bound[:first])
+    within(l[:first], wl[:first], lb[:first])
+
+
+def test_fwd_queries_that_are_not_finite_stay_in_their_rows(A):
+    rng = np.random.default_rng(77)
+    c = R.make_cache(rng, 2, 1, 64, 64, [300, 90])
+    q = R.make_queries(rng, 2, 4, 64)
+    want, wl, bound, lb = R.attention(c, q, 4)
+    t = R.torch_q(q, "bf16")
+    t[0, 1, 7], t[0, 2, 3], t[1, 0, 0] = float("nan"), float("inf"), float("-inf")
+    out, lse = A.cache_fwd(t.cuda(), dev_cache(A, c), dev(c.pages), dev(c.lens), out_dtype=torch.float32)
+    o, l = out.cpu().double().numpy(), lse.cpu().double().numpy()
+    bad = np.zeros((2, 4), dtype=bool)
+    bad[0, 1] = bad[0, 2] = bad[1, 0] = True
+    assert np.isnan(o[bad]).all() and np.isnan(l[bad]).all()
+    within(o[~bad], want[~bad], bound[~bad])
+    within(l[~bad], wl[~bad], lb[~bad])
