@@ -39,6 +39,24 @@ __device__ inline int tile_visits(const FwdParams& p, const Seq& s, int tile, in
     return (seen + kVisit - 1) / kVisit;
 }
 
+// Workgroup -> tile, range, KV head and sequence.  Tiles run fastest and each XCD
+// takes a contiguous run: the tiles that read the same keys share an L2.
+__device__ inline bool workgroup_of(const FwdParams& p, int& tile, int& range, int& hk, int& b)
+{
+    const int total = p.bt.B * p.cache.Hkv * p.ranges * p.tiles;
+    const int per_xcd = (total + kNumXcd - 1) / kNumXcd;
+    const int slot = (int)(blockIdx.x / kNumXcd), L = (int)(blockIdx.x % kNumXcd) * per_xcd + slot;
+    if (slot >= per_xcd || L >= total)
+        return false;
+    tile = p.tiles - 1 - L % p.tiles;           // (causal: the longest first)
+    int rest = L / p.tiles;
+    range = rest % p.ranges;
+    rest /= p.ranges;
+    hk = rest % p.cache.Hkv;
+    b = rest / p.cache.Hkv;
+    return true;
+}
+
 // Four channels of a row's result: acc / l (inv = 1 / l), in units of 2^m.
 template <int D>
 __device__ inline void write_row(const FwdParams& p, const Seq& s, int hk, int R, int piece, f32x4 acc, float l, float inv, float m)
@@ -83,13 +101,9 @@ __global__ void __launch_bounds__(256, 1) cache_fwd_kernel(FwdParams p)
     __shared__ uint8_t kbyte[kMaxChunk * PPV], vbyte[kMaxChunk * PPV];
     __shared__ float lsh[NW][TR], msh[NW][TR];
 
-    const int range = (int)(blockIdx.x % p.ranges);
-    int rest = (int)(blockIdx.x / p.ranges);
-    if (rest >= p.bt.B * p.cache.Hkv * p.tiles)
+    int tile, range, hk, b;
+    if (!workgroup_of(p, tile, range, hk, b))
         return;
-    const int tile = p.tiles - 1 - rest % p.tiles;      // (causal: the longest first)
-    rest /= p.tiles;
-    const int hk = rest % p.cache.Hkv, b = rest / p.cache.Hkv;
     const Seq s = uniform(sequence(p.bt, b, p.max_len));
     const int rows = s.n * p.gr.G;
     const int row0 = tile * TR;

@@ -40,18 +40,9 @@ __global__ void __launch_bounds__(256, 2) cache_fwd_tile_kernel(FwdParams p)
     __shared__ int pids[kTileChunk * PPV];
     __shared__ uint8_t kbyte[kTileChunk * PPV], vbyte[kTileChunk * PPV];
 
-    // workgroup -> (sequence, KV head, range, tile), each XCD a contiguous run: the
-    // tiles that read the same keys share an L2
-    const int total = p.bt.B * p.cache.Hkv * p.ranges * p.tiles;
-    const int per_xcd = (total + kNumXcd - 1) / kNumXcd;
-    const int L = (int)(blockIdx.x % kNumXcd) * per_xcd + (int)(blockIdx.x / kNumXcd);
-    if ((int)(blockIdx.x / kNumXcd) >= per_xcd || L >= total)
+    int tile, range, hk, b;
+    if (!workgroup_of(p, tile, range, hk, b))
         return;
-    const int tile = p.tiles - 1 - L % p.tiles;         // (causal: the longest first)
-    int rest = L / p.tiles;
-    const int range = rest % p.ranges;
-    rest /= p.ranges;
-    const int hk = rest % p.cache.Hkv, b = rest / p.cache.Hkv;
     const Seq s = uniform(sequence(p.bt, b, p.max_len));
     const int rows = s.n * p.gr.G;
     const int row0 = tile * TR;
