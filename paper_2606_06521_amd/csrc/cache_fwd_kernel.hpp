@@ -185,11 +185,12 @@ __global__ void __launch_bounds__(256, 1) cache_fwd_kernel(FwdParams p)
     // Q^T fragments: k-step 2 i + e of lane (n, g): channels 64 i + 16 g + 8 e on
     bf16x8 qf[2 * KP];
     {
-        const int i = p.gr.token(row);
-        const int64_t at = (int64_t)(s.first + i) * p.q.st + (int64_t)(hk * p.gr.G + (row - i * p.gr.G)) * p.q.sh;
+        // (rows past the last take its Q and are not written)
+        const int at_row = min(row, rows - 1), i = p.gr.token(at_row);
+        const int64_t at = (int64_t)(s.first + i) * p.q.st + (int64_t)(hk * p.gr.G + (at_row - i * p.gr.G)) * p.q.sh;
 #pragma unroll
         for (int j = 0; j < 2 * KP; ++j)
-            qf[j] = row < rows ? load_q8<E4M3>(p.q.data, at + 64 * (j / 2) + 16 * g + 8 * (j % 2)) : bf16x8{};
+            qf[j] = load_q8<E4M3>(p.q.data, at + 64 * (j / 2) + 16 * g + 8 * (j % 2));
     }
 #pragma unroll
     for (int c = 0; c < (kMaxChunk * PPV + 255) / 256; ++c) {

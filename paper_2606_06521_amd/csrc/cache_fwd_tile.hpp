@@ -65,21 +65,8 @@ __global__ void __launch_bounds__(256, 2) cache_fwd_tile_kernel(FwdParams p)
     const int seen = p.causal ? min(max(s.pos0 + p.gr.token(min(row0 + TR, rows) - 1) + 1, 0), s.len) : s.len;
 
     const int np = max(v1 - v0, 0) * PPV;
-    for (int i = tid; i < np; i += 256) {
-        const int pid = page_of(p.bt, p.cache.n_pages, b, v0 * PPV + i);
-        const size_t at = (size_t)(pid < 0 ? 0 : pid) * p.cache.Hkv + hk;
-        pids[i] = pid;
-        kbyte[i] = pid < 0 ? 127 : p.cache.ks[at];
-        vbyte[i] = pid < 0 ? 127 : p.cache.vs[at];
-    }
-    bf16x8 qf[2 * KP];
-    {
-        const int i = p.gr.token(row);
-        const int64_t at = (int64_t)(s.first + i) * p.q.st + (int64_t)(hk * p.gr.G + (row - i * p.gr.G)) * p.q.sh;
-#pragma unroll
-        for (int j = 0; j < 2 * KP; ++j)
-            qf[j] = row < rows ? load_q8<E4M3>(p.q.data, at + 32 * (j / 2) + 16 * h + 8 * (j % 2)) : bf16x8{};
-    }
+    for (int i = tid; i < np; i += 256)
+        pids[i] = page_of(p.bt, p.cache.n_pages, b, v0 * PPV + i);
     __syncthreads();
 
     const size_t block_bytes = (size_t)PAGE * D;
@@ -106,7 +93,23 @@ __global__ void __launch_bounds__(256, 2) cache_fwd_tile_kernel(FwdParams p)
         for (int j = 0; j < LPW; ++j)
             load_lds16(vb, v_off, src + 1024 * j, st + STAGE + 1024 * j);
     };
+    // the first visit's K and V travel while the scales and Q arrive
     issue(v0);
+    for (int i = tid; i < np; i += 256) {
+        const int pid = pids[i];
+        const size_t at = (size_t)(pid < 0 ? 0 : pid) * p.cache.Hkv + hk;
+        kbyte[i] = pid < 0 ? 127 : p.cache.ks[at];
+        vbyte[i] = pid < 0 ? 127 : p.cache.vs[at];
+    }
+    bf16x8 qf[2 * KP];
+    {
+        // (rows past the last take its Q and are not written)
+        const int at_row = min(row, rows - 1), i = p.gr.token(at_row);
+        const int64_t at = (int64_t)(s.first + i) * p.q.st + (int64_t)(hk * p.gr.G + (at_row - i * p.gr.G)) * p.q.sh;
+#pragma unroll
+        for (int j = 0; j < 2 * KP; ++j)
+            qf[j] = load_q8<E4M3>(p.q.data, at + 32 * (j / 2) + 16 * h + 8 * (j % 2));
+    }
 
     f32x16 o[DT];
 #pragma unroll
