@@ -427,17 +427,24 @@ def _heads(t, name, device, types):
     if len(shape) != 3 or dtype not in types or t.get_device() != device or (strides[2] != 1 and shape[2] > 1):
         raise ValueError(f"{name} must be [T, H, d] with contiguous channels on cuda:{device}, of a type in "
                          f"{[str(x) for x in types]}")
-    return attn_fp8_heads(t.data_ptr(), strides[0], strides[1], _TYPES[dtype])
+    # (a stride that no element is found by may be any number)
+    return attn_fp8_heads(t.data_ptr(), strides[0] if shape[0] > 1 else 0, strides[1] if shape[1] > 1 else 0,
+                          _TYPES[dtype])
 
 
 def _empty(shape, dtype, device, stream):
     """Memory that belongs to the stream the call runs on."""
     if stream is None:
-        return torch.empty(shape, dtype=dtype, device=device)
+        return torch.empty(shape, dtype=dtype, device=_cuda(device))
     if not isinstance(stream, torch.cuda.Stream):
         stream = torch.cuda.ExternalStream(stream.cuda_stream, device=device)
     with torch.cuda.stream(stream):
-        return torch.empty(shape, dtype=dtype, device=device)
+        return torch.empty(shape, dtype=dtype, device=_cuda(device))
+
+
+@functools.lru_cache(maxsize=None)
+def _cuda(index):
+    return torch.device("cuda", index)
 
 
 def _rotation(table, positions, T, layout, device):
@@ -497,9 +504,12 @@ def rope(x, table, positions, *, layout: str = "half", out=None, stream=None):
     r = _rotation(table, positions, T, layout, dev)
     if out is None:
         out = _empty((T, H, d), x.dtype, dev, stream)
+        ho = attn_fp8_heads(out.data_ptr(), H * d, d, hx.type)
     elif out.shape != x.shape:
         raise ValueError("out must have x's shape")
-    st = _lib.attn_fp8_rope(hx, _heads(out, "out", dev, (x.dtype,)), T, H, d, r, _stream(stream))
+    else:
+        ho = _heads(out, "out", dev, (x.dtype,))
+    st = _lib.attn_fp8_rope(hx, ho, T, H, d, r, _stream(stream))
     if st != ATTN_OK:
         raise AttnError(st)
     return out
@@ -525,14 +535,17 @@ def cache_append(cache, k, v, pages, lens, *, cu=None, max_q=None, table=None, p
     if q is not None:
         if r is None:
             raise ValueError("q is rotated along: that needs a table")
-        hq, Hq = _heads(q, "q", dev, (k.dtype,)), q.shape[1]
-        if q.shape[0] != T or q.shape[2] != c.d:
+        hq, shape = _heads(q, "q", dev, (k.dtype,)), q.shape
+        Hq = shape[1]
+        if shape[0] != T or shape[2] != c.d:
             raise ValueError(f"q must be [{T}, Hq, {c.d}]")
         if q_out is None:
-            q_out = _empty(tuple(q.shape), q.dtype, dev, stream)
-        elif q_out.shape != q.shape:
+            q_out = _empty(shape, q.dtype, dev, stream)
+            ho = attn_fp8_heads(q_out.data_ptr(), Hq * c.d, c.d, hq.type)
+        elif q_out.shape != shape:
             raise ValueError("q_out must have q's shape")
-        ho = _heads(q_out, "q_out", dev, (k.dtype,))
+        else:
+            ho = _heads(q_out, "q_out", dev, (k.dtype,))
     st = _lib.attn_fp8_cache_append(c, bt, hk, hv, r, hq, ho, Hq, _stream(stream))
     if st != ATTN_OK:
         raise AttnError(st)

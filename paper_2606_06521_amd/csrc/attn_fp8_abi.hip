@@ -23,7 +23,7 @@ __device__ __align__(256) uint8_t scratch[kScratchBytes];
 
 namespace {
 
-constexpr int kVersion = 630;   // 0.6.3: workspaces between the least and the reported size
+constexpr int kVersion = 700;   // 0.7.0: the KV cache (attn_fp8_cache.h)
 
 // Clears the diagnostic's output arrays on the caller's stream (a kernel, not
 // a memset node, so the call stays safe inside a captured graph).
@@ -441,7 +441,8 @@ const char* attn_fp8_strerror(int status)
                "256-byte aligned and not shorter than the least size of its shape (one of "
                "attn_fp8_kv_workspace_bytes always does)";
     case ATTN_ERR_UNSUPPORTED:
-        return "unsupported configuration (d and block_kv must be 64 or 128)";
+        return "unsupported configuration (d, block_kv and a cache's page must be 64 or 128, the rotated "
+               "channels a multiple of 16; sizes within the limits of the headers)";
     case ATTN_ERR_HIP:
         return "the HIP runtime rejected the kernel launch";
     case ATTN_ERR_SCRATCH:

@@ -527,3 +527,118 @@ def test_fwd_queries_that_are_not_finite_stay_in_their_rows(A):
     assert np.isnan(o[bad]).all() and np.isnan(l[bad]).all()
     within(o[~bad], want[~bad], bound[~bad])
     within(l[~bad], wl[~bad], lb[~bad])
+
+
+# ---- sizes and arguments at the edges ----
+
+def test_cache_beyond_four_gigabytes(A):
+    """Pages whose bytes lie past 2^32 of the arrays: append, attention, weights, eviction."""
+    rng = np.random.default_rng(91)
+    Hkv, page, d, n_pages = 8, 128, 128, 40000
+    c = R.make_cache(rng, 2, Hkv, page, d, [300, 140], extra=4)
+    # the small cache's pages at the end of a large one
+    big = [torch.empty((n_pages, Hkv, page, d), dtype=torch.uint8, device="cuda") for _ in range(2)]
+    scales = [torch.full((n_pages, Hkv), 127, dtype=torch.uint8, device="cuda") for _ in range(2)]
+    at = n_pages - c.n_pages
+    log(f"cache of {big[0].numel() / 2 ** 30:.1f} GiB")
+    assert at * Hkv * page * d > 1 << 32
+    for x, y in zip(big + scales, (c.k, c.v, c.ks, c.vs)):
+        x[at:] = dev(y)
+    gc = A.KVCache(*big, *scales)
+    pages = dev(np.where(c.pages >= 0, c.pages + at, -1).astype(np.int32))
+
+    def same():
+        same_cache([x[at:] for x in gc], c)
+
+    t = torch.from_numpy(rng.standard_normal((2, 2, Hkv, d))).bfloat16()
+    c.lens = c.lens + 1
+    A.cache_append(gc, t[0].cuda(), t[1].cuda(), pages, dev(c.lens))
+    c.append(t[0].double().numpy(), t[1].double().numpy())
+    same()
+    q = R.make_queries(rng, 2, Hkv, d)
+    out, lse = A.cache_fwd(R.torch_q(q, "bf16").cuda(), gc, pages, dev(c.lens), out_dtype=torch.float32)
+    want, wl, bound, lb = R.attention(c, q, 1)
+    # (the appended tokens are off the grid: their scores round to FP32)
+    within(out.cpu().double().numpy(), want, bound + 2e-4)
+    within(lse.cpu().double().numpy(), wl, lb + 1e-5)
+    w = torch.zeros((2, Hkv, pages.shape[1] * page), device="cuda")
+    A.cache_weights(R.torch_q(q, "bf16").cuda(), lse, gc, pages, dev(c.lens), w)
+    ww = R.weights(c, q, lse.cpu().numpy(), 1, w.shape[2])
+    within(w.cpu().double().numpy(), ww, 2.0 ** -16 * ww + 1e-12)
+    spare = np.array([p for p in range(c.n_pages) if p not in c.pages][:2], dtype=np.int32).reshape(2, 1)
+    kept, _, _ = A.cache_evict(gc, pages, dev(c.lens), w, gc, dev(spare + at), 100)
+    wk, _, _ = R.evict(c, w.cpu().numpy(), 100, 4, 0, c, spare)
+    assert np.array_equal(kept.cpu().numpy(), wk)
+    same()
+
+
+def test_token_offsets_outside_the_call(A):
+    """cu entries past T or in disorder: what lies inside is done, nothing outside is touched."""
+    rng = np.random.default_rng(92)
+    c = R.make_cache(rng, 3, 2, 64, 64, [70, 40, 9])
+    q = R.make_queries(rng, 5, 4, 64)
+    inside = np.array([0, 3, 5, 5], dtype=np.int32)
+    for cu in ([0, 3, 99, 1 << 30], [-4, 3, 5, 2]):
+        cu = np.array(cu, dtype=np.int32)
+        log(f"cu {cu.tolist()}")
+        out = torch.full((5, 4, 64), 7.0, device="cuda")
+        lse = torch.full((5, 4), 7.0, device="cuda")
+        A.cache_fwd(R.torch_q(q, "bf16").cuda(), dev_cache(A, c), dev(c.pages), dev(c.lens), cu=dev(cu), max_q=5, out=out, lse=lse)
+        want, wl, bound, lb = R.attention(c, q, 2, cu=inside)
+        within(out.cpu().double().numpy(), want, bound)
+        within(lse.cpu().double().numpy(), wl, lb)
+
+
+def test_strides_of_single_tokens_and_heads_are_not_looked_at(A):
+    rng = np.random.default_rng(93)
+    c = R.make_cache(rng, 1, 1, 64, 64, [50])
+    q = R.torch_q(R.make_queries(rng, 1, 1, 64), "bf16").cuda()
+    odd = torch.as_strided(q, (1, 1, 64), (3, 5, 1))
+    args = dev_cache(A, c), dev(c.pages), dev(c.lens)
+    assert torch.equal(A.cache_fwd(odd, *args)[0], A.cache_fwd(q, *args)[0])
+    t, pos = A.rope_table(8, 64), torch.tensor([3], dtype=torch.int32, device="cuda")
+    assert torch.equal(A.rope(odd, t, pos), A.rope(q, t, pos))
+
+
+def test_binding_refuses_what_does_not_fit(A):
+    """Checked before the library is called; nothing is launched."""
+    rng = np.random.default_rng(94)
+    c = R.make_cache(rng, 2, 2, 64, 64, [70, 40])
+    gc, pages, lens = dev_cache(A, c), dev(c.pages), dev(c.lens)
+    q = torch.zeros((2, 4, 64), dtype=torch.bfloat16, device="cuda")
+    k = torch.zeros((2, 2, 64), dtype=torch.bfloat16, device="cuda")
+    w = torch.zeros((2, 2, 128), device="cuda")
+    lse = torch.zeros((2, 4), device="cuda")
+    table, pos = A.rope_table(128, 64), torch.zeros(2, dtype=torch.int32, device="cuda")
+    cu = torch.tensor([0, 1, 2], dtype=torch.int32, device="cuda")
+    bad = [
+        lambda: A.cache_fwd(q.float(), gc, pages, lens), lambda: A.cache_fwd(q[:, :3], gc, pages, lens),
+        lambda: A.cache_fwd(q[..., :32], gc, pages, lens), lambda: A.cache_fwd(q, gc, pages.long(), lens),
+        lambda: A.cache_fwd(q, gc, pages, lens[:1]), lambda: A.cache_fwd(q, gc, pages, lens, cu=cu),
+        lambda: A.cache_fwd(q, gc, pages, lens, cu=cu[:2], max_q=1), lambda: A.cache_fwd(q, gc, pages, lens, max_q=0),
+        lambda: A.cache_fwd(q, gc, pages, lens, out=torch.empty((2, 4, 32), device="cuda")),
+        lambda: A.cache_fwd(q, gc, pages, lens, lse=lse.double()), lambda: A.cache_fwd(q, gc._replace(v=gc.k[:1]), pages, lens),
+        lambda: A.cache_fwd(q, gc._replace(k_scale=gc.k_scale[:, :1]), pages, lens),
+        lambda: A.cache_fwd(q.cpu(), gc, pages, lens), lambda: A.cache_fwd(q, gc._replace(k=gc.k.cpu()), pages, lens),
+        lambda: A.cache_fwd(q.repeat(2, 1, 1)[:3], gc, pages, lens),
+        lambda: A.cache_append(gc, k, k[:, :1], pages, lens), lambda: A.cache_append(gc, k, k.half(), pages, lens),
+        lambda: A.cache_append(gc, k, k, pages, lens, q=q), lambda: A.cache_append(gc, k, k, pages, lens, table=table, q=q[:1]),
+        lambda: A.cache_append(gc, k, k, pages, lens, table=table.double()),
+        lambda: A.cache_append(gc, k, k, pages, lens, table=table, positions=pos.long()),
+        lambda: A.cache_weights(q, lse, gc, pages, lens, w[:, :, :100]), lambda: A.cache_weights(q, lse[:1], gc, pages, lens, w),
+        lambda: A.cache_weights(q, lse, gc, pages, lens, w.double()),
+        lambda: A.cache_weights(q, lse, gc, pages, lens, w[:1].expand(2, 2, 128)),
+        lambda: A.cache_evict(gc, pages, lens, w, gc, pages, 64), lambda: A.cache_evict(gc, pages, lens, w, gc, pages[:, :1], 0),
+        lambda: A.cache_evict(gc, pages, lens, w, A.kv_cache(4, 2, 64, page=128), pages[:, :1].contiguous(), 64),
+        lambda: A.rope(q, table, pos.long()), lambda: A.rope(q, table[..., 0], pos), lambda: A.rope(q[0], table, pos),
+        lambda: A.rope(q, table, pos, out=q[:1]), lambda: A.rope(q.double(), table, pos),
+    ]
+    for i, call in enumerate(bad):
+        with pytest.raises((ValueError, TypeError)):
+            call()
+    for call in (lambda: A.cache_fwd(q, gc, pages, lens, sm_scale=0.0), lambda: A.cache_fwd(q, gc, pages, lens, max_len=-1),
+                 lambda: A.rope(q, A.rope_table(8, 8), pos), lambda: A.cache_append(gc, k, k, pages, lens, table=A.rope_table(8, 24))):
+        with pytest.raises(A.AttnError):
+            call()
+    with pytest.raises(KeyError):
+        A.rope(q, table, pos, layout="other")
