@@ -46,18 +46,16 @@ __device__ inline void rotate32(const Rotation& r, float* x, const float* cs)
     }
 }
 
-// A 64-bit value as FP32 with the last bit set where it is not exact: every
-// later rounding to fewer bits is that of the 64-bit value.
+// A 64-bit value as FP32 with the last bit set where it is not exact: every later
+// rounding to fewer bits is that of the 64-bit value (of at least 2^-126; smaller
+// ones round to FP32's subnormals first).
 __device__ inline float to_odd(double x)
 {
-    const float f = (float)x;
-    const double back = (double)f;
-    if (back == x || !(__builtin_fabs(x) < __builtin_inf()))
-        return f;
-    const uint32_t u = __float_as_uint(f);
-    if (u & 1)
-        return f;
-    return __uint_as_float(__builtin_fabs(x) > __builtin_fabs(back) ? u + 1 : u - 1);
+    uint64_t u = __builtin_bit_cast(uint64_t, x);
+    uint32_t lo = (uint32_t)u;
+    lo = (lo & 0xE0000000u) | (lo & 0x1FFFFFFFu ? 0x20000000u : 0u);
+    u = (u & 0xFFFFFFFF00000000ull) | lo;
+    return (float)__builtin_bit_cast(double, u);
 }
 
 __device__ inline void rotate64(const Rotation& r, float* x, const float* cs)
