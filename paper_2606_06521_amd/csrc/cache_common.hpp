@@ -276,6 +276,10 @@ __device__ inline int ones(int count)
     return (int)(0x38383838u & (uint32_t)((1ull << (8 * min(max(count, 0), 4))) - 1));
 }
 
+// Largest of scores; NaN if one is NaN (an instruction for two values; fmax would
+// first have to quieten each score).
+__device__ inline float max_of(float a, float b) { return __builtin_elementwise_maximum(a, b); }
+
 // ---- host side ----
 
 struct FwdParams {

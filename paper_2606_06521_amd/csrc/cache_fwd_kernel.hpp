@@ -260,7 +260,7 @@ __global__ void __launch_bounds__(256, 1) cache_fwd_kernel(FwdParams p)
             float mx = sc[4 * hf][0];
 #pragma unroll
             for (int i = 1; i < 16; ++i)
-                mx = fmax_f(mx, sc[4 * hf + i / 4][i % 4]);
+                mx = max_of(mx, sc[4 * hf + i / 4][i % 4]);
             const auto sw = __builtin_amdgcn_permlane16_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
             mx = fmax_f(__uint_as_float(sw[0]), __uint_as_float(sw[1]));
             // (all of them NaN: any M hands the NaN on)

@@ -200,7 +200,7 @@ __global__ void __launch_bounds__(256, 2) cache_fwd_tile_kernel(FwdParams p)
             float mx = sc[kt][0];
 #pragma unroll
             for (int r = 1; r < 16; ++r)
-                mx = fmax_f(mx, sc[kt][r]);
+                mx = max_of(mx, sc[kt][r]);
             mx = halves_max(mx);
             M[kt] = mx != mx ? 0.f : __builtin_ceilf(mx * c[kt / 2]);
         }
