@@ -126,7 +126,18 @@ __global__ void __launch_bounds__(512, 1) weights_stream_kernel(WeightParams p, 
         for (int r = 0; r < 4; ++r)
             row_of(p, s, hk, 16 * t + 4 * g + r, rows, lse2[t][r], last[t][r]);
     }
+    // the weights themselves, for the update at the end (one wait instead of one per entry)
+    float* const out = p.w + (int64_t)b * p.sb + (int64_t)hk * p.sh + v0 * kVisit;
+    constexpr int OWN = kStreamChunk * kVisit / (64 * NW);
+    const int n_out = min((v1 - v0) * kVisit, s.len - v0 * kVisit);
+    float old[OWN];
+#pragma unroll
+    for (int j = 0; j < OWN; ++j)
+        old[j] = tid + 64 * NW * j < n_out ? out[tid + 64 * NW * j] : 0.f;
     // (used here, so that their wait is here and not in the loop)
+#pragma unroll
+    for (int j = 0; j < OWN; ++j)
+        asm volatile("" : "+v"(old[j]));
 #pragma unroll
     for (int t = 0; t < RT; ++t) {
 #pragma unroll
@@ -189,11 +200,11 @@ __global__ void __launch_bounds__(512, 1) weights_stream_kernel(WeightParams p, 
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
-    float* const out = p.w + (int64_t)b * p.sb + (int64_t)hk * p.sh;
-    for (int i = tid; i < (v1 - v0) * kVisit; i += 64 * NW) {
-        const int t = v0 * kVisit + i;
-        if (t < s.len && pids[i / PAGE] >= 0)
-            out[t] += acc_w[i];
+#pragma unroll
+    for (int j = 0; j < OWN; ++j) {
+        const int i = tid + 64 * NW * j;
+        if (i < n_out && pids[i / PAGE] >= 0)
+            out[i] = old[j] + acc_w[i];
     }
 }
 
