@@ -603,14 +603,14 @@ def cache_fwd(q, cache, pages, lens, *, cu=None, max_q=None, causal: bool = True
 
 
 def _weights(weights, B, Hkv, least, device):
-    if (weights.dim() != 3 or weights.shape[0] != B or weights.shape[1] != Hkv or weights.shape[2] < least
-            or weights.dtype != torch.float32 or weights.get_device() != device
-            or (weights.shape[2] > 1 and weights.stride(2) != 1)
-            or (Hkv > 1 and weights.stride(1) < weights.shape[2])
-            or (B > 1 and weights.stride(0) < (Hkv - 1) * weights.stride(1) + weights.shape[2])):
+    shape = weights.shape
+    sb, sh, sn = weights.stride() if len(shape) == 3 else (0, 0, 0)
+    if (len(shape) != 3 or shape[0] != B or shape[1] != Hkv or shape[2] < least or weights.dtype is not torch.float32
+            or weights.get_device() != device or (sn != 1 and shape[2] > 1) or (Hkv > 1 and sh < shape[2])
+            or (B > 1 and sb < (Hkv - 1) * sh + shape[2])):
         raise ValueError(f"weights must be float32 [{B}, {Hkv}, at least {least}] with contiguous rows that do not "
                          f"overlap, on cuda:{device}")
-    return weights.data_ptr(), weights.stride(0), max(weights.stride(1), weights.shape[2])
+    return weights.data_ptr(), sb if B > 1 else 0, sh if Hkv > 1 else shape[2]
 
 
 def cache_weights(q, lse, cache, pages, lens, weights, *, cu=None, max_q=None, causal: bool = True, sm_scale=None,
@@ -650,15 +650,21 @@ def cache_evict(cache, pages, lens, weights, to, new_pages, budget, *, n_sink: i
     np_ = _ints(new_pages, (B, -(-budget // c.page)), "new_pages", dev)
     p, sb, sh = _weights(weights, B, c.Hkv, W * c.page, dev)
     shape = (B, c.Hkv, budget)
-    kept = _empty(shape, torch.int32, dev, stream) if kept is None else kept
-    new_lens = _empty((B,), torch.int32, dev, stream) if new_lens is None else new_lens
-    new_weights = _empty(shape, torch.float32, dev, stream) if new_weights is None else new_weights
-    if (new_weights.dtype != torch.float32 or tuple(new_weights.shape) != shape or not new_weights.is_contiguous()
+    if kept is None:
+        kept = _empty(shape, torch.int32, dev, stream)
+    else:
+        _ints(kept, shape, "kept", dev)
+    if new_lens is None:
+        new_lens = _empty((B,), torch.int32, dev, stream)
+    else:
+        _ints(new_lens, (B,), "new_lens", dev)
+    if new_weights is None:
+        new_weights = _empty(shape, torch.float32, dev, stream)
+    elif (new_weights.dtype != torch.float32 or new_weights.shape != shape or not new_weights.is_contiguous()
             or new_weights.get_device() != dev):
         raise ValueError(f"new_weights must be a contiguous float32 tensor {list(shape)}")
     st = _lib.attn_fp8_cache_evict(c, bt, ct, np_, p, sb, sh, int(budget), int(n_sink), int(n_recent),
-                                   _ints(kept, shape, "kept", dev), _ints(new_lens, (B,), "new_lens", dev),
-                                   new_weights.data_ptr(), _stream(stream))
+                                   kept.data_ptr(), new_lens.data_ptr(), new_weights.data_ptr(), _stream(stream))
     if st != ATTN_OK:
         raise AttnError(st)
     return kept, new_lens, new_weights

