@@ -4,7 +4,7 @@ The C entry points are exposed under their C names; ``fwd`` and
 ``p_underflow_count`` are thin conveniences that take torch tensors on the GPU,
 check their dtypes and shapes, allocate outputs with torch and pass the
 current torch stream; ``rope``, ``cache_append``, ``cache_fwd``, ``cache_weights``
-and ``cache_evict`` do the same for the KV cache.  Every step of the computation
+and ``cache_evict`` do the same for the KV cache, through a native module.  Every step of the computation
 runs in the HIP kernels; there is no fallback.  If the shared library is missing the import fails.
 """
 from __future__ import annotations
@@ -37,6 +37,7 @@ if not os.path.exists(LIB_PATH):
     raise ImportError(f"{LIB_PATH} is not built; run __graft_entry__.build() "
                       "(hipcc --offload-arch=gfx950)")
 _lib = ctypes.CDLL(LIB_PATH)
+from . import _cache_binding as _binding  # noqa: E402  (its symbols are the library's)
 
 _P, _I, _F, _Z = ctypes.c_void_p, ctypes.c_int, ctypes.c_float, ctypes.c_size_t
 _lib.attn_fp8_fwd.argtypes = [_P, _P, _P, _P, _P] + [_I] * 8 + [_F, _I, _P]
@@ -342,10 +343,10 @@ def block_gap_diag(q, k, v, *, S: float = 256.0, order: str = "reverse", causal:
     return hist, bz, counts
 
 
-# ---- the KV cache: torch conveniences ----
+# ---- the KV cache: torch conveniences (csrc/cache_binding.cpp checks the tensors, allocates
+# outputs and workspaces and passes the current stream) ----
 
-_TYPES = {torch.float32: ATTN_TYPE_F32, torch.bfloat16: ATTN_TYPE_BF16, torch.float16: ATTN_TYPE_F16,
-          torch.float8_e4m3fn: ATTN_TYPE_E4M3}
+_OUT_TYPES = {torch.float32: ATTN_TYPE_F32, torch.bfloat16: ATTN_TYPE_BF16}
 
 
 class KVCache(NamedTuple):
@@ -368,96 +369,19 @@ def kv_cache(n_pages, Hkv, d, *, page: int = 128, device="cuda"):
     return KVCache(codes(), codes(), scales(), scales())
 
 
-# (a short call is host time: one attribute of a tensor costs 0.05 to 0.2 us, and a
-# device as a number a third of a device as an object)
-_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
-
-
-def _device(t):
-    """The current device's number, which has to be the tensor's."""
-    i = t.get_device()
-    if i < 0:
-        raise ValueError("tensors must be on the GPU")
-    if i != _current_device():
-        raise ValueError(f"tensors are on {t.device}, the current device is cuda:{torch.cuda.current_device()}")
-    return i
-
-
-def _ints(t, shape, name, device):
-    if t.dtype is not torch.int32 or t.shape != shape or not t.is_contiguous() or t.get_device() != device:
-        raise ValueError(f"{name} must be a contiguous int32 tensor {list(shape)} on cuda:{device}")
-    return t.data_ptr()
-
-
-def _cache(cache, device):
-    k, v, ks, vs = cache
-    shape, scales = k.shape, ks.shape
-    if (len(shape) != 4 or v.shape != shape or len(scales) != 2 or vs.shape != scales or scales[0] != shape[0]
-            or scales[1] != shape[1]):
-        raise ValueError("a cache has k, v [pages, Hkv, page, d] and k_scale, v_scale [pages, Hkv]")
-    if (k.dtype not in _FAST_V or v.dtype not in _FAST_V or ks.dtype is not torch.uint8
-            or vs.dtype is not torch.uint8):
-        raise TypeError("a cache has float8_e4m3fn (or uint8) codes and uint8 scales")
-    if not (k.get_device() == v.get_device() == ks.get_device() == vs.get_device() == device and k.is_contiguous()
-            and v.is_contiguous() and ks.is_contiguous() and vs.is_contiguous()):
-        raise ValueError("a cache's tensors must be contiguous and on the inputs' device")
-    return attn_fp8_cache(k.data_ptr(), v.data_ptr(), ks.data_ptr(), vs.data_ptr(), *shape)
-
-
-def _batch(pages, lens, cu, T, max_q, device):
-    shape = pages.shape
-    if len(shape) != 2:
-        raise ValueError("pages must be [B, W]")
-    B, W = shape
-    if cu is None:
-        n = T // B if B else 0
-        if B * n != T:
-            raise ValueError(f"{T} tokens of {B} sequences: give cu")
-        max_q = n if max_q is None else max_q
-        if max_q < n:
-            raise ValueError(f"max_q = {max_q}, but each sequence has {n} new tokens")
-    elif max_q is None:
-        raise ValueError("cu needs max_q, the most new tokens of a sequence")
-    return attn_fp8_batch(_ints(pages, shape, "pages", device), _ints(lens, (B,), "lens", device),
-                          None if cu is None else _ints(cu, (B + 1,), "cu", device), B, W, T, max(int(max_q), 1))
-
-
-def _heads(t, name, device, types):
-    shape, strides, dtype = t.shape, t.stride(), t.dtype
-    if len(shape) != 3 or dtype not in types or t.get_device() != device or (strides[2] != 1 and shape[2] > 1):
-        raise ValueError(f"{name} must be [T, H, d] with contiguous channels on cuda:{device}, of a type in "
-                         f"{[str(x) for x in types]}")
-    # (a stride that no element is found by may be any number)
-    return attn_fp8_heads(t.data_ptr(), strides[0] if shape[0] > 1 else 0, strides[1] if shape[1] > 1 else 0,
-                          _TYPES[dtype])
-
-
-def _empty(shape, dtype, device, stream):
-    """Memory that belongs to the stream the call runs on."""
+def _call(stream, f, *args):
+    """A call of the native binding, on `stream` (outputs and workspace belong to it) or
+    the current one."""
     if stream is None:
-        return torch.empty(shape, dtype=dtype, device=_cuda(device))
-    if not isinstance(stream, torch.cuda.Stream):
-        stream = torch.cuda.ExternalStream(stream.cuda_stream, device=device)
-    with torch.cuda.stream(stream):
-        return torch.empty(shape, dtype=dtype, device=_cuda(device))
-
-
-@functools.lru_cache(maxsize=None)
-def _cuda(index):
-    return torch.device("cuda", index)
-
-
-def _rotation(table, positions, T, layout, device):
-    shape = table.shape
-    if (len(shape) != 3 or shape[2] != 2 or table.dtype is not torch.float32 or not table.is_contiguous()
-            or table.get_device() != device):
-        raise ValueError(f"table must be a contiguous float32 tensor [positions, rot / 2, 2] on cuda:{device}")
-    p = None if positions is None else _ints(positions, (T,), "positions", device)
-    return attn_fp8_rotation(table.data_ptr(), p, shape[0], 2 * shape[1], LAYOUTS[layout])
-
-
-_INPUTS = (torch.float32, torch.bfloat16, torch.float16)
-_QUERIES = (torch.bfloat16, torch.float8_e4m3fn)
+        r = f(*args)
+    else:
+        if not isinstance(stream, torch.cuda.Stream):
+            stream = torch.cuda.ExternalStream(stream.cuda_stream)
+        with torch.cuda.stream(stream):
+            r = f(*args)
+    if type(r) is int:
+        raise AttnError(r)
+    return r
 
 
 def rope_table(n_pos, rot, *, base: float = 10000.0, scaling: str = "none", factor: float = 1.0,
@@ -498,21 +422,7 @@ def rope(x, table, positions, *, layout: str = "half", out=None, stream=None):
     and heads that are multiples of 16 bytes) with its first rot channels rotated by
     row positions[t] of the table (rope_table); layout "half" pairs channel i with
     i + rot / 2, "interleaved" 2 i with 2 i + 1.  out may be x."""
-    dev = _device(x)
-    hx = _heads(x, "x", dev, _INPUTS)
-    T, H, d = x.shape
-    r = _rotation(table, positions, T, layout, dev)
-    if out is None:
-        out = _empty((T, H, d), x.dtype, dev, stream)
-        ho = attn_fp8_heads(out.data_ptr(), H * d, d, hx.type)
-    elif out.shape != x.shape:
-        raise ValueError("out must have x's shape")
-    else:
-        ho = _heads(out, "out", dev, (x.dtype,))
-    st = _lib.attn_fp8_rope(hx, ho, T, H, d, r, _stream(stream))
-    if st != ATTN_OK:
-        raise AttnError(st)
-    return out
+    return _call(stream, _binding.rope, x, table, positions, LAYOUTS[layout], out)
 
 
 def cache_append(cache, k, v, pages, lens, *, cu=None, max_q=None, table=None, positions=None,
@@ -522,55 +432,8 @@ def cache_append(cache, k, v, pages, lens, *, cu=None, max_q=None, table=None, p
     [B, W], lens int32 [B] (the new tokens included), cu int32 [B + 1] with max_q (None:
     T / B tokens each).  positions None: the tokens' places in their sequences.  With
     q [T, Hq, d] its rotation is done in the same launch and returned."""
-    dev = _device(k)
-    c = _cache(cache, dev)
-    hk, hv = _heads(k, "k", dev, _INPUTS), _heads(v, "v", dev, (k.dtype,))
-    T = k.shape[0]
-    if k.shape != v.shape or k.shape[1] != c.Hkv or k.shape[2] != c.d:
-        raise ValueError(f"k, v must be [T, {c.Hkv}, {c.d}]")
-    bt = _batch(pages, lens, cu, T, max_q, dev)
-    r = None if table is None else _rotation(table, positions, T, layout, dev)
-    hq = ho = None
-    Hq = 0
-    if q is not None:
-        if r is None:
-            raise ValueError("q is rotated along: that needs a table")
-        hq, shape = _heads(q, "q", dev, (k.dtype,)), q.shape
-        Hq = shape[1]
-        if shape[0] != T or shape[2] != c.d:
-            raise ValueError(f"q must be [{T}, Hq, {c.d}]")
-        if q_out is None:
-            q_out = _empty(shape, q.dtype, dev, stream)
-            ho = attn_fp8_heads(q_out.data_ptr(), Hq * c.d, c.d, hq.type)
-        elif q_out.shape != shape:
-            raise ValueError("q_out must have q's shape")
-        else:
-            ho = _heads(q_out, "q_out", dev, (k.dtype,))
-    st = _lib.attn_fp8_cache_append(c, bt, hk, hv, r, hq, ho, Hq, _stream(stream))
-    if st != ATTN_OK:
-        raise AttnError(st)
-    return q_out
-
-
-@functools.lru_cache(maxsize=4096)
-def _cache_workspace_bytes(device_index, n_pages, Hkv, page, d, B, W, T, max_q, Hq, max_len):
-    """The size depends on these sizes and on the device's CU count alone."""
-    st, n = attn_fp8_cache_workspace_bytes(attn_fp8_cache(None, None, None, None, n_pages, Hkv, page, d),
-                                           attn_fp8_batch(None, None, None, B, W, T, max_q), Hq, max_len)
-    if st != ATTN_OK:
-        raise AttnError(st)
-    return n
-
-
-def _queries(q, cache, pages, lens, cu, max_q, sm_scale):
-    dev = _device(q)
-    c = _cache(cache, dev)
-    hq = _heads(q, "q", dev, _QUERIES)
-    T, Hq, d = q.shape
-    if d != c.d or Hq % c.Hkv:
-        raise ValueError(f"q must be [T, Hq, {c.d}] with Hq a multiple of {c.Hkv}")
-    bt = _batch(pages, lens, cu, T, max_q, dev)
-    return dev, c, hq, T, Hq, d, bt, 1.0 / math.sqrt(d) if sm_scale is None else float(sm_scale)
+    return _call(stream, _binding.append, cache, k, v, pages, lens, cu, max_q, table, positions, LAYOUTS[layout], q,
+                 q_out)
 
 
 def cache_fwd(q, cache, pages, lens, *, cu=None, max_q=None, causal: bool = True, sm_scale=None,
@@ -582,35 +445,8 @@ def cache_fwd(q, cache, pages, lens, *, cu=None, max_q=None, causal: bool = True
     at position lens[b] - n + i and sees the keys up to it (causal=False: all).
     pages, lens, cu, max_q as for cache_append.  sm_scale None: 1 / sqrt(d).
     max_len: no sequence is longer (0: as long as pages allows)."""
-    dev, c, hq, T, Hq, d, bt, sm = _queries(q, cache, pages, lens, cu, max_q, sm_scale)
-    if out is None:
-        out = _empty((T, Hq, d), out_dtype, dev, stream)
-    elif out.shape != q.shape or not out.is_contiguous() or out.get_device() != dev:
-        raise ValueError("out must be a contiguous tensor of q's shape on its device")
-    if out.dtype not in (torch.bfloat16, torch.float32):
-        raise TypeError("out is bfloat16 or float32")
-    if lse is None:
-        lse = _empty((T, Hq), torch.float32, dev, stream) if want_lse else None
-    elif lse.shape != (T, Hq) or lse.dtype != torch.float32 or not lse.is_contiguous() or lse.get_device() != dev:
-        raise ValueError(f"lse must be a contiguous float32 tensor [{T}, {Hq}]")
-    n = _cache_workspace_bytes(dev, c.n_pages, c.Hkv, c.page, d, bt.B, bt.W, T, bt.max_q, Hq, int(max_len))
-    ws = _empty((n,), torch.uint8, dev, stream) if n else None
-    st = _lib.attn_fp8_cache_fwd(c, bt, hq, Hq, out.data_ptr(), _TYPES[out.dtype], _ptr(lse), int(bool(causal)), sm,
-                                 float(q_descale), int(max_len), _ptr(ws), n, _stream(stream))
-    if st != ATTN_OK:
-        raise AttnError(st)
-    return out, lse
-
-
-def _weights(weights, B, Hkv, least, device):
-    shape = weights.shape
-    sb, sh, sn = weights.stride() if len(shape) == 3 else (0, 0, 0)
-    if (len(shape) != 3 or shape[0] != B or shape[1] != Hkv or shape[2] < least or weights.dtype is not torch.float32
-            or weights.get_device() != device or (sn != 1 and shape[2] > 1) or (Hkv > 1 and sh < shape[2])
-            or (B > 1 and sb < (Hkv - 1) * sh + shape[2])):
-        raise ValueError(f"weights must be float32 [{B}, {Hkv}, at least {least}] with contiguous rows that do not "
-                         f"overlap, on cuda:{device}")
-    return weights.data_ptr(), sb if B > 1 else 0, sh if Hkv > 1 else shape[2]
+    return _call(stream, _binding.fwd, q, cache, pages, lens, cu, max_q, causal, sm_scale, q_descale, max_len, out,
+                 _OUT_TYPES[out_dtype], lse, want_lse)
 
 
 def cache_weights(q, lse, cache, pages, lens, weights, *, cu=None, max_q=None, causal: bool = True, sm_scale=None,
@@ -618,17 +454,8 @@ def cache_weights(q, lse, cache, pages, lens, weights, *, cu=None, max_q=None, c
     """Adds to weights [B, Hkv, n] (float32, in place; n at least the longest sequence,
     max_len or W * page) the attention weight that each cached token receives from the
     new tokens q and the query heads of its group; lse is cache_fwd's for the same call."""
-    dev, c, hq, T, Hq, d, bt, sm = _queries(q, cache, pages, lens, cu, max_q, sm_scale)
-    if lse.shape != (T, Hq) or lse.dtype != torch.float32 or not lse.is_contiguous() or lse.get_device() != dev:
-        raise ValueError(f"lse must be a contiguous float32 tensor [{T}, {Hq}]")
-    most = bt.W * c.page
-    most = min(most, int(max_len)) if max_len else most
-    p, sb, sh = _weights(weights, bt.B, c.Hkv, most, dev)
-    st = _lib.attn_fp8_cache_weights(c, bt, hq, Hq, lse.data_ptr(), int(bool(causal)), sm, float(q_descale),
-                                     int(max_len), p, sb, sh, _stream(stream))
-    if st != ATTN_OK:
-        raise AttnError(st)
-    return weights
+    return _call(stream, _binding.weights, q, lse, cache, pages, lens, weights, cu, max_q, causal, sm_scale, q_descale,
+                 max_len)
 
 
 def cache_evict(cache, pages, lens, weights, to, new_pages, budget, *, n_sink: int = 4, n_recent: int = 0,
@@ -639,32 +466,5 @@ def cache_evict(cache, pages, lens, weights, to, new_pages, budget, *, n_sink: i
     n_recent, and the ones of the largest weights [B, Hkv, n] (equal ones: the earlier).
     Returns (kept [B, Hkv, budget] int32: where each was, then -1; new_lens [B] int32;
     new_weights [B, Hkv, budget] float32: theirs, then 0)."""
-    dev = _device(lens)
-    c, ct = _cache(cache, dev), _cache(to, dev)
-    if pages.dim() != 2:
-        raise ValueError("pages must be [B, W]")
-    B, W = pages.shape
-    if (ct.Hkv, ct.page, ct.d) != (c.Hkv, c.page, c.d) or budget < 1:
-        raise ValueError("both caches have the same heads, page and d, and budget is at least 1")
-    bt = attn_fp8_batch(_ints(pages, (B, W), "pages", dev), _ints(lens, (B,), "lens", dev), None, B, W, 0, 1)
-    np_ = _ints(new_pages, (B, -(-budget // c.page)), "new_pages", dev)
-    p, sb, sh = _weights(weights, B, c.Hkv, W * c.page, dev)
-    shape = (B, c.Hkv, budget)
-    if kept is None:
-        kept = _empty(shape, torch.int32, dev, stream)
-    else:
-        _ints(kept, shape, "kept", dev)
-    if new_lens is None:
-        new_lens = _empty((B,), torch.int32, dev, stream)
-    else:
-        _ints(new_lens, (B,), "new_lens", dev)
-    if new_weights is None:
-        new_weights = _empty(shape, torch.float32, dev, stream)
-    elif (new_weights.dtype != torch.float32 or new_weights.shape != shape or not new_weights.is_contiguous()
-            or new_weights.get_device() != dev):
-        raise ValueError(f"new_weights must be a contiguous float32 tensor {list(shape)}")
-    st = _lib.attn_fp8_cache_evict(c, bt, ct, np_, p, sb, sh, int(budget), int(n_sink), int(n_recent),
-                                   kept.data_ptr(), new_lens.data_ptr(), new_weights.data_ptr(), _stream(stream))
-    if st != ATTN_OK:
-        raise AttnError(st)
-    return kept, new_lens, new_weights
+    return _call(stream, _binding.evict, cache, pages, lens, weights, to, new_pages, budget, n_sink, n_recent, kept,
+                 new_lens, new_weights)

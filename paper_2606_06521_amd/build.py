@@ -1,7 +1,8 @@
-"""Build libattn_fp8.so (the HIP kernels and the C ABI) for gfx950 with hipcc.
+"""Build libattn_fp8.so (the HIP kernels and the C ABI) for gfx950 with hipcc, and
+_cache_binding.so (the cache calls on torch tensors) with g++.
 
 Every call compiles from source.  Objects go to ``_build/`` at the repository
-root; the shared library lands next to this file so it travels with the tree.
+root; the shared libraries land next to this file so they travel with the tree.
 """
 from __future__ import annotations
 
@@ -15,6 +16,7 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 BUILD = os.path.join(ROOT, "_build")
 LIB = os.path.join(HERE, "libattn_fp8.so")
+BINDING = os.path.join(HERE, "_cache_binding.so")
 
 SOURCES = ["attn_fp8_abi.hip", "attn_fast.hip", "attn_fast_pair.hip", "attn_fast_qk8.hip",
            "attn_fast_qk8_pair.hip", "attn_faithful.hip", "attn_prefill.hip", "attn_kv_bf16_16.hip",
@@ -50,6 +52,26 @@ def hip_library(jobs: int | None = None) -> str:
     return LIB
 
 
+def binding() -> str:
+    """The Python module of the cache calls; links the library and torch."""
+    import sysconfig
+
+    from torch.utils import cpp_extension
+
+    include = [*cpp_extension.include_paths(), sysconfig.get_paths()["include"], "/opt/rocm/include"]
+    tmp = BINDING + f".tmp{os.getpid()}"
+    cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-D__HIP_PLATFORM_AMD__=1", "-DUSE_ROCM",
+           *("-I" + d for d in include), os.path.join(CSRC, "cache_binding.cpp"), "-o", tmp,
+           *("-L" + d for d in cpp_extension.library_paths()), "-ltorch_python", "-ltorch_cpu", "-ltorch", "-lc10",
+           "-lc10_hip", "-L" + HERE, "-lattn_fp8", "-Wl,-rpath,$ORIGIN"]
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError(f"g++ failed for cache_binding.cpp:\n{r.stderr}")
+    os.replace(tmp, BINDING)
+    return BINDING
+
+
 if __name__ == "__main__":
     print(hip_library())
+    print(binding())
     sys.exit(0)
