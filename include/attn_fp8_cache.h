@@ -21,13 +21,14 @@
  * of sequence b from cu[b] to cu[b + 1]: they are its last ones, token i of n is
  * position lens[b] - n + i.  cu = NULL: T / B tokens of each sequence.
  * lens, pages and cu are read on the device, so a captured call follows them:
- *   - lens[b] above W * page (at most 2^26, else ATTN_ERR_UNSUPPORTED) counts as
- *     W * page, below 0 as 0;
- *   - a page number outside 0 .. n_pages - 1 is no page: its tokens are not
- *     written, and no query sees them;
+ *   - lens[b] below 0 counts as 0; a page number outside 0 .. n_pages - 1 is no
+ *     page, and what lies past the W pages of a sequence has none (W * page is at
+ *     most 2^26, else ATTN_ERR_UNSUPPORTED).  Tokens without a page are not written,
+ *     and no query sees them; nor are tokens before position 0, whose queries see
+ *     no key;
  *   - a sequence has at most max_q new tokens; those beyond are left out (not
  *     written, their rows of an output left as they were), as are cu entries
- *     outside 0 .. T and tokens before position 0.
+ *     outside 0 .. T.
  * Rows of q, out and lse behind cu[B] are not touched.
  */
 #ifndef ATTN_FP8_CACHE_H
@@ -122,7 +123,7 @@ int attn_fp8_cache_append(const attn_fp8_cache *cache, const attn_fp8_batch *bat
  *   out        contiguous [T][Hq][d], BF16 or F32 by out_type, 16-byte aligned.
  *   lse        FP32 [T][Hq], or NULL.
  *   sm_scale, q_descale   finite and > 0.
- *   max_len    no lens[b] is larger (larger ones count as max_len); 0: W * page.
+ *   max_len    no lens[b] is larger (keys from max_len on are not seen); 0: W * page.
  *              The plan goes by it, so a close bound is a faster call.
  *   workspace  256-byte aligned device memory of workspace_bytes, scratch of this
  *              call alone; at least what attn_fp8_cache_workspace_bytes gives,

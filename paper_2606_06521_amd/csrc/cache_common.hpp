@@ -42,8 +42,9 @@ struct Rotation {
     int n_pos, rot, layout;      // layout 0: halves, 1: interleaved
 };
 
-// Sequence b: its length (at most max_len), its new tokens [first, first + n) of
-// the call (at most max_q, inside [0, T)), the position of the first of them.
+// Sequence b: the keys there are (its length, at most max_len), its new tokens
+// [first, first + n) of the call (at most max_q, inside [0, T)), the position of the
+// first of them (by its whole length: it may lie before 0 or past the keys).
 struct Seq {
     int len, first, n, pos0;
 };
@@ -51,7 +52,8 @@ struct Seq {
 __device__ inline Seq sequence(const Batch& bt, int b, int max_len)
 {
     Seq s;
-    s.len = min(max(bt.lens[b], 0), max_len);
+    const int whole = max(bt.lens[b], 0);
+    s.len = min(whole, max_len);
     int n;
     if (bt.cu) {
         const int c0 = bt.cu[b], c1 = bt.cu[b + 1];
@@ -61,9 +63,7 @@ __device__ inline Seq sequence(const Batch& bt, int b, int max_len)
         s.first = b * bt.uniform;
         n = bt.uniform;
     }
-    // (position of the first new token, which may lie before token 0 or, past the
-    // first max_q, leave tokens out at the end)
-    s.pos0 = s.len - n;
+    s.pos0 = whole - n;
     s.n = min(n, bt.max_q);
     return s;
 }
@@ -93,11 +93,12 @@ __device__ inline int page_of(const Batch& bt, int n_pages, int b, int block)
 
 // ---- E4M3 blocks ----
 
-// Least e >= -127 with amax <= 448 * 2^e (amax finite, >= 0).
+// Least e >= -127 with amax <= 448 * 2^e (amax >= 0; past FP32's largest: as that).
 __device__ inline int block_exponent(float amax)
 {
     if (amax == 0.f)
         return -127;
+    amax = __builtin_fminf(amax, 0x1.fffffep127f);
     const int t = __builtin_amdgcn_frexp_expf(amax);
     const float f = __builtin_amdgcn_frexp_mantf(amax);   // [0.5, 1): 448 = 0.875 * 2^9
     return max(t - 9 + (f > 0.875f ? 1 : 0), -127);

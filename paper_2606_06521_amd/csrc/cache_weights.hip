@@ -35,7 +35,7 @@ __device__ inline void row_of(const WeightParams& p, const Seq& s, int hk, int R
     const int at = min(R, rows - 1), i = p.gr.token(at);
     const float x = p.lse[(int64_t)(s.first + i) * p.Hq + hk * p.gr.G + (at - i * p.gr.G)];
     lse2 = x == -INFINITY ? INFINITY : x * 1.4426950408889634f;
-    last = R >= rows ? -1 : p.causal ? s.pos0 + i : s.len - 1;
+    last = R >= rows ? -1 : p.causal ? min(s.pos0 + i, s.len - 1) : s.len - 1;
 }
 
 // Q operand of row R (past the last: any row): k-step 2 i + e of lane group g:

@@ -56,14 +56,15 @@ def rotate(x, table, pos, layout):
 
 
 def tokens(lens, cu, T, b, W, page, max_q):
-    """(length, first packed token, new tokens, position of the first)."""
-    n = min(max(int(lens[b]), 0), W * page)
+    """(keys there are, first packed token, new tokens, position of the first)."""
+    whole = max(int(lens[b]), 0)
+    n = min(whole, W * page)
     if cu is None:
         q = T // len(lens)
         first = b * q
     else:
         first, q = int(cu[b]), int(cu[b + 1]) - int(cu[b])
-    return n, first, min(q, max_q), n - q
+    return n, first, min(q, max_q), whole - q
 
 
 class Pages:

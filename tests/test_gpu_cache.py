@@ -642,3 +642,43 @@ def test_binding_refuses_what_does_not_fit(A):
             call()
     with pytest.raises(KeyError):
         A.rope(q, table, pos, layout="other")
+
+
+def test_tokens_past_the_page_table_have_no_place(A):
+    """lens past W * page: the tokens that fit are written where they belong, no older one is overwritten;
+    queries of the others see every key there is."""
+    rng = np.random.default_rng(95)
+    c = R.make_cache(rng, 2, 2, 64, 64, [128, 128])
+    c.lens = np.array([129, 131], dtype=np.int32)          # 1 past the table; 3 past it, one inside
+    new = [1, 4]
+    t = torch.from_numpy(rng.standard_normal((2, 5, 2, 64))).bfloat16()
+    gc, cu = dev_cache(A, c), cu_of(new)
+    A.cache_append(gc, t[0].cuda(), t[1].cuda(), dev(c.pages), dev(c.lens), cu=dev(cu), max_q=4)
+    before = c.copy()
+    c.append(t[0].double().numpy(), t[1].double().numpy(), cu=cu, max_q=4)
+    same_cache(gc, c)
+    assert np.array_equal(c.k[c.pages[0]], before.k[before.pages[0]])
+    c = before
+    q = R.make_queries(rng, 5, 4, 64)
+    run_fwd(A, c, q, 2, "bf16", new=new)
+    lse = R.attention(c, q, 2, cu=cu)[1].astype(np.float32)
+    w = torch.zeros((2, 2, 128), device="cuda")
+    A.cache_weights(R.torch_q(q, "bf16").cuda(), dev(lse), dev_cache(A, c), dev(c.pages), dev(c.lens), w, cu=dev(cu), max_q=4)
+    want = R.weights(c, q, lse, 2, 128, cu=cu)
+    within(w.cpu().double().numpy(), want, 2.0 ** -17 * want)
+
+
+def test_largest_values_survive_append_and_eviction(A):
+    """Values next to FP32's largest: 2^128 after rounding, as codes and scales."""
+    c = R.make_cache(np.random.default_rng(96), 1, 1, 64, 64, [3])
+    x = torch.full((3, 1, 64), 1.0)
+    x[0, 0, 5], x[1, 0, 6], x[2, 0, 7] = 3.4e38, -3.3e38, 1e38
+    gc = dev_cache(A, c)
+    A.cache_append(gc, x.cuda(), x.cuda(), dev(c.pages), dev(c.lens))
+    c.append(x.double().numpy(), x.double().numpy())
+    same_cache(gc, c)
+    to, new_pages = c.copy(), np.array([[c.n_pages - 1 if c.pages[0, 0] != c.n_pages - 1 else 0]], dtype=np.int32)
+    w = torch.tensor([[[1.0, 2.0, 0.0] + [0.0] * 61]]).cuda()
+    A.cache_evict(gc, dev(c.pages), dev(c.lens), w, gc, dev(new_pages), 2, n_sink=0)
+    R.evict(c, w.cpu().numpy(), 2, 0, 0, to, new_pages)
+    same_cache(gc, to)
