@@ -226,22 +226,29 @@ __global__ void __launch_bounds__(256, 1) cache_fwd_kernel(FwdParams p)
         const bool there[2] = {pids[pi] >= 0, pids[pi + PPV - 1] >= 0};
         // ---- scores (K is older than V: wait for all but V's loads) ----
         asm volatile("s_waitcnt vmcnt(%0)" :: "n"(NI) : "memory");
+        i32x4 raw[KT][KP];
+#pragma unroll
+        for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+            for (int i = 0; i < KP; ++i) {
+                const int r = krow + 64 * (kt / 4) + 4 * (kt % 4);
+                raw[kt][i] = *reinterpret_cast<const i32x4*>(kst + r * D + 16 * ((4 * i + g) ^ kswz(r)));
+            }
+        // (all in registers: the stage takes the next visit)
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        issue_k(v + NW);
         f32x4 sc[KT];
 #pragma unroll
         for (int kt = 0; kt < KT; ++kt) {
-            const int r = krow + 64 * (kt / 4) + 4 * (kt % 4);
             f32x4 acc = {};
 #pragma unroll
             for (int i = 0; i < KP; ++i) {
-                const i32x4 x = *reinterpret_cast<const i32x4*>(kst + r * D + 16 * ((4 * i + g) ^ kswz(r)));
+                const i32x4 x = raw[kt][i];
                 acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen((uint32_t)x[0], (uint32_t)x[1]), qf[2 * i], acc, 0, 0, 0);
                 acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen((uint32_t)x[2], (uint32_t)x[3]), qf[2 * i + 1], acc, 0, 0, 0);
             }
             sc[kt] = acc;
         }
-        // (every fragment has been read: the stage takes the next visit)
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-        issue_k(v + NW);
         // ---- keys the row does not see ----
         const int t0 = v * kVisit;
         if (t0 + kVisit - 1 > pos_min || !there[0] || !there[1]) {

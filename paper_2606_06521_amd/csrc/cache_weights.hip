@@ -332,16 +332,19 @@ __global__ void __launch_bounds__(256, 2) weights_tall_kernel(WeightParams p, in
                 }
                 const f32x4 l4 = *reinterpret_cast<const f32x4*>(&lse_s[buf][r0 + 4 * g]);
                 const i32x4 e4 = *reinterpret_cast<const i32x4*>(&last_s[buf][r0 + 4 * g]);
+                // (the tiles' chains of matrix instructions side by side: none waits for itself)
+                f32x4 acc[KT];
+#pragma unroll
+                for (int j = 0; j < 2 * KP; ++j)
+#pragma unroll
+                    for (int kt = 0; kt < KT; ++kt)
+                        acc[kt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(qf[j], kf[kt][j], j == 0 ? f32x4{} : acc[kt], 0, 0, 0);
 #pragma unroll
                 for (int kt = 0; kt < KT; ++kt) {
-                    f32x4 acc = {};
-#pragma unroll
-                    for (int j = 0; j < 2 * KP; ++j)
-                        acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(qf[j], kf[kt][j], acc, 0, 0, 0);
                     const int t = t0 + 64 * kh + 16 * kt + n;
 #pragma unroll
                     for (int r = 0; r < 4; ++r) {
-                        const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(acc[r], c, -l4[r]));
+                        const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(acc[kt][r], c, -l4[r]));
                         sum[kt] += !decltype(masked)::value || t <= e4[r] ? x : 0.f;
                     }
                 }

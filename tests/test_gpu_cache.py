@@ -682,3 +682,73 @@ def test_largest_values_survive_append_and_eviction(A):
     A.cache_evict(gc, dev(c.pages), dev(c.lens), w, gc, dev(new_pages), 2, n_sink=0)
     R.evict(c, w.cpu().numpy(), 2, 0, 0, to, new_pages)
     same_cache(gc, to)
+
+
+def test_two_streams_and_two_graphs_at_once(A):
+    """Split calls (each with a workspace of its own) side by side on two streams, and two captured ones
+    replayed in turn: all equal the calls by themselves."""
+    rng = np.random.default_rng(97)
+    sets = []
+    for n in (9000, 5000):
+        c = R.make_cache(rng, 2, 2, 128, 128, [n, 300])
+        args = (R.torch_q(R.make_queries(rng, 2, 8, 128), "bf16").cuda(), dev_cache(A, c), dev(c.pages), dev(c.lens))
+        st, nbytes = A.attn_fp8_cache_workspace_bytes(A.attn_fp8_cache(None, None, None, None, c.n_pages, 2, 128, 128),
+                                                      A.attn_fp8_batch(None, None, None, 2, c.pages.shape[1], 2, 1), 8, 0)
+        assert st == 0 and nbytes > 0
+        sets.append((args, A.cache_fwd(*args)))
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in sets]
+    got = [[A.cache_fwd(*args, stream=s) for _ in range(8)] for (args, _), s in zip(sets, streams)]
+    torch.cuda.synchronize()
+    for (_, want), calls in zip(sets, got):
+        for o, l in calls:
+            assert torch.equal(o, want[0]) and torch.equal(l, want[1])
+    graphs = []
+    for args, want in sets:
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            r = A.cache_fwd(*args)
+        graphs.append((g, r, want))
+    for i in range(4):
+        log(f"replay {i}")
+        for g, r, want in graphs:
+            r[0].fill_(3.0)
+            g.replay()
+        A.cache_fwd(*sets[0][0])
+        torch.cuda.synchronize()
+        for _, r, want in graphs:
+            assert torch.equal(r[0], want[0]) and torch.equal(r[1], want[1])
+
+
+def test_every_call_on_another_stream(A):
+    """The whole step on a stream of its own, behind work that is still running there."""
+    rng = np.random.default_rng(98)
+    B, Hq, Hkv, d, page = 2, 4, 2, 64, 64
+    c = R.make_cache(rng, B, Hkv, page, d, [200, 100], extra=6)
+    spare = np.array([p for p in range(c.n_pages) if p not in c.pages][:4], dtype=np.int32).reshape(2, 2)
+    x = torch.from_numpy(rng.standard_normal((B, Hq + 2 * Hkv, d))).bfloat16().cuda()
+    table, pages, lens, new_pages = A.rope_table(256, d), dev(c.pages), dev(c.lens), dev(spare)
+
+    def step(stream):
+        gc = dev_cache(A, c)
+        w = torch.zeros((B, Hkv, pages.shape[1] * page), device="cuda")
+        late = torch.zeros_like(x)
+        torch.cuda.synchronize()
+        if stream is None:
+            late.copy_(x)
+        else:
+            with torch.cuda.stream(stream):
+                torch.cuda._sleep(20_000_000)       # the inputs arrive late on that stream
+                late.copy_(x)
+        kw = dict(stream=stream)
+        q = A.cache_append(gc, late[:, Hq:Hq + Hkv], late[:, Hq + Hkv:], pages, lens, table=table, q=late[:, :Hq], **kw)
+        r = A.rope(late[:, :Hq], table, torch.tensor([199, 99], dtype=torch.int32, device="cuda") if stream is None else pos, **kw)
+        out, lse = A.cache_fwd(q, gc, pages, lens, **kw)
+        A.cache_weights(q, lse, gc, pages, lens, w, **kw)
+        kept, nl, nw = A.cache_evict(gc, pages, lens, w, gc, new_pages, 100, **kw)
+        torch.cuda.synchronize()
+        return [q, r, out, lse, w, kept, nl, nw, *(t.view(torch.uint8) for t in gc)]
+
+    pos = torch.tensor([199, 99], dtype=torch.int32, device="cuda")
+    for a, b in zip(step(None), step(torch.cuda.Stream())):
+        assert torch.equal(a, b)
