@@ -108,7 +108,7 @@ hipError_t fwd_go(const FwdParams& p, int rows, bool e4m3, int64_t grid, hipStre
 //   16 rows:  a workgroup per CU (two at d = 64), whose four waves take a visit each; a
 //             wave's visit takes 3 of them at d = 128
 //   128 rows: two workgroups per CU, each of them a visit at a time: 4.1 in company, 2.5 alone
-// (at d = 64 0.6 of both), 8 and 11 to begin and end, and where a tile is split its
+// (at d = 64 0.6 of both), a workgroup's first loads and last sum 6 or 9, and where a tile is split its
 // merge: a launch, and the partial sums written and read.  Measured at 16 x 8 heads x
 // 8192 keys: 32 rows 51 (16-row tiles) against 82, 96 rows 149 against 113; one
 // sequence x 8 heads x 32768 keys: 64 rows 33 against 46, 256 rows 94 against 61.
@@ -127,7 +127,7 @@ double plan_time(FwdPlan& pl, int rows, int64_t heads, int64_t run, int visits, 
     pl.bytes = pl.ranges > 1 ? (size_t)units * pl.ranges * rows * (d + 2) * sizeof(float) : 0;
     const double wgs = (double)units * pl.ranges, rounds = std::ceil(wgs / slots), each = std::min(pl.chunk, visits);
     const double visit = (d == 64 ? 0.6 : 1.0) * (tall ? (wgs > n_cu ? 4.1 : 2.5) : 3.0 * (slots > n_cu && wgs > n_cu ? 1.5 : 1.0) / 4);
-    return (tall ? 11 : 8) + rounds * each * visit + (pl.ranges > 1 ? 5 + 2e-6 * pl.bytes / 2.5 : 0);
+    return 2 + rounds * ((tall ? 9 : 6) + each * visit) + (pl.ranges > 1 ? 5 + 2e-6 * pl.bytes / 2.5 : 0);
 }
 
 }  // namespace

@@ -12,10 +12,11 @@
 // its way while this one is computed with Q in registers (two waves on a SIMD: one
 // hides the other's latencies); the sums wait in LDS for one update of the weights
 // at the end.  What bounds it is the stream of K.  With more rows (chunks) a workgroup
-// takes one visit, widens its keys to bf16 registers once (64 keys a wave) and
-// runs over the rows 64 at a time, the next 64 on their way into the other of two
-// LDS stages, each wave two 16-row tiles of them; what bounds that is the exp2 of
-// every (row, key).
+// takes 128 keys, widens them to bf16 registers once (64 keys a wave) and runs over
+// the rows 64 at a time, the next 64 on their way into the other of two LDS stages,
+// each wave two 16-row tiles of them; what bounds that is the exp2 of every (row,
+// key).  Where blocks of 128 keys do not fill the GPU they are of 32 keys, and the
+// waves share out the rows instead.
 #include "cache_common.hpp"
 
 #include <algorithm>
@@ -208,11 +209,13 @@ __global__ void __launch_bounds__(512, 1) weights_stream_kernel(WeightParams p, 
     }
 }
 
-template <int D, int PAGE, bool E4M3>
-__global__ void __launch_bounds__(256, 2) weights_tall_kernel(WeightParams p, int visits)
+template <int D, int PAGE, bool E4M3, int KEYS>
+__global__ void __launch_bounds__(256, 2) weights_tall_kernel(WeightParams p, int blocks)
 {
-    constexpr int KT = 4, KP = D / 64, CPR = D / 16, PPV = kVisit / PAGE;
-    constexpr int STAGE = kVisit * D, LPW = STAGE / 1024 / 4;
+    constexpr int KT = KEYS == 32 ? 2 : 4;          // 16-key tiles of a wave
+    constexpr int NK = KEYS / (16 * KT), NR = 4 / NK;   // the waves: NK runs of keys, NR of a segment's rows
+    constexpr int KP = D / 64, CPR = D / 16, WROWS = KEYS / 4;   // rows of K that a wave loads
+    constexpr int STAGE = KEYS * D, LPW = (STAGE / 4 + 1023) / 1024;
     constexpr int SEG = 64;                         // rows of a segment
     constexpr int QB = E4M3 ? 1 : 2, QROW = QB * D; // bytes of a query's element and row
     constexpr int QC = QROW / 16, QRPI = 1024 / QROW, QLPW = 16 * QROW / 1024;   // chunks of a row, rows per load, loads of 16 rows
@@ -220,19 +223,18 @@ __global__ void __launch_bounds__(256, 2) weights_tall_kernel(WeightParams p, in
     __shared__ __attribute__((aligned(1024))) uint8_t qst[2][SEG * QROW];
     __shared__ __attribute__((aligned(16))) float lse_s[2][SEG];
     __shared__ __attribute__((aligned(16))) int last_s[2][SEG];
-    __shared__ float half_w[kVisit];
-    const int v = (int)(blockIdx.x % visits);       // (causal: the first keys have the most rows)
-    const int rest = (int)(blockIdx.x / visits);
+    __shared__ float part_w[NR][KEYS];
+    const int v = (int)(blockIdx.x % blocks);       // (causal: the first keys have the most rows)
+    const int rest = (int)(blockIdx.x / blocks);
     const int hk = rest % p.cache.Hkv, b = rest / p.cache.Hkv;
     const Seq s = uniform(sequence(p.bt, b, p.max_len));
-    const int t0 = v * kVisit;
+    const int t0 = v * KEYS;
     if (t0 >= s.len || s.n <= 0)
         return;
     const int tid = threadIdx.x, lane = tid & 63;
     const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int n = lane & 15, g = lane >> 4;
-    // the wave's keys: a half of the visit; its row tiles: two of a segment's four
-    const int kh = w & 1, rh = w >> 1;
+    const int kh = w % NK, rh = w / NK;
     const int rows = s.n * p.gr.G;
     const int segs = (rows + SEG - 1) / SEG;
     // (causal: the rows before the first that sees key t0 add nothing)
@@ -268,19 +270,21 @@ __global__ void __launch_bounds__(256, 2) weights_tall_kernel(WeightParams p, in
     };
     if (first < segs)
         issue_q(first, 0);
-    // and 32 rows of K
+    // and WROWS rows of K, of one page
     const int lr = lane / CPR, lc = lane % CPR;
-    const int sub = PPV == 2 ? w >> 1 : 0;
-    const int lpid = __builtin_amdgcn_readfirstlane(page_of(p.bt, p.cache.n_pages, b, v * PPV + sub));
+    const int k0 = t0 + WROWS * w;
+    const int lpid = __builtin_amdgcn_readfirstlane(page_of(p.bt, p.cache.n_pages, b, k0 / PAGE));
     {
-        const int left = lpid < 0 ? 0 : min(max(s.len - (t0 + sub * PAGE), 0), PAGE) * D;
-        const i32x4 kb = bytes_buffer(p.cache.k + ((size_t)(lpid < 0 ? 0 : lpid) * p.cache.Hkv + hk) * (PAGE * D), left);
-        const int src = (32 * w - sub * PAGE) * D;
+        const int left = lpid < 0 ? 0 : min(min(max(s.len - k0, 0), WROWS), PAGE - k0 % PAGE) * D;
+        const i32x4 kb = bytes_buffer(p.cache.k + ((size_t)(lpid < 0 ? 0 : lpid) * p.cache.Hkv + hk) * (PAGE * D) + k0 % PAGE * D, left);
+        // (fewer rows than a load holds: the other lanes stay out)
+        if (lr < WROWS) {
 #pragma unroll
-        for (int j = 0; j < LPW; ++j)
-            load_lds16(kb, lr * D + 16 * (lc ^ stage_swz<D>(lr)), src + 1024 * j, lds + w * (32 * D) + 1024 * j);
+            for (int j = 0; j < LPW; ++j)
+                load_lds16(kb, lr * D + 16 * (lc ^ stage_swz<D>(lr)), 1024 * j, lds + w * (WROWS * D) + 1024 * j);
+        }
     }
-    const int pid = __builtin_amdgcn_readfirstlane(page_of(p.bt, p.cache.n_pages, b, v * PPV + (PPV == 2 ? kh : 0)));
+    const int pid = __builtin_amdgcn_readfirstlane(page_of(p.bt, p.cache.n_pages, b, (t0 + 16 * KT * kh) / PAGE));
     const float c = pid < 0 ? 0.f : __builtin_amdgcn_ldexpf(p.c, (int)p.cache.ks[(size_t)pid * p.cache.Hkv + hk] - 127);
     float lse2 = 0.f;
     int last = -1;
@@ -295,7 +299,7 @@ __global__ void __launch_bounds__(256, 2) weights_tall_kernel(WeightParams p, in
     float sum[KT];
 #pragma unroll
     for (int kt = 0; kt < KT; ++kt) {
-        const int r = 64 * kh + 16 * kt + n;
+        const int r = 16 * KT * kh + 16 * kt + n;
         sum[kt] = 0.f;
 #pragma unroll
         for (int i = 0; i < KP; ++i) {
@@ -311,12 +315,12 @@ __global__ void __launch_bounds__(256, 2) weights_tall_kernel(WeightParams p, in
                 row_of(p, s, hk, SEG * (seg + 1) + tid, rows, lse2, last);
             issue_q(seg + 1, buf ^ 1);
         }
-        // every row of the segment sees every key of the visit
-        const bool all = SEG * (seg + 1) <= rows && (!p.causal || s.pos0 + p.gr.token(SEG * seg) >= t0 + kVisit - 1) && t0 + kVisit <= s.len;
+        // every row of the segment sees every key of the block
+        const bool all = SEG * (seg + 1) <= rows && (!p.causal || s.pos0 + p.gr.token(SEG * seg) >= t0 + KEYS - 1) && t0 + KEYS <= s.len;
         auto tiles = [&](auto masked) __attribute__((always_inline)) {
 #pragma unroll
-            for (int q = 0; q < 2; ++q) {
-                const int r0 = 32 * rh + 16 * q;
+            for (int q = 0; q < NK; ++q) {
+                const int r0 = 16 * (NK * rh + q);
                 bf16x8 qf[2 * KP];
 #pragma unroll
                 for (int i = 0; i < KP; ++i) {
@@ -341,7 +345,7 @@ __global__ void __launch_bounds__(256, 2) weights_tall_kernel(WeightParams p, in
                         acc[kt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(qf[j], kf[kt][j], j == 0 ? f32x4{} : acc[kt], 0, 0, 0);
 #pragma unroll
                 for (int kt = 0; kt < KT; ++kt) {
-                    const int t = t0 + 64 * kh + 16 * kt + n;
+                    const int t = t0 + 16 * (KT * kh + kt) + n;
 #pragma unroll
                     for (int r = 0; r < 4; ++r) {
                         const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(acc[kt][r], c, -l4[r]));
@@ -365,13 +369,20 @@ __global__ void __launch_bounds__(256, 2) weights_tall_kernel(WeightParams p, in
 #pragma unroll
     for (int kt = 0; kt < KT; ++kt)
         sum[kt] = over_groups(sum[kt]);
-    const float x = of_group(g, sum);
-    if (rh == 1)
-        half_w[64 * kh + lane] = x;
+    // lane (n, g) has key n of tile g
+    const float x = KT == 4 ? of_group(g, sum) : g & 1 ? sum[1] : sum[0];
+    const int at = 16 * KT * kh + lane % (16 * KT);
+    if (lane < 16 * KT)
+        part_w[rh][at] = x;
     __syncthreads();
-    const int t = t0 + 64 * kh + lane;
-    if (rh == 0 && t < s.len && pid >= 0)
-        p.w[(int64_t)b * p.sb + (int64_t)hk * p.sh + t] += x + half_w[64 * kh + lane];
+    const int t = t0 + at;
+    if (rh == 0 && lane < 16 * KT && t < s.len && pid >= 0) {
+        float total = part_w[0][at];
+#pragma unroll
+        for (int i = 1; i < NR; ++i)
+            total += part_w[i][at];
+        p.w[(int64_t)b * p.sb + (int64_t)hk * p.sh + t] += total;
+    }
 }
 
 }  // namespace
@@ -385,14 +396,22 @@ hipError_t launch_cache_weights(const WeightParams& p, int d, int page, bool e4m
     const int64_t want = std::max<int64_t>(1, n_cu / heads);
     const int chunk = (int)std::min<int64_t>(std::max<int64_t>(8, (visits + want - 1) / want), kStreamChunk);
     const int ranges = (visits + chunk - 1) / chunk;
-    const int64_t grid = heads * (tall ? visits : ranges);
+    // Keys of a block with many rows: 128, or 32 where that leaves CUs without a block (1 x 2
+    // heads x 2048 keys, 256 x 4 rows: 19.6 us with 128, 13.2 with 32; 1 x 8 x 5269, 607 x 8 rows,
+    // 336 blocks: 82 and 83; 8 x 8 x 1024, 64 x 4 rows, 512 blocks: 12 and 16)
+    const int keys = heads * visits < n_cu ? 32 : 128;
+    const int blocks = (p.max_len + keys - 1) / keys;
+    const int64_t grid = heads * (tall ? blocks : ranges);
     if (grid > 1 << 30)
         return hipErrorInvalidValue;
     auto by_type = [&](auto dc, auto pc, auto ec) {
         constexpr int D = decltype(dc)::value, PAGE = decltype(pc)::value;
         constexpr bool E = decltype(ec)::value;
-        if (tall)
-            hipLaunchKernelGGL((weights_tall_kernel<D, PAGE, E>), dim3((unsigned)grid), dim3(256), 0, s, p, visits);
+        auto tall_of = [&](auto kern) { hipLaunchKernelGGL(kern, dim3((unsigned)grid), dim3(256), 0, s, p, blocks); };
+        if (tall && keys == 128)
+            tall_of(weights_tall_kernel<D, PAGE, E, 128>);
+        else if (tall)
+            tall_of(weights_tall_kernel<D, PAGE, E, 32>);
         else if (rows <= 16)
             hipLaunchKernelGGL((weights_stream_kernel<D, PAGE, E, 1>), dim3((unsigned)grid), dim3(512), 0, s, p, chunk, ranges);
         else

@@ -294,7 +294,7 @@ def test_fwd_queries_with_strides(A):
 
 @pytest.mark.parametrize("d,page,G,kind", [(64, 64, 2, "e4m3"), (64, 128, 1, "bf16"), (128, 64, 4, "bf16"), (128, 128, 8, "e4m3")])
 @pytest.mark.parametrize("lens,new,causal", [([1], [1], True), ([300, 0, 129], [1, 0, 1], True), ([500, 90, 64], [37, 90, 64], True),
-                                             ([260, 33], [20, 3], False)])
+                                             ([260, 33], [20, 3], False), ([18000, 300], [70, 90], True)])
 def test_weights(A, lens, new, causal, d, page, G, kind):
     Hkv = 2
     log(f"weights {lens} {new} d={d} page={page} G={G} {kind}")
