@@ -9,9 +9,8 @@ namespace attn {
 // element types (the values of ATTN_TYPE_*)
 constexpr int kTypeF32 = 0, kTypeBf16 = 1, kTypeF16 = 2, kTypeE4m3 = 3;
 
-// Keys per group of P with a scale of its own: what one scale of an E4M3 MFMA
-// operand covers.  Keys per visit of the attention kernels.
-constexpr int kGroup = 32, kVisit = 128;
+// Keys per visit of the attention kernels.
+constexpr int kVisit = 128;
 
 // The batch, as the device reads it.  Nothing in lens, cu or pages is trusted:
 // whatever they hold, no access leaves the arrays.

@@ -11,11 +11,13 @@
 // from their LDS stage to registers at once, so that the wave's next visit is on
 // its way while this one is computed with Q in registers (two waves on a SIMD: one
 // hides the other's latencies); the sums wait in LDS for one update of the weights
-// at the end.  What bounds it is the stream of K.  With more rows (chunks) a workgroup
-// takes 128 keys, widens them to bf16 registers once (64 keys a wave) and runs over
+// at the end.  What bounds it is the stream of K: 16 x 8 heads x 8192 keys x 4 rows,
+// d = 128, 34 us, 4.3 TB/s, of which 8 to begin and end.  With more rows (chunks) a
+// workgroup takes 128 keys, widens them to bf16 registers once (64 keys a wave) and runs over
 // the rows 64 at a time, the next 64 on their way into the other of two LDS stages,
-// each wave two 16-row tiles of them; what bounds that is the exp2 of every (row,
-// key).  Where blocks of 128 keys do not fill the GPU they are of 32 keys, and the
+// each wave two 16-row tiles of them; what bounds that is the vector work of every
+// (row, key), at three waves a SIMD (38 % busy): 2 x 8 heads x 8192 keys x 1024 rows
+// (half of them ragged) 43 us.  Where blocks of 128 keys do not fill the GPU they are of 32 keys, and the
 // waves share out the rows instead.
 #include "cache_common.hpp"
 
@@ -76,7 +78,7 @@ template <int D, int PAGE, bool E4M3, int RT>
 __global__ void __launch_bounds__(512, 1) weights_stream_kernel(WeightParams p, int chunk, int ranges)
 {
     constexpr int NW = 8, PPV = kVisit / PAGE, KT = kVisit / 16, KP = D / 64, CPR = D / 16;
-    constexpr int STAGE = kVisit * D, NI = STAGE / 1024, RPI = 1024 / D, IPP = NI / PPV;
+    constexpr int STAGE = kVisit * D, NI = STAGE / 1024, IPP = NI / PPV;
     __shared__ __attribute__((aligned(1024))) uint8_t lds[NW * STAGE];
     __shared__ float acc_w[kStreamChunk * kVisit];
     __shared__ int pids[kStreamChunk * PPV];
