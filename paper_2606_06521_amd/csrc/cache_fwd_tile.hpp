@@ -13,7 +13,7 @@
 // What bounds it is vector work: per key and row an exp2 (half of the rate), an FMA,
 // an add, half a maximum and half a convert, and the widening of K's codes to bf16,
 // which 32 rows share: 66 % of the time, beside 38 % of the matrix cores'.  8 heads x 2048 x 4
-// rows against 16384 keys, d = 128: 411 to 421 us, 1.22 to 1.25 PFLOP/s; a large bf16
+// rows against 16384 keys, d = 128: 411 to 432 us over several runs, 1.19 to 1.25 PFLOP/s; a large bf16
 // product reaches 1.40.
 #pragma once
 
