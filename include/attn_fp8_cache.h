@@ -26,6 +26,7 @@
  *     most 2^26, else ATTN_ERR_UNSUPPORTED).  Tokens without a page are not written,
  *     and no query sees them; nor are tokens before position 0, whose queries see
  *     no key;
+ *   - T is at most 2^30 (else ATTN_ERR_UNSUPPORTED);
  *   - a sequence has at most max_q new tokens; those beyond are left out (not
  *     written, their rows of an output left as they were), as are cu entries
  *     outside 0 .. T.
@@ -159,7 +160,8 @@ int attn_fp8_cache_weights(const attn_fp8_cache *cache, const attn_fp8_batch *ba
  * what is left of the budget) and those of the largest weight; equal weights go
  * to the lower token, NaN counts as the lowest.  Sequences of at most budget
  * tokens move whole.  The moved block's scale is that of its own values.
- *   from, batch    the cache; of batch pages, lens, B and W are used.
+ *   from, batch    the cache, of at least one page; of batch pages, lens, B and W
+ *                  are used.
  *   to, new_pages  the cache that takes them (it may be the same arrays) and
  *                  int32 [B][ceil(budget / page)]: pages that hold none of the
  *                  batch's tokens.  Its slots that get no token are left alone.

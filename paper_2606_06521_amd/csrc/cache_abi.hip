@@ -41,8 +41,9 @@ int check_sizes(const attn_fp8_cache* c, const attn_fp8_batch* bt)
         return ATTN_ERR_UNSUPPORTED;
     if (c->page != 64 && c->page != 128)
         return ATTN_ERR_UNSUPPORTED;
-    // (the merge of a split call holds at most 4096 ranges)
-    if ((int64_t)bt->W * c->page > 1 << 26 || c->Hkv > 1 << 16 || bt->max_q > 1 << 26)
+    // (the merge of a split call holds at most 4096 ranges; the distance of a key and a
+    // token's position fits 32 bits)
+    if ((int64_t)bt->W * c->page > 1 << 26 || c->Hkv > 1 << 16 || bt->max_q > 1 << 26 || bt->T > 1 << 30)
         return ATTN_ERR_UNSUPPORTED;
     return ATTN_OK;
 }
@@ -284,8 +285,8 @@ int attn_fp8_cache_evict(const attn_fp8_cache* from, const attn_fp8_batch* batch
     if (st != ATTN_OK)
         return st;
     if (to->Hkv != from->Hkv || to->page != from->page || to->d != from->d || stride_b < 0 || stride_h < 0 || budget < 1 ||
-        n_sink < 0 || n_recent < 0)
-        return ATTN_ERR_INVALID_ARG;
+        n_sink < 0 || n_recent < 0 || (batch->B > 0 && from->n_pages < 1))
+        return ATTN_ERR_INVALID_ARG;    // (rows without a page load those of page 0)
     if (budget > 1 << 20)
         return ATTN_ERR_UNSUPPORTED;
     if (batch->B == 0)

@@ -218,3 +218,16 @@ def test_rope_table_is_the_formula_and_refuses(A):
         a.update(kw)
         with pytest.raises(ValueError):
             A.rope_table(a.pop("n_pos"), a.pop("rot"), **a)
+
+
+def test_sizes_past_32_bit_positions_and_caches_without_pages_are_refused(A):
+    """Past 2^30 tokens a key's distance from a position would wrap; an eviction loads page 0
+    for rows that have none."""
+    b, q, r = batch(A, cu=FAKE, T=(1 << 30) + 1), heads(A), rotation(A)
+    assert A.attn_fp8_cache_fwd(cache(A), b, q, 4, FAKE, 1, FAKE, 1, 0.1, 1.0, 0, None, 0, None) == -2
+    assert A.attn_fp8_cache_weights(cache(A), b, q, 4, FAKE, 1, 0.1, 1.0, 0, FAKE, 1024, 512, None) == -2
+    assert A.attn_fp8_cache_append(cache(A), b, q, q, r, None, None, 4, None) == -2
+    assert A.attn_fp8_cache_workspace_bytes(cache(A), b, 4, 0) == (-2, 0)
+    evict = lambda c, b: A.attn_fp8_cache_evict(c, b, cache(A), FAKE, FAKE, 1024, 512, 64, 4, 0, FAKE, FAKE, FAKE, None)
+    assert evict(cache(A, n_pages=0), batch(A)) == -1
+    assert evict(cache(A, n_pages=0), batch(A, B=0)) == 0
