@@ -123,7 +123,8 @@ int attn_fp8_cache_append(const attn_fp8_cache *cache, const attn_fp8_batch *bat
  *              (beyond: ATTN_ERR_UNSUPPORTED).
  *   out        contiguous [T][Hq][d], BF16 or F32 by out_type, 16-byte aligned.
  *   lse        FP32 [T][Hq], or NULL.
- *   sm_scale, q_descale   finite and > 0.
+ *   sm_scale, q_descale   finite and > 0, and so log2(e) times their product: a normal
+ *              FP32 number.
  *   max_len    no lens[b] is larger (keys from max_len on are not seen); 0: W * page.
  *              The plan goes by it, so a close bound is a faster call.
  *   workspace  256-byte aligned device memory of workspace_bytes, scratch of this

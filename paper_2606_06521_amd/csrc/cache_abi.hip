@@ -100,6 +100,9 @@ attn::Rotation rotation_of(const attn_fp8_rotation* r)
 
 int status(hipError_t e) { return e == hipSuccess ? ATTN_OK : ATTN_ERR_HIP; }
 
+// What a raw score is multiplied by on a block scale of 1.
+float factor_of(float sm_scale, float q_descale) { return (float)(1.4426950408889634074 * (double)sm_scale * (double)q_descale); }
+
 // The sizes and scalars that attention and weights share.
 int check_attention(const attn_fp8_cache* c, const attn_fp8_batch* bt, int Hq, int causal, float sm_scale, float q_descale,
                     int max_len)
@@ -108,7 +111,7 @@ int check_attention(const attn_fp8_cache* c, const attn_fp8_batch* bt, int Hq, i
     if (st != ATTN_OK)
         return st;
     if (Hq < 1 || Hq % c->Hkv != 0 || max_len < 0 || (causal != 0 && causal != 1) || !(sm_scale > 0.f) || !isfinite(sm_scale) ||
-        !(q_descale > 0.f) || !isfinite(q_descale))
+        !(q_descale > 0.f) || !isfinite(q_descale) || !isnormal(factor_of(sm_scale, q_descale)))
         return ATTN_ERR_INVALID_ARG;
     // (the row numbers of a sequence and KV head times the group stay below 2^32)
     const int G = Hq / c->Hkv;
@@ -232,7 +235,7 @@ int attn_fp8_cache_fwd(const attn_fp8_cache* cache, const attn_fp8_batch* batch,
     p.gr = attn::group_of(Hq / cache->Hkv);
     p.causal = causal;
     p.max_len = longest(cache, batch, max_len);
-    p.c = (float)(1.4426950408889634074 * (double)sm_scale * (double)q_descale);
+    p.c = factor_of(sm_scale, q_descale);
     const attn::FwdPlan pl = attn::cache_fwd_plan(batch->B, cache->Hkv, p.gr.G, batch->max_q, p.max_len, cache->d, n_cu);
     if (pl.bytes > 0 && (!workspace || workspace_bytes < pl.bytes))
         return ATTN_ERR_INVALID_ARG;
@@ -268,7 +271,7 @@ int attn_fp8_cache_weights(const attn_fp8_cache* cache, const attn_fp8_batch* ba
     p.gr = attn::group_of(Hq / cache->Hkv);
     p.causal = causal;
     p.max_len = most;
-    p.c = (float)(1.4426950408889634074 * (double)sm_scale * (double)q_descale);
+    p.c = factor_of(sm_scale, q_descale);
     int n_cu = 0;
     if ((st = device_cus(n_cu)) != ATTN_OK)
         return st;

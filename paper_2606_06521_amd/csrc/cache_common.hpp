@@ -118,6 +118,13 @@ __device__ inline void from_e4m3(uint32_t w, float* x)
     x[3] = __builtin_amdgcn_cvt_f32_fp8((int)w, 3);
 }
 
+// Factor of a block's scores, c 2^(byte - 127), kept off 0 and infinity: a masked key's
+// -inf stays one, and a score of 0 too.
+__device__ inline float score_factor(float c, int byte)
+{
+    return __builtin_amdgcn_fmed3f(__builtin_amdgcn_ldexpf(c, byte - 127), 0x1p-149f, 0x1.fffffep127f);
+}
+
 // ---- eight consecutive values of an element type ----
 
 template <int TYPE>

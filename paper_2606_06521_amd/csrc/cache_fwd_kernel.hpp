@@ -222,8 +222,7 @@ __global__ void __launch_bounds__(256, 1) cache_fwd_kernel(FwdParams p)
     for (int v = v0 + w; v < v1; v += NW) {
         // the pages of the visit's two halves
         const int pi = (v - v0) * PPV;
-        const float c[2] = {__builtin_amdgcn_ldexpf(p.c, (int)kbyte[pi] - 127),
-                            __builtin_amdgcn_ldexpf(p.c, (int)kbyte[pi + PPV - 1] - 127)};
+        const float c[2] = {score_factor(p.c, kbyte[pi]), score_factor(p.c, kbyte[pi + PPV - 1])};
         const int sa = vbyte[pi + (g >= 2 ? PPV - 1 : 0)];
         const bool there[2] = {pids[pi] >= 0, pids[pi + PPV - 1] >= 0};
         // ---- scores (K is older than V: wait for all but V's loads) ----

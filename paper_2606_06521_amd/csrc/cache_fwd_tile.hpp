@@ -166,8 +166,7 @@ __global__ void __launch_bounds__(256, 2) cache_fwd_tile_kernel(FwdParams p)
         if (wrow0 >= rows)
             continue;
         const int pi = (v - v0) * PPV;
-        const float c[2] = {__builtin_amdgcn_ldexpf(p.c, (int)kbyte[pi] - 127),
-                            __builtin_amdgcn_ldexpf(p.c, (int)kbyte[pi + PPV - 1] - 127)};
+        const float c[2] = {score_factor(p.c, kbyte[pi]), score_factor(p.c, kbyte[pi + PPV - 1])};
         const int sa[2] = {vbyte[pi], vbyte[pi + PPV - 1]};
         const bool there[2] = {pids[pi] >= 0, pids[pi + PPV - 1] >= 0};
         f32x16 sc[KT];

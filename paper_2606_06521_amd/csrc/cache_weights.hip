@@ -169,7 +169,7 @@ __global__ void __launch_bounds__(512, 1) weights_stream_kernel(WeightParams p, 
         float sum[KT];
 #pragma unroll
         for (int kt = 0; kt < KT; ++kt) {
-            const float c = __builtin_amdgcn_ldexpf(p.c, (int)kbyte[(v - v0) * PPV + 16 * kt / PAGE] - 127);
+            const float c = score_factor(p.c, kbyte[(v - v0) * PPV + 16 * kt / PAGE]);
             bf16x8 kf[2 * KP];
 #pragma unroll
             for (int i = 0; i < KP; ++i) {
@@ -287,7 +287,7 @@ __global__ void __launch_bounds__(256, 2) weights_tall_kernel(WeightParams p, in
         }
     }
     const int pid = __builtin_amdgcn_readfirstlane(page_of(p.bt, p.cache.n_pages, b, (t0 + 16 * KT * kh) / PAGE));
-    const float c = pid < 0 ? 0.f : __builtin_amdgcn_ldexpf(p.c, (int)p.cache.ks[(size_t)pid * p.cache.Hkv + hk] - 127);
+    const float c = pid < 0 ? 0.f : score_factor(p.c, p.cache.ks[(size_t)pid * p.cache.Hkv + hk]);
     float lse2 = 0.f;
     int last = -1;
     if (tid < SEG) {

@@ -231,3 +231,11 @@ def test_sizes_past_32_bit_positions_and_caches_without_pages_are_refused(A):
     evict = lambda c, b: A.attn_fp8_cache_evict(c, b, cache(A), FAKE, FAKE, 1024, 512, 64, 4, 0, FAKE, FAKE, FAKE, None)
     assert evict(cache(A, n_pages=0), batch(A)) == -1
     assert evict(cache(A, n_pages=0), batch(A, B=0)) == 0
+
+
+@pytest.mark.parametrize("sm,qd", [(1e-30, 1e-30), (1e30, 1e30), (1e-20, 1e-19), (3e38, 1.0)])
+def test_factors_that_fp32_does_not_hold_are_refused(A, sm, qd):
+    """log2(e) sm_scale q_descale of 0, infinity or below 2^-126."""
+    c, b, q = cache(A), batch(A), heads(A)
+    assert A.attn_fp8_cache_fwd(c, b, q, 4, FAKE, 1, FAKE, 1, sm, qd, 0, None, 0, None) == -1
+    assert A.attn_fp8_cache_weights(c, b, q, 4, FAKE, 1, sm, qd, 0, FAKE, 1024, 512, None) == -1

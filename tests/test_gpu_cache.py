@@ -529,6 +529,24 @@ def test_fwd_queries_that_are_not_finite_stay_in_their_rows(A):
     within(l[~bad], wl[~bad], lb[~bad])
 
 
+@pytest.mark.parametrize("d,page,G,new", [(64, 64, 2, 6), (128, 128, 4, 1), (128, 64, 4, 130), (64, 128, 8, 40)])
+def test_factors_below_fp32_leave_masked_keys_out(A, d, page, G, new):
+    """Blocks of zeros (scale 2^-127) and a small descale: the factor of their scores lies below FP32's
+    least value, the scores are 0, and keys that a row does not see get nothing."""
+    rng = np.random.default_rng(d + G)
+    n = 200 + new
+    c = R.make_cache(rng, 1, 1, page, d, [n])
+    c.k[:], c.ks[:] = 0, 0
+    q = R.make_queries(rng, new, G, d)
+    log(f"small factor d={d} page={page} G={G} new={new}")
+    _, lse, _ = run_fwd(A, c, q, G, "bf16", sm_scale=2.0 ** -10, q_descale=2.0 ** -30)
+    w = torch.zeros((1, 1, c.pages.shape[1] * page), device="cuda")
+    A.cache_weights(R.torch_q(q, "bf16").cuda(), lse, dev_cache(A, c), dev(c.pages), dev(c.lens), w, sm_scale=2.0 ** -10,
+                    q_descale=2.0 ** -30)
+    want = R.weights(c, q, lse.cpu().numpy(), G, w.shape[2], sm_scale=2.0 ** -10, q_descale=2.0 ** -30)
+    within(w.cpu().double().numpy(), want, 2.0 ** -17 * want)
+
+
 # ---- sizes and arguments at the edges ----
 
 def test_cache_beyond_four_gigabytes(A):
