@@ -145,7 +145,8 @@ int attn_fp8_cache_workspace_bytes(const attn_fp8_cache *cache, const attn_fp8_b
  * Attention weight that the cached tokens receive: adds to weights[b][hk][t] the
  * softmax weights exp(z - lse) of key t over the new tokens and query heads of
  * the group that see it (z = x_t ln 2 as above).  lse is what attn_fp8_cache_fwd
- * gave for the same call; a row of lse = -inf adds nothing.
+ * gave for the same call (its FP32 rounding is in z - lse: weights are good while |lse|
+ * is far below 2^23); a row of lse = -inf adds nothing.
  *   weights    FP32 [B][Hkv][..], stride_b and stride_h elements apart; entries
  *              t < min(lens[b], max_len) are updated, the others left as they
  *              were.  max_len 0: W * page.  max_len <= stride_h.

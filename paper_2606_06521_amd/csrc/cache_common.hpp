@@ -287,6 +287,24 @@ __device__ inline int ones(int count)
 // first have to quieten each score).
 __device__ inline float max_of(float a, float b) { return __builtin_elementwise_maximum(a, b); }
 
+// A lane's part of a query row: f for which all |x| of the row on a score factor c are below
+// 2^22 if c f <= 1 for its lanes (|code| <= 448).  Beyond, a score's FP32 product and the
+// exact one may differ by more than the codes have room for (448 / 2^8).
+template <int N>
+__device__ inline float far_factor(const bf16x8* q, int d)
+{
+    typedef uint16_t u16x8 __attribute__((ext_vector_type(8)));
+    u16x8 m = {};
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+        m = __builtin_elementwise_max(m, __builtin_bit_cast(u16x8, q[i]) & (u16x8)((uint16_t)0x7FFF));
+    uint16_t top = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        top = m[i] > top ? m[i] : top;
+    return __uint_as_float((uint32_t)top << 16) * (448.f / 0x1p22f * (float)d);
+}
+
 // ---- host side ----
 
 struct FwdParams {

@@ -204,6 +204,7 @@ __global__ void __launch_bounds__(256, 1) cache_fwd_kernel(FwdParams p)
     }
     lds_barrier();
 
+    const float far = far_factor<2 * KP>(qf, D);
     f32x4 o[DT];
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt)
@@ -222,7 +223,7 @@ __global__ void __launch_bounds__(256, 1) cache_fwd_kernel(FwdParams p)
     for (int v = v0 + w; v < v1; v += NW) {
         // the pages of the visit's two halves
         const int pi = (v - v0) * PPV;
-        const float c[2] = {score_factor(p.c, kbyte[pi]), score_factor(p.c, kbyte[pi + PPV - 1])};
+        float c[2] = {score_factor(p.c, kbyte[pi]), score_factor(p.c, kbyte[pi + PPV - 1])};
         const int sa = vbyte[pi + (g >= 2 ? PPV - 1 : 0)];
         const bool there[2] = {pids[pi] >= 0, pids[pi + PPV - 1] >= 0};
         // ---- scores (K is older than V: wait for all but V's loads) ----
@@ -273,6 +274,15 @@ __global__ void __launch_bounds__(256, 1) cache_fwd_kernel(FwdParams p)
             mx = fmax_f(__uint_as_float(sw[0]), __uint_as_float(sw[1]));
             // (all of them NaN: any M hands the NaN on)
             M[hf] = mx != mx ? 0.f : __builtin_ceilf(mx * c[hf]);
+        }
+        // (there the FP32 products themselves are the scores)
+        if (__ballot(fmax_f(c[0], c[1]) * far > 1.f) != 0) {
+#pragma unroll
+            for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    sc[kt][r] *= c[kt / 4];
+            c[0] = c[1] = 1.f;
         }
         const float hi = fmax_f(M[0], M[1]);
         if (__ballot(hi > ref + kSlack) != 0) {

@@ -13,8 +13,8 @@
 // What bounds it is vector work: per key and row an exp2 (half of the rate), an FMA,
 // an add, half a maximum and half a convert, and the widening of K's codes to bf16,
 // which 32 rows share: 66 % of the time, beside 38 % of the matrix cores'.  8 heads x 2048 x 4
-// rows against 16384 keys, d = 128: 411 to 432 us over several runs, 1.19 to 1.25 PFLOP/s; a large bf16
-// product reaches 1.40.
+// rows against 16384 keys, d = 128: 406 us, 1.27 PFLOP/s (2 % more or less from card to card); a large
+// bf16 product reaches 1.40.
 #pragma once
 
 #include "cache_fwd_kernel.hpp"
@@ -113,6 +113,12 @@ __global__ void __launch_bounds__(256, 2) cache_fwd_tile_kernel(FwdParams p)
             qf[j] = load_q8<E4M3>(p.q.data, at + 32 * (j / 2) + 16 * h + 8 * (j % 2));
     }
 
+    // (of the wave's rows, in a scalar register; NaN of a row does not count)
+    float far = far_factor<2 * KP>(qf, D);
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1)
+        far = fmax_f(far, __shfl_xor(far, off, 64));
+    far = __uint_as_float((uint32_t)__builtin_amdgcn_readfirstlane((int)__float_as_uint(far)));
     f32x16 o[DT];
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt)
@@ -166,7 +172,7 @@ __global__ void __launch_bounds__(256, 2) cache_fwd_tile_kernel(FwdParams p)
         if (wrow0 >= rows)
             continue;
         const int pi = (v - v0) * PPV;
-        const float c[2] = {score_factor(p.c, kbyte[pi]), score_factor(p.c, kbyte[pi + PPV - 1])};
+        float c[2] = {score_factor(p.c, kbyte[pi]), score_factor(p.c, kbyte[pi + PPV - 1])};
         const int sa[2] = {vbyte[pi], vbyte[pi + PPV - 1]};
         const bool there[2] = {pids[pi] >= 0, pids[pi + PPV - 1] >= 0};
         f32x16 sc[KT];
@@ -204,6 +210,15 @@ __global__ void __launch_bounds__(256, 2) cache_fwd_tile_kernel(FwdParams p)
                 mx = max_of(mx, sc[kt][r]);
             mx = halves_max(mx);
             M[kt] = mx != mx ? 0.f : __builtin_ceilf(mx * c[kt / 2]);
+        }
+        // (there the FP32 products themselves are the scores)
+        if (__ballot(fmax_f(c[0], c[1]) * far > 1.f) != 0) {
+#pragma unroll
+            for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    sc[kt][r] *= c[kt / 2];
+            c[0] = c[1] = 1.f;
         }
         const float hi = fmax_f(fmax_f(M[0], M[1]), fmax_f(M[2], M[3]));
         if (__ballot(hi > ref + kSlack) != 0) {

@@ -547,6 +547,39 @@ def test_factors_below_fp32_leave_masked_keys_out(A, d, page, G, new):
     within(w.cpu().double().numpy(), want, 2.0 ** -17 * want)
 
 
+@pytest.mark.parametrize("d,page,G,new", [(64, 64, 2, 6), (128, 128, 4, 1), (128, 64, 4, 130), (64, 128, 8, 40)])
+def test_fwd_scores_beyond_two_to_the_thirty(A, d, page, G, new):
+    """Scores so large that FP32 has no fraction for them: the softmax of their FP32 values, whose
+    differences are 0 or far above 30, so a row's result is the mean of the values of its largest keys.
+    Its bound: the matrix core's 8 2^-13 of the largest product; lse is M ln 2 in FP32, two roundings
+    and log2 of a count."""
+    rng = np.random.default_rng(3 * d + G)
+    n = 260 + new
+    c = R.make_cache(rng, 1, 1, page, d, [n])
+    c.ks[:] = rng.choice([163, 167, 171], c.ks.shape)
+    q = R.make_queries(rng, new, G, d)
+    q[::3] = -np.abs(q[::3])                            # with the keys of some blocks all positive: all scores
+    c.k[c.pages[0, 0]] &= 0x7F                          # of a block, or nearly, below 0
+    log(f"far scores d={d} page={page} G={G} new={new}")
+    out, lse, _ = run_fwd(A, c, q, G, "bf16", check=False)
+    c32 = np.float32(R.LOG2E * np.float32(1 / math.sqrt(d)).astype(np.float64))
+    D, cf, _ = R.scores(c, 0, 0, q.reshape(-1, d), c32)
+    assert np.array_equal(D, D.astype(np.float32))
+    x = (D.astype(np.float32) * cf.astype(np.float32)).astype(np.float64)
+    see = np.arange(n)[None] <= np.repeat(n - new + np.arange(new), G)[:, None]
+    x = np.where(see, x, -np.inf)
+    top = x.max(1, keepdims=True)
+    others = np.where(x == top, -np.inf, x).max(1)
+    assert (np.abs(top) > 2.0 ** 30).all() and (top[:, 0] - others > 64).all()
+    v, ve, _ = R.Pages.keys(c, 0, 0, "v")
+    v = v * 2.0 ** ve[:, None]
+    p = (x == top) / (x == top).sum(1, keepdims=True)
+    o, l = out.cpu().double().numpy().reshape(-1, d), lse.cpu().double().numpy().reshape(-1)
+    within(o, p @ v, np.broadcast_to(2.0 ** -10 * np.abs(v).max(), o.shape))
+    wl = (top[:, 0] + np.log2((x == top).sum(1))) * math.log(2.0)
+    within(l, wl, 2.0 ** -22 * np.abs(wl))
+
+
 # ---- sizes and arguments at the edges ----
 
 def test_cache_beyond_four_gigabytes(A):
