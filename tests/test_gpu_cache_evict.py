@@ -1,0 +1,76 @@
+"""Eviction from long caches: each of the kernels that choose (by the tokens that the page table has
+room for: up to 4096, 8192 and 16384 in registers, any number beyond), against the definition."""
+import numpy as np
+import pytest
+import torch
+
+from tests import cache_ref as R
+from tests.gpu_helpers import log
+from tests.test_gpu_cache import dev, dev_cache, same_cache
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def A():
+    from paper_2606_06521_amd import attn_fp8
+    return attn_fp8
+
+
+def hard_weights(rng, shape):
+    """Few distinct values (ties at the border), zeros of both signs, negative ones, NaN, infinities."""
+    w = np.round(rng.standard_normal(shape) * 4).astype(np.float32)
+    flat = w.reshape(-1)
+    for x, n in ((np.nan, 40), (np.inf, 9), (-np.inf, 9), (-0.0, 40)):
+        flat[rng.integers(0, flat.size, n)] = x
+    return w
+
+
+# lens, tokens that the table has room for, budget, n_sink, n_recent
+CASES = [
+    ([4097, 5000, 64], 5000, 1001, 4, 32), ([8192, 700], 8192, 8000, 0, 0), ([300, 129, 0], 7000, 100, 4, 0),
+    ([12000, 8193, 1], 12000, 2500, 4, 100), ([16384], 16384, 130, 0, 0), ([16383, 900], 16384, 16000, 64, 3000),
+    ([16385, 3000], 16385, 4001, 4, 32), ([40000, 17000], 40000, 9000, 0, 128), ([20000], 20000, 19999, 4, 16),
+    ([300, 129, 0, 64], 33000, 100, 4, 32), ([1025, 1024, 1023], 33000, 1000, 0, 1), ([20000], 20000, 50, 20, 60),
+]
+
+
+@pytest.mark.parametrize("d,page", [(64, 64), (128, 128)])
+@pytest.mark.parametrize("case", range(len(CASES)))
+def test_evict(A, case, d, page):
+    lens, room, budget, n_sink, n_recent = CASES[case]
+    B, Hkv, W = len(lens), 2, -(-room // page)
+    log(f"evict {lens} of {W * page} budget={budget} sink={n_sink} recent={n_recent} d={d} page={page}")
+    rng = np.random.default_rng(sum(lens) + budget)
+    c = R.make_cache(rng, B, Hkv, page, d, lens, W=W, spread=12)
+    w = hard_weights(rng, (B, Hkv, W * page))
+    nb = -(-budget // page)
+    to = R.make_cache(rng, B, Hkv, page, d, [nb * page] * B)
+    new_pages = to.pages.copy()
+    gt = dev_cache(A, to)
+    kept, new_lens, nw = A.cache_evict(dev_cache(A, c), dev(c.pages), dev(c.lens), dev(w), gt, dev(new_pages), budget,
+                                       n_sink=n_sink, n_recent=n_recent)
+    wk, wl, ww = R.evict(c, w, budget, n_sink, n_recent, to, new_pages)
+    assert np.array_equal(kept.cpu().numpy(), wk)
+    assert np.array_equal(new_lens.cpu().numpy(), wl)
+    assert np.array_equal(nw.cpu().numpy(), ww, equal_nan=True)
+    same_cache(gt, to)
+
+
+@pytest.mark.parametrize("room", [4096, 8192, 16384, 20000])
+def test_weights_of_one_value_and_of_all_bits(A, room):
+    """All weights equal (the earliest stay), and weights of any bits."""
+    rng = np.random.default_rng(room)
+    c = R.make_cache(rng, 1, 2, 64, 64, [room - 5])
+    n_w = c.pages.shape[1] * 64
+    same = np.full((1, 2, n_w), 0.25, dtype=np.float32)
+    bits = rng.integers(0, 1 << 32, (1, 2, n_w), dtype=np.uint64).astype(np.uint32).view(np.float32)
+    for name, w in (("same", same), ("bits", bits)):
+        log(f"evict {name} {room}")
+        to = R.make_cache(rng, 1, 2, 64, 64, [1000 + 24])
+        gt = dev_cache(A, to)
+        kept, _, nw = A.cache_evict(dev_cache(A, c), dev(c.pages), dev(c.lens), dev(w), gt, dev(to.pages), 1000, n_sink=2, n_recent=7)
+        wk, _, ww = R.evict(c, w, 1000, 2, 7, to, to.pages)
+        assert np.array_equal(kept.cpu().numpy(), wk)
+        assert torch.equal(nw.cpu().view(torch.int32), torch.from_numpy(ww).view(torch.int32))
+        same_cache(gt, to)
