@@ -125,6 +125,19 @@ __device__ inline float score_factor(float c, int byte)
     return __builtin_amdgcn_fmed3f(__builtin_amdgcn_ldexpf(c, byte - 127), 0x1p-149f, 0x1.fffffep127f);
 }
 
+// Binary exponent of 2^(from - to), from <= to powers of two of a row's sums: applied with
+// ldexp, since as a number it underflows where a sum of large values does not (a sum of 2^128
+// at most: 2^-300 of it is 0).  from = -inf: a sum of 0.
+__device__ inline int shift_of(float from, float to)
+{
+    return from == to || from == -INFINITY ? 0 : (int)__builtin_fmaxf(from - to, -300.f);
+}
+
+// What of V's scale byte goes into the scale of P: a matrix core's scale ends at 2^-127, a group's
+// power of two relative to the row's does not (down to -119 - this it is exact; up to kSlack
+// the byte stays below 255).
+__device__ inline int lent_scale(int vbyte) { return min(vbyte, 119); }
+
 // ---- eight consecutive values of an element type ----
 
 template <int TYPE>

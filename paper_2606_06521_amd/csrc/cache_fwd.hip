@@ -67,11 +67,11 @@ __global__ void __launch_bounds__(256) cache_merge(FwdParams p, int tile_rows)
         const float* at = base + c * stride;
         const f32x4 x = *reinterpret_cast<const f32x4*>(at + rr * D + 4 * piece);
         const float lc = at[tile_rows * D + rr], mc = PARTS > 1 ? msh[c] : at[tile_rows * (D + 1) + rr];
-        const float f = mc == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mc - m);
+        const int down = shift_of(mc, m);
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-            acc[e] += x[e] * f;
-        l += lc * f;
+            acc[e] += __builtin_amdgcn_ldexpf(x[e], down);
+        l += __builtin_amdgcn_ldexpf(lc, down);
     }
     if constexpr (PARTS > 1) {
         osh[sub][part][piece] = acc;

@@ -224,7 +224,8 @@ __global__ void __launch_bounds__(256, 1) cache_fwd_kernel(FwdParams p)
         // the pages of the visit's two halves
         const int pi = (v - v0) * PPV;
         float c[2] = {score_factor(p.c, kbyte[pi]), score_factor(p.c, kbyte[pi + PPV - 1])};
-        const int sa = vbyte[pi + (g >= 2 ? PPV - 1 : 0)];
+        const int lent[2] = {lent_scale(vbyte[pi]), lent_scale(vbyte[pi + PPV - 1])};
+        const int sa = vbyte[pi + (g >= 2 ? PPV - 1 : 0)] - (g >= 2 ? lent[1] : lent[0]);
         const bool there[2] = {pids[pi] >= 0, pids[pi + PPV - 1] >= 0};
         // ---- scores (K is older than V: wait for all but V's loads) ----
         asm volatile("s_waitcnt vmcnt(%0)" :: "n"(NI) : "memory");
@@ -288,14 +289,14 @@ __global__ void __launch_bounds__(256, 1) cache_fwd_kernel(FwdParams p)
         if (__ballot(hi > ref + kSlack) != 0) {
             const float top = halves_max(hi);
             const float to = top > ref + kSlack ? top : ref;
-            const float f = to == ref || ref == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(ref - to);
+            const int down = shift_of(ref, to);
             ref = to;
-            ell *= f;
+            ell = __builtin_amdgcn_ldexpf(ell, down);
 #pragma unroll
             for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
                 for (int r = 0; r < 4; ++r)
-                    o[dt][r] *= f;
+                    o[dt][r] = __builtin_amdgcn_ldexpf(o[dt][r], down);
         }
         i32x8 pk;
         uint32_t sb[2];
@@ -303,7 +304,7 @@ __global__ void __launch_bounds__(256, 1) cache_fwd_kernel(FwdParams p)
         for (int hf = 0; hf < 2; ++hf) {
             const bool none = M[hf] == -INFINITY;
             const float nm = none ? 0.f : -M[hf];
-            // (at most kSlack; 2^-300 is none)
+            // (at most kSlack; 2^-300 of anything is 0)
             const int up = (int)__builtin_fmaxf(none ? -300.f : M[hf] - ref, -300.f);
             float sum = 0.f;
 #pragma unroll
@@ -320,8 +321,8 @@ __global__ void __launch_bounds__(256, 1) cache_fwd_kernel(FwdParams p)
                 pk[kt] = __builtin_bit_cast(int, word);
             }
             ell += __builtin_amdgcn_ldexpf(sum, up);
-            // the group's scale, and the 2^8 of the codes taken back (2^-127 is as good as none)
-            sb[hf] = (uint32_t)max(127 - 8 + up, 0);
+            // the group's scale, and the 2^8 of the codes taken back
+            sb[hf] = (uint32_t)max(127 - 8 + lent[hf] + up, 0);
         }
         // group j of the visit's four gets its scale from lane group j: 0 and 1 are the
         // first half's of lane groups 0, 1 and 2, 3; 2 and 3 the second half's
@@ -379,14 +380,14 @@ __global__ void __launch_bounds__(256, 1) cache_fwd_kernel(FwdParams p)
 #pragma unroll
     for (int i = 1; i < NW; ++i)
         m = fmax_f(m, msh[i][n]);
-    const float f = ref == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ref - m);
+    const int down = shift_of(ref, m);
     float* const mw = reinterpret_cast<float*>(lds) + (w * TR + n) * MS;
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) {
         f32x4 x;
 #pragma unroll
         for (int r = 0; r < 4; ++r)
-            x[r] = o[dt][r] * f;
+            x[r] = __builtin_amdgcn_ldexpf(o[dt][r], down);
         *reinterpret_cast<f32x4*>(mw + 16 * dt + 4 * g) = x;
     }
     __syncthreads();

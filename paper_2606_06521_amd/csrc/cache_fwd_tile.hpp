@@ -173,7 +173,8 @@ __global__ void __launch_bounds__(256, 2) cache_fwd_tile_kernel(FwdParams p)
             continue;
         const int pi = (v - v0) * PPV;
         float c[2] = {score_factor(p.c, kbyte[pi]), score_factor(p.c, kbyte[pi + PPV - 1])};
-        const int sa[2] = {vbyte[pi], vbyte[pi + PPV - 1]};
+        const int lent[2] = {lent_scale(vbyte[pi]), lent_scale(vbyte[pi + PPV - 1])};
+        const int sa[2] = {vbyte[pi] - lent[0], vbyte[pi + PPV - 1] - lent[1]};
         const bool there[2] = {pids[pi] >= 0, pids[pi + PPV - 1] >= 0};
         f32x16 sc[KT];
         __builtin_amdgcn_s_setprio(1);
@@ -223,14 +224,14 @@ __global__ void __launch_bounds__(256, 2) cache_fwd_tile_kernel(FwdParams p)
         const float hi = fmax_f(fmax_f(M[0], M[1]), fmax_f(M[2], M[3]));
         if (__ballot(hi > ref + kSlack) != 0) {
             const float to = hi > ref + kSlack ? hi : ref;
-            const float f = to == ref || ref == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(ref - to);
+            const int down = shift_of(ref, to);
             ref = to;
-            ell *= f;
+            ell = __builtin_amdgcn_ldexpf(ell, down);
 #pragma unroll
             for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
                 for (int r = 0; r < 16; ++r)
-                    o[dt][r] *= f;
+                    o[dt][r] = __builtin_amdgcn_ldexpf(o[dt][r], down);
         }
         int pk[4 * KT], sb[KT];
 #pragma unroll
@@ -253,7 +254,7 @@ __global__ void __launch_bounds__(256, 2) cache_fwd_tile_kernel(FwdParams p)
                 pk[4 * kt + r4] = __builtin_bit_cast(int, word);
             }
             ell += __builtin_amdgcn_ldexpf(sum, up);
-            sb[kt] = max(127 - 8 + up, 0);
+            sb[kt] = max(127 - 8 + lent[kt / 2] + up, 0);
         }
         // ---- O^T += V^T P^T ----
         __builtin_amdgcn_s_setprio(1);

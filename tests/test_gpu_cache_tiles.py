@@ -206,6 +206,52 @@ def test_queries_that_are_not_finite_stay_in_their_rows(A):
     within(l[~bad], wl[~bad], lb[~bad])
 
 
+def far_cache(rng, page, d, lens):
+    """Blocks whose scores lie hundreds of powers of two apart and whose values do too: where a
+    row's near blocks have a zero code, its far ones are what is left."""
+    c = R.make_cache(rng, len(lens), 2, page, d, lens)
+    c.ks[:] = rng.integers(118, 133, c.ks.shape)
+    c.vs[:] = rng.choice([20, 60, 100, 127, 180, 200], c.vs.shape)
+    return c
+
+
+def check_far(A, c, q, G, kind, new, max_q):
+    """As check, with FP32's range: sums below 2^-100 (each of n <= 2^11 keys drops what lies below
+    2^-126 as an FP32 number, or is of a group below 2^(-119 - 119) with values of at most 2^83; by
+    l >= 1/2) are not looked at."""
+    o, l = call(A, c, q, kind, new, max_q, sm_scale=0.25, q_descale=0.75)
+    want, wl, bound, lb = R.attention(c, q, G, cu=cu_of(new), sm_scale=0.25, q_descale=0.75)
+    within(o, want, bound + 2.0 ** -100)
+    within(l, wl, lb)
+    return want, bound
+
+
+@pytest.mark.parametrize("kind", ["bf16", "e4m3"])
+@pytest.mark.parametrize("d,page", [(64, 64), (128, 128), (128, 64)])
+def test_far_groups_of_large_values(A, d, page, kind):
+    rng = np.random.default_rng(8)
+    new = [60, 41]
+    c = far_cache(rng, page, d, [700, 450])
+    q = R.make_queries(rng, sum(new), 4, d)
+    max_q, _ = tall(c, 2, new)
+    log(f"tall far groups d={d} page={page} {kind}")
+    check_far(A, c, q, 2, kind, new, max_q)
+
+
+@pytest.mark.parametrize("B,G,max_q,n,d,rows", [(2, 4, 1, 2000, 64, 16), (2, 4, 1, 2000, 128, 16), (2, 4, 400, 2000, 128, 128),
+                                                (2, 8, 12, 500, 64, 16)])
+def test_far_groups_in_ranges_and_waves(A, B, G, max_q, n, d, rows):
+    """The same where waves, and ranges with a merge, stand at their own powers of two."""
+    rng = np.random.default_rng(n + d + max_q)
+    new = [min(max_q, 30), 1]
+    c = far_cache(rng, 64, d, [n, 130])
+    plan = fwd_plan(B, 2, G, max_q, c.pages.shape[1] * 64, d, n_cu())
+    assert plan.rows == rows and (plan.ranges > 1) == (n == 2000)
+    q = R.make_queries(rng, sum(new), 2 * G, d)
+    log(f"far groups G={G} max_q={max_q} n={n} d={d} ranges={plan.ranges}")
+    check_far(A, c, q, G, "bf16", new, max_q)
+
+
 @pytest.mark.parametrize("d,page,G,new", [(64, 64, 2, 6), (128, 128, 4, 1), (128, 64, 4, 130), (64, 128, 8, 40)])
 def test_factors_below_fp32_leave_masked_keys_out(A, d, page, G, new):
     """Blocks of zeros (scale 2^-127) and a small descale: scores of 0, and keys that a row does not see
