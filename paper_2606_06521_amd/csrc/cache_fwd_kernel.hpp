@@ -179,7 +179,8 @@ __global__ void __launch_bounds__(256, 1) cache_fwd_kernel(FwdParams p)
 #pragma unroll
     for (int c = 0; c < (kMaxChunk * PPV + 255) / 256; ++c) {
         const int i = tid + 256 * c;
-        const int pid = i < np ? pids[i] : -1;
+        // (a page behind the last key that a row sees may hold anything)
+        const int pid = i < np && (v0 * PPV + i) * PAGE < seen ? pids[i] : -1;
         const size_t at = (size_t)(pid < 0 ? 0 : pid) * p.cache.Hkv + hk;
         kb0[c] = pid < 0 ? 127 : p.cache.ks[at];
         vb0[c] = pid < 0 ? 127 : p.cache.vs[at];

@@ -98,7 +98,8 @@ __global__ void __launch_bounds__(256, 2) cache_fwd_tile_kernel(FwdParams p)
     // the first visit's K and V travel while the scales and Q arrive
     issue(v0);
     for (int i = tid; i < np; i += 256) {
-        const int pid = pids[i];
+        // (a page behind the last key that a row sees may hold anything)
+        const int pid = (v0 * PPV + i) * PAGE < seen ? pids[i] : -1;
         const size_t at = (size_t)(pid < 0 ? 0 : pid) * p.cache.Hkv + hk;
         kbyte[i] = pid < 0 ? 127 : p.cache.ks[at];
         vbyte[i] = pid < 0 ? 127 : p.cache.vs[at];

@@ -329,3 +329,32 @@ def test_captured_chunk_follows_the_lengths(A):
         t = sum(new)
         assert torch.equal(out[:t], eager[i][0][:t]) and torch.equal(lse[:t], eager[i][1][:t])
         assert bool((out[t:] == 3.0).all())
+
+
+@pytest.mark.parametrize("byte", [0, 200, 255])
+@pytest.mark.parametrize("max_q", [1, 16, 0])
+@pytest.mark.parametrize("d", [64, 128])
+def test_scales_of_pages_behind_the_length_are_not_looked_at(A, d, max_q, byte):
+    """Pages reserved for later tokens, whose codes and scale bytes nobody has written: a visit of 128 keys
+    holds two pages of 64.  max_q 0: tiles of 128 rows."""
+    rng = np.random.default_rng(d + max_q)
+    lens, new = [40, 190, 64], [1, min(max(max_q, 1), 7), 1]
+    c = R.make_cache(rng, 3, 2, 64, d, [n + 64 for n in lens])
+    c.lens[:] = lens
+    if max_q == 0:
+        new = [30, 50, 1]
+        max_q, _ = tall(c, 2, new)
+    for b, n in enumerate(lens):
+        later = c.pages[b, -(-n // 64):]
+        later = later[later >= 0]
+        assert later.size
+        c.k[later], c.v[later], c.ks[later], c.vs[later] = 0x7F, 0x7F, 127, 127
+        c.k[c.pages[b, n // 64], :, n % 64:], c.v[c.pages[b, n // 64], :, n % 64:] = 0x7F, 0x7F
+    q = R.make_queries(rng, sum(new), 4, d)
+    log(f"scales behind the length d={d} max_q={max_q} byte={byte}")
+    o, l = check(A, c, q, 2, "bf16", new, max_q)
+    for b, n in enumerate(lens):
+        later = c.pages[b, -(-n // 64):]
+        c.ks[later[later >= 0]], c.vs[later[later >= 0]] = byte, byte
+    o2, l2 = call(A, c, q, "bf16", new, max_q)
+    assert np.array_equal(o, o2) and np.array_equal(l, l2)
