@@ -111,7 +111,7 @@ int attn_fp8_cache_append(const attn_fp8_cache *cache, const attn_fp8_batch *bat
  * KV head h / (Hq / Hkv).  With D the dot product of q and the codes of key t,
  *   x_t = D 2^(k byte - 127) log2(e) sm_scale q_descale     (FP32)
  * over the keys the query sees: t <= its position with causal = 1, all lens[b]
- * with causal = 0.  P is rounded to E4M3 in groups of 32 keys [32 g, 32 g + 32),
+ * with causal = 0 (none in either case for a token before position 0).  P is rounded to E4M3 in groups of 32 keys [32 g, 32 g + 32),
  * each relative to its own power of two:
  *   M_g = ceil(largest x_t of the group),  code_t = E4M3(2^8 2^(x_t - M_g)),
  * so no group underflows for another's maximum and neither the codes nor their

@@ -442,7 +442,8 @@ def cache_fwd(q, cache, pages, lens, *, cu=None, max_q=None, causal: bool = True
     """Attention of new tokens q [T, Hq, d] (bfloat16 or float8_e4m3fn) over their
     sequences' cached ones, the new ones included; returns (out [T, Hq, d] of out_dtype
     (bfloat16 or float32), lse [T, Hq] float32 or None).  Token i of a sequence's n is
-    at position lens[b] - n + i and sees the keys up to it (causal=False: all).
+    at position lens[b] - n + i and sees the keys up to it (causal=False: all); before
+    position 0, as the front of a padded batch, it sees none and gets out = 0, lse = -inf.
     pages, lens, cu, max_q as for cache_append.  sm_scale None: 1 / sqrt(d).
     max_len: no sequence is longer (0: as long as pages allows)."""
     return _call(stream, _binding.fwd, q, cache, pages, lens, cu, max_q, causal, sm_scale, q_descale, max_len, out,

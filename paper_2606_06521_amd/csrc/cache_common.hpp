@@ -74,6 +74,13 @@ __device__ inline Seq uniform(const Seq& s)
             __builtin_amdgcn_readfirstlane(s.pos0)};
 }
 
+// The last key that the query at position `at` sees of `len` (below 0: none; a token before
+// position 0 sees none, causal or not).
+__device__ inline int last_key(int at, int causal, int len)
+{
+    return at < 0 ? -1 : causal ? min(at, len - 1) : len - 1;
+}
+
 // Query rows of a (sequence, KV head): row R is head R % G of token R / G.
 struct Group {
     int G;

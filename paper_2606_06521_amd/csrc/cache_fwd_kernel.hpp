@@ -121,8 +121,8 @@ __global__ void __launch_bounds__(256, 1) cache_fwd_kernel(FwdParams p)
     const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int n = lane & 15, g = lane >> 4;
     const int row = row0 + n;
-    const int pos = row < rows ? (p.causal ? min(s.pos0 + p.gr.token(row), s.len - 1) : s.len - 1) : -1;   // the last key the row sees
-    const int pos_min = p.causal ? min(s.pos0 + p.gr.token(row0), s.len - 1) : s.len - 1;
+    const int pos = row < rows ? last_key(s.pos0 + p.gr.token(row), p.causal, s.len) : -1;
+    const int pos_min = last_key(s.pos0 + p.gr.token(row0), p.causal, s.len);
     const int seen = p.causal ? min(max(s.pos0 + p.gr.token(min(row0 + TR, rows) - 1) + 1, 0), s.len) : s.len;
 
     // the range's page numbers, then their scales

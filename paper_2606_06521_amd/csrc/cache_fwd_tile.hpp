@@ -61,9 +61,9 @@ __global__ void __launch_bounds__(256, 2) cache_fwd_tile_kernel(FwdParams p)
     const int n = lane & 31, h = lane >> 5;
     const int wrow0 = row0 + 32 * w;                    // the wave's first row
     const int row = wrow0 + n;
-    const int pos = row < rows ? (p.causal ? min(s.pos0 + p.gr.token(row), s.len - 1) : s.len - 1) : -1;
-    const int pos_min = p.causal ? min(s.pos0 + p.gr.token(wrow0), s.len - 1) : s.len - 1;
-    const int tile_pos_min = p.causal ? min(s.pos0 + p.gr.token(row0), s.len - 1) : s.len - 1;
+    const int pos = row < rows ? last_key(s.pos0 + p.gr.token(row), p.causal, s.len) : -1;
+    const int pos_min = last_key(s.pos0 + p.gr.token(wrow0), p.causal, s.len);
+    const int tile_pos_min = last_key(s.pos0 + p.gr.token(row0), p.causal, s.len);
     const int seen = p.causal ? min(max(s.pos0 + p.gr.token(min(row0 + TR, rows) - 1) + 1, 0), s.len) : s.len;
 
     const int np = max(v1 - v0, 0) * PPV;

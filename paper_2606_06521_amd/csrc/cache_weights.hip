@@ -38,7 +38,7 @@ __device__ inline void row_of(const WeightParams& p, const Seq& s, int hk, int R
     const int at = min(R, rows - 1), i = p.gr.token(at);
     const float x = p.lse[(int64_t)(s.first + i) * p.Hq + hk * p.gr.G + (at - i * p.gr.G)];
     lse2 = x == -INFINITY ? INFINITY : x * 1.4426950408889634f;
-    last = R >= rows ? -1 : p.causal ? min(s.pos0 + i, s.len - 1) : s.len - 1;
+    last = R >= rows ? -1 : last_key(s.pos0 + i, p.causal, s.len);
 }
 
 // Q operand of row R (past the last: any row): k-step 2 i + e of lane group g:
@@ -318,7 +318,7 @@ __global__ void __launch_bounds__(256, 2) weights_tall_kernel(WeightParams p, in
             issue_q(seg + 1, buf ^ 1);
         }
         // every row of the segment sees every key of the block
-        const bool all = SEG * (seg + 1) <= rows && (!p.causal || s.pos0 + p.gr.token(SEG * seg) >= t0 + KEYS - 1) && t0 + KEYS <= s.len;
+        const bool all = SEG * (seg + 1) <= rows && s.pos0 + p.gr.token(SEG * seg) >= (p.causal ? t0 + KEYS - 1 : 0) && t0 + KEYS <= s.len;
         auto tiles = [&](auto masked) __attribute__((always_inline)) {
 #pragma unroll
             for (int q = 0; q < NK; ++q) {

@@ -358,3 +358,36 @@ def test_scales_of_pages_behind_the_length_are_not_looked_at(A, d, max_q, byte):
         c.ks[later[later >= 0]], c.vs[later[later >= 0]] = byte, byte
     o2, l2 = call(A, c, q, "bf16", new, max_q)
     assert np.array_equal(o, o2) and np.array_equal(l, l2)
+
+
+@pytest.mark.parametrize("d,page,G", [(64, 64, 2), (128, 128, 4)])
+@pytest.mark.parametrize("lens,new,wide", [([25, 9, 300], [40, 9, 30], False), ([25, 9, 300], [40, 9, 30], True), ([2], [3], False),
+                                           ([130], [200], True), ([0, 5], [7, 7], False), ([700, 20], [12, 24], False)])
+def test_tokens_before_position_0_see_nothing(A, lens, new, wide, d, page, G):
+    """A padded batch: more new tokens than the sequence has, not causal.  The others see every key, and the
+    weights count the others alone.  wide: tiles of 128 rows."""
+    rng = np.random.default_rng(sum(lens) + d)
+    c = R.make_cache(rng, len(lens), 2, page, d, lens)
+    c.v[c.pages[0, 0], :, 1, 5] = 0x7F                   # a NaN that nobody else sees
+    q = R.make_queries(rng, sum(new), 2 * G, d)
+    max_q = tall(c, G, new)[0] if wide else max(new)
+    cu = cu_of(new)
+    log(f"before 0: {lens} {new} d={d} max_q={max_q}")
+    want, wl, bound, lb = R.attention(c, q, G, cu=cu, causal=False)
+    before = np.concatenate([np.arange(n - m, n) < 0 for n, m in zip(lens, new)])
+    want[before], bound[before], wl[before], lb[before] = 0, 0, -np.inf, 0
+    o, l = call(A, c, q, "bf16", new, max_q, causal=False)
+    hit = np.isnan(want)
+    assert np.array_equal(np.isnan(o), hit)
+    within(np.where(hit, 0, o), np.where(hit, 0, want), np.where(hit, 0, bound))
+    assert np.array_equal(np.isinf(l), np.isinf(wl))
+    fin = np.isfinite(wl)
+    if fin.any():
+        within(l[fin], wl[fin], lb[fin])
+    # weights of the visible rows; lse of the others as a caller of another library might give it
+    n_w = c.pages.shape[1] * page
+    lse = np.where(fin, wl, 0.0).astype(np.float32)
+    w = torch.zeros((len(lens), 2, n_w), device="cuda")
+    A.cache_weights(R.torch_q(q, "bf16").cuda(), dev(lse), dev_cache(A, c), dev(c.pages), dev(c.lens), w, cu=dev(cu), max_q=max_q, causal=False)
+    ww = R.weights(c, q, np.where(fin, lse, -np.inf), G, n_w, cu=cu, causal=False)
+    within(w.cpu().double().numpy(), ww, 2.0 ** -17 * ww)
