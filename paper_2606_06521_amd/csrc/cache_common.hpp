@@ -99,12 +99,11 @@ __device__ inline int page_of(const Batch& bt, int n_pages, int b, int block)
 
 // ---- E4M3 blocks ----
 
-// Least e >= -127 with amax <= 448 * 2^e (amax >= 0; past FP32's largest: as that).
+// Least e >= -127 with amax <= 448 * 2^e (amax >= 0 and finite).
 __device__ inline int block_exponent(float amax)
 {
     if (amax == 0.f)
         return -127;
-    amax = __builtin_fminf(amax, 0x1.fffffep127f);
     const int t = __builtin_amdgcn_frexp_expf(amax);
     const float f = __builtin_amdgcn_frexp_mantf(amax);   // [0.5, 1): 448 = 0.875 * 2^9
     return max(t - 9 + (f > 0.875f ? 1 : 0), -127);

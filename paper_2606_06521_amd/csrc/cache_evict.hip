@@ -246,7 +246,7 @@ __global__ void __launch_bounds__(256) evict_move(EvictParams p)
     // (all rows' loads of a step at once: the chain is paid once, not per row)
     i32x4 code[NP];
     int ex[NP], from[NP], tok[NP];
-    float amax = 0.f;
+    int e = -127;       // the block's exponent (of codes and bytes: the values may lie past FP32's largest)
 #pragma unroll
     for (int q = 0; q < NP; ++q)
         tok[q] = kept[min(q * TPP + tk, z - 1)];
@@ -274,17 +274,17 @@ __global__ void __launch_bounds__(256) evict_move(EvictParams p)
             for (int e = 0; e < 4; ++e)
                 top = fmax_f(top, __builtin_fabsf(y[e]));   // (a NaN code does not count)
         }
-        amax = fmax_f(amax, q * TPP + tk < z ? __builtin_amdgcn_ldexpf(top, ex[q]) : 0.f);
+        if (q * TPP + tk < z && top > 0.f)
+            e = max(e, block_exponent(top) + ex[q]);
     }
 #pragma unroll
     for (int off = 32; off > 0; off >>= 1)
-        amax = fmax_f(amax, __shfl_xor(amax, off, 64));
-    __shared__ float wave_max[4];
+        e = max(e, __shfl_xor(e, off, 64));
+    __shared__ int wave_max[4];
     if ((threadIdx.x & 63) == 0)
-        wave_max[threadIdx.x >> 6] = amax;
+        wave_max[threadIdx.x >> 6] = e;
     __syncthreads();
-    amax = fmax_f(fmax_f(wave_max[0], wave_max[1]), fmax_f(wave_max[2], wave_max[3]));
-    const int e = block_exponent(amax);
+    e = max(max(wave_max[0], wave_max[1]), max(wave_max[2], wave_max[3]));
     const size_t to = (size_t)pid * p.to.Hkv + hk;
     uint8_t* const dst = (is_v ? p.to.v : p.to.k) + to * (PAGE * D);
     if (threadIdx.x == 0)

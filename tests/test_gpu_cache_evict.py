@@ -74,3 +74,19 @@ def test_weights_of_one_value_and_of_all_bits(A, room):
         assert np.array_equal(kept.cpu().numpy(), wk)
         assert torch.equal(nw.cpu().view(torch.int32), torch.from_numpy(ww).view(torch.int32))
         same_cache(gt, to)
+
+
+@pytest.mark.parametrize("d,page", [(64, 64), (128, 128)])
+def test_blocks_beyond_fp32(A, d, page):
+    """Scale bytes up to 254: values up to 448 2^127, kept as codes and bytes."""
+    rng = np.random.default_rng(d)
+    c = R.make_cache(rng, 2, 2, page, d, [300, 140])
+    c.ks[:], c.vs[:] = rng.integers(236, 255, c.ks.shape), rng.choice([0, 20, 247, 248, 254], c.vs.shape)
+    w = rng.random((2, 2, c.pages.shape[1] * page)).astype(np.float32)
+    to = R.make_cache(rng, 2, 2, page, d, [128, 128])
+    gt = dev_cache(A, to)
+    log(f"evict beyond FP32 d={d} page={page}")
+    kept, _, _ = A.cache_evict(dev_cache(A, c), dev(c.pages), dev(c.lens), dev(w), gt, dev(to.pages), 128)
+    wk, _, _ = R.evict(c, w, 128, 4, 0, to, to.pages)
+    assert np.array_equal(kept.cpu().numpy(), wk)
+    same_cache(gt, to)
