@@ -466,6 +466,6 @@ def cache_evict(cache, pages, lens, weights, to, new_pages, budget, *, n_sink: i
     `cache`, then pages that hold none of these sequences): the first n_sink, the last
     n_recent, and the ones of the largest weights [B, Hkv, n] (equal ones: the earlier).
     Returns (kept [B, Hkv, budget] int32: where each was, then -1; new_lens [B] int32;
-    new_weights [B, Hkv, budget] float32: theirs, then 0)."""
+    new_weights [B, Hkv, budget] float32: theirs, then 0); given ones overlap no input."""
     return _call(stream, _binding.evict, cache, pages, lens, weights, to, new_pages, budget, n_sink, n_recent, kept,
                  new_lens, new_weights)

@@ -100,6 +100,18 @@ attn::Rotation rotation_of(const attn_fp8_rotation* r)
 
 int status(hipError_t e) { return e == hipSuccess ? ATTN_OK : ATTN_ERR_HIP; }
 
+// Elements of four bytes; none at a null address.
+struct Span {
+    const void* at;
+    __int128 n;         // (strides are the caller's: any number of 64 bits)
+};
+
+bool overlap(const Span& x, const Span& y)
+{
+    const __int128 a = (uintptr_t)x.at, b = (uintptr_t)y.at;
+    return a && b && x.n > 0 && y.n > 0 && a < b + 4 * y.n && b < a + 4 * x.n;
+}
+
 // What a raw score is multiplied by on a block scale of 1.
 float factor_of(float sm_scale, float q_descale) { return (float)(1.4426950408889634074 * (double)sm_scale * (double)q_descale); }
 
@@ -299,6 +311,22 @@ int attn_fp8_cache_evict(const attn_fp8_cache* from, const attn_fp8_batch* batch
     if (!new_pages || !weights || !kept || !new_lens || misaligned(new_pages, 4) || misaligned(weights, 4) || misaligned(kept, 4) ||
         misaligned(new_lens, 4) || misaligned(new_weights, 4) || stride_h < (int64_t)batch->W * from->page)
         return ATTN_ERR_INVALID_ARG;
+    // (workgroups read lens, pages and weights while others write; rows of weights end at W * page)
+    const int64_t heads = (int64_t)batch->B * from->Hkv, nb = (budget + from->page - 1) / from->page;
+    const Span outs[] = {{kept, heads * budget}, {new_lens, batch->B}, {new_weights, heads * budget}};
+    const Span ins[] = {{batch->lens, batch->B},
+                        {batch->pages, (int64_t)batch->B * batch->W},
+                        {new_pages, batch->B * nb},
+                        {weights, (__int128)(batch->B - 1) * stride_b + (__int128)(from->Hkv - 1) * stride_h +
+                                      (int64_t)batch->W * from->page}};
+    for (int i = 0; i < 3; ++i) {
+        for (const Span& in : ins)
+            if (overlap(outs[i], in))
+                return ATTN_ERR_INVALID_ARG;
+        for (int j = 0; j < i; ++j)
+            if (overlap(outs[i], outs[j]))
+                return ATTN_ERR_INVALID_ARG;
+    }
     attn::EvictParams p{};
     p.bt = batch_of(batch);
     p.from = cache_of(from);
@@ -310,7 +338,7 @@ int attn_fp8_cache_evict(const attn_fp8_cache* from, const attn_fp8_batch* batch
     p.budget = budget;
     p.n_sink = n_sink;
     p.n_recent = n_recent;
-    p.nb = (budget + from->page - 1) / from->page;
+    p.nb = (int)nb;
     p.kept = kept;
     p.new_lens = new_lens;
     p.new_w = new_weights;
