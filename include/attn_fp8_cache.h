@@ -149,7 +149,8 @@ int attn_fp8_cache_workspace_bytes(const attn_fp8_cache *cache, const attn_fp8_b
  * is far below 2^23); a row of lse = -inf adds nothing.
  *   weights    FP32 [B][Hkv][..], stride_b and stride_h elements apart; entries
  *              t < min(lens[b], max_len) are updated, the others left as they
- *              were.  max_len 0: W * page.  max_len <= stride_h.
+ *              were.  max_len 0: W * page.  max_len <= stride_h, and rows do not
+ *              overlap: those of a sequence side by side, or those of a head.
  */
 int attn_fp8_cache_weights(const attn_fp8_cache *cache, const attn_fp8_batch *batch,
                            const attn_fp8_heads *q, int Hq, const float *lse, int causal,

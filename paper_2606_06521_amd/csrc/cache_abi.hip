@@ -271,6 +271,10 @@ int attn_fp8_cache_weights(const attn_fp8_cache* cache, const attn_fp8_batch* ba
     if ((q->type != ATTN_TYPE_BF16 && q->type != ATTN_TYPE_E4M3) || !lse || !weights || misaligned(lse, 4) ||
         misaligned(weights, 4) || stride_h < most)
         return ATTN_ERR_INVALID_ARG;
+    // (rows are updated without atomics: sequences outermost or heads outermost, none over another)
+    const __int128 sb = stride_b, sh = stride_h;
+    if (batch->B > 1 && sb < (cache->Hkv - 1) * sh + most && (sb < most || (cache->Hkv > 1 && sh < (batch->B - 1) * sb + most)))
+        return ATTN_ERR_INVALID_ARG;
     attn::WeightParams p{};
     p.bt = batch_of(batch);
     p.cache = cache_of(cache);

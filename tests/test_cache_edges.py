@@ -1,7 +1,7 @@
 """Refusals of the cache calls at their edges, on the host (no GPU needed): nothing is launched."""
 import pytest
 
-from tests.test_cache_abi import batch, cache
+from tests.test_cache_abi import batch, cache, heads
 
 MB = 1 << 20   # addresses are never dereferenced
 
@@ -39,3 +39,22 @@ def test_evict_takes_neighbours(A):
     for kw in (dict(), dict(new_lens=2 * MB + 8), dict(new_lens=2 * MB - 8), dict(kept=4 * MB + 4 * (1024 + 512 + 512)),
                dict(kept=4 * MB - 4 * 256), dict(nw=5 * MB + 4 * 256), dict(nw=None)):
         assert evict(A, **kw) == A.ATTN_ERR_HIP, kw
+
+
+def weights(A, sb, sh, B=2, Hkv=2):
+    return A.attn_fp8_cache_weights(cache(A, Hkv=Hkv), batch(A, B=B, T=B), heads(A), 2 * Hkv, MB, 1, 0.1, 1.0, 0, 4 * MB, sb, sh, None)
+
+
+@pytest.mark.parametrize("sb,sh,B,Hkv", [(0, 512, 2, 2), (512, 512, 2, 2), (1023, 512, 2, 2), (511, 1 << 20, 2, 2), (512, 1023, 2, 2),
+                                         (512, 1024, 3, 2), (0, 512, 2, 1), (511, 512, 2, 1)])
+def test_weights_refuses_rows_that_overlap(A, sb, sh, B, Hkv):
+    """Two sequences that add to the same entries (512 of a row) would lose one another's sums."""
+    assert weights(A, sb, sh, B, Hkv) == A.ATTN_ERR_INVALID_ARG
+
+
+def test_weights_takes_either_order_of_rows(A):
+    import torch
+    if torch.cuda.is_available():
+        pytest.skip("would launch on made-up addresses")
+    for sb, sh, B, Hkv in ((1024, 512, 2, 2), (512, 1024, 2, 2), (512, 1536, 3, 2), (0, 512, 1, 2), (512, 512, 2, 1), (1 << 62, 1 << 40, 4, 2)):
+        assert weights(A, sb, sh, B, Hkv) == A.ATTN_ERR_HIP, (sb, sh, B, Hkv)
