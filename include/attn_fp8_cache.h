@@ -26,7 +26,8 @@
  *     most 2^26, else ATTN_ERR_UNSUPPORTED).  Tokens without a page are not written,
  *     and no query sees them; nor are tokens before position 0, whose queries see
  *     no key;
- *   - T is at most 2^30 (else ATTN_ERR_UNSUPPORTED);
+ *   - T is at most 2^30 and a launch (by B, max_q, the heads and bounds, not by lens and
+ *     cu) has less than 2^32 threads, else ATTN_ERR_UNSUPPORTED;
  *   - a sequence has at most max_q new tokens; those beyond are left out (not
  *     written, their rows of an output left as they were), as are cu entries
  *     outside 0 .. T.
@@ -84,7 +85,7 @@ typedef struct attn_fp8_rotation {
  * from rot on are copied.  FP32, rounded once to the type of x.
  *   x, out     [T][H][d] of one type, F32, BF16 or F16; out may be x.
  *   d          a multiple of 16, at most 1024; rot <= d.
- * T or H = 0 is a no-op.
+ * T or H = 0 is a no-op; T H d / 16 is below 2^32 (else ATTN_ERR_UNSUPPORTED).
  */
 int attn_fp8_rope(const attn_fp8_heads *x, const attn_fp8_heads *out, int T, int H, int d,
                   const attn_fp8_rotation *rotation, void *stream);

@@ -98,7 +98,8 @@ attn::Rotation rotation_of(const attn_fp8_rotation* r)
     return {r->table, r->positions, r->n_pos, r->rot, r->layout};
 }
 
-int status(hipError_t e) { return e == hipSuccess ? ATTN_OK : ATTN_ERR_HIP; }
+// (a launch that would need too large a grid was not tried)
+int status(hipError_t e) { return e == hipSuccess ? ATTN_OK : e == hipErrorNotSupported ? ATTN_ERR_UNSUPPORTED : ATTN_ERR_HIP; }
 
 // Elements of four bytes; none at a null address.
 struct Span {
@@ -127,7 +128,9 @@ int check_attention(const attn_fp8_cache* c, const attn_fp8_batch* bt, int Hq, i
         return ATTN_ERR_INVALID_ARG;
     // (the row numbers of a sequence and KV head times the group stay below 2^32)
     const int G = Hq / c->Hkv;
-    return G > 256 || (int64_t)G * bt->max_q > 1 << 24 ? ATTN_ERR_UNSUPPORTED : ATTN_OK;
+    if (G > 256 || (int64_t)G * bt->max_q > 1 << 24 || !attn::cache_fwd_fits(bt->B, c->Hkv, G, bt->max_q))
+        return ATTN_ERR_UNSUPPORTED;
+    return ATTN_OK;
 }
 
 int longest(const attn_fp8_cache* c, const attn_fp8_batch* bt, int max_len)
@@ -211,8 +214,12 @@ int attn_fp8_cache_workspace_bytes(const attn_fp8_cache* cache, const attn_fp8_b
     int n_cu = 0;
     if (device_cus(n_cu) != ATTN_OK)
         return ATTN_ERR_HIP;
-    *bytes = attn::cache_fwd_plan(batch->B, cache->Hkv, Hq / cache->Hkv, batch->max_q, longest(cache, batch, max_len), cache->d,
-                                  n_cu).bytes;
+    const int G = Hq / cache->Hkv;
+    const attn::FwdPlan pl = attn::cache_fwd_plan(batch->B, cache->Hkv, G, batch->max_q, longest(cache, batch, max_len), cache->d, n_cu);
+    attn::FwdGrids g;
+    if (attn::cache_fwd_grids(batch->B, cache->Hkv, G, batch->max_q, cache->d, pl, g) != hipSuccess)
+        return ATTN_ERR_UNSUPPORTED;
+    *bytes = pl.bytes;
     return ATTN_OK;
 }
 
@@ -317,7 +324,7 @@ int attn_fp8_cache_evict(const attn_fp8_cache* from, const attn_fp8_batch* batch
         return ATTN_ERR_INVALID_ARG;
     // (workgroups read lens, pages and weights while others write; rows of weights end at W * page)
     const int64_t heads = (int64_t)batch->B * from->Hkv, nb = (budget + from->page - 1) / from->page;
-    const Span outs[] = {{kept, heads * budget}, {new_lens, batch->B}, {new_weights, heads * budget}};
+    const Span outs[] = {{kept, (__int128)heads * budget}, {new_lens, batch->B}, {new_weights, (__int128)heads * budget}};
     const Span ins[] = {{batch->lens, batch->B},
                         {batch->pages, (int64_t)batch->B * batch->W},
                         {new_pages, batch->B * nb},

@@ -326,6 +326,15 @@ __device__ inline float far_factor(const bf16x8* q, int d)
 
 // ---- host side ----
 
+// Workgroups of a launch, or hipErrorNotSupported: the threads of one are a 32-bit number.
+// (128 bits: products of the caller's sizes)
+inline hipError_t grid_of(__int128 workgroups, int threads, unsigned& grid)
+{
+    const bool fits = workgroups * threads < (__int128)1 << 32;
+    grid = fits ? (unsigned)workgroups : 0;
+    return fits ? hipSuccess : hipErrorNotSupported;
+}
+
 struct FwdParams {
     Batch bt;
     Cache cache;
@@ -374,9 +383,19 @@ struct FwdPlan {
 };
 FwdPlan cache_fwd_plan(int B, int Hkv, int G, int max_q, int max_len, int d, int n_cu);
 
+// Whether a call can be launched at all, by the fewest workgroups of a plan; the grids of
+// one plan's launches (hipErrorNotSupported: too large).
+bool cache_fwd_fits(int B, int Hkv, int G, int max_q);
+struct FwdGrids {
+    unsigned tiles, merges;
+    int merge_rows;         // rows of a merging workgroup
+};
+hipError_t cache_fwd_grids(int B, int Hkv, int G, int max_q, int d, const FwdPlan& plan, FwdGrids& g);
+
 hipError_t launch_rope(const Heads& x, const Heads& out, int T, int H, int d, int type, const Rotation& r, hipStream_t s);
 hipError_t launch_append(const Batch& bt, const Cache& c, int d, int page, const Heads& k, const Heads& v, int type,
                          const Rotation& r, const Heads& q, const Heads& q_out, int Hq, hipStream_t s);
+// (the launches: hipErrorNotSupported if a grid is too large, before any of them)
 hipError_t launch_cache_fwd(FwdParams p, const FwdPlan& plan, int d, int page, bool e4m3, hipStream_t s);
 hipError_t launch_cache_weights(const WeightParams& p, int d, int page, bool e4m3, int n_cu, hipStream_t s);
 hipError_t launch_cache_evict(const EvictParams& p, int d, int page, hipStream_t s);

@@ -314,11 +314,15 @@ __global__ void __launch_bounds__(256) evict_move(EvictParams p)
 
 hipError_t launch_cache_evict(const EvictParams& p, int d, int page, hipStream_t s)
 {
-    const int64_t heads = (int64_t)p.bt.B * p.from.Hkv, moves = heads * p.nb * 2;
-    if (moves > 1 << 30)
-        return hipErrorInvalidValue;
+    const int64_t heads = (int64_t)p.bt.B * p.from.Hkv;
+    unsigned picks, moves;
+    hipError_t e = grid_of(heads, kPick, picks);
+    if (e == hipSuccess)
+        e = grid_of((__int128)heads * p.nb * 2, 256, moves);
+    if (e != hipSuccess)
+        return e;
     const int most = p.bt.W * page;
-    auto pick = [&](auto kern) { hipLaunchKernelGGL(kern, dim3((unsigned)heads), dim3(kPick), 0, s, p, most); };
+    auto pick = [&](auto kern) { hipLaunchKernelGGL(kern, dim3(picks), dim3(kPick), 0, s, p, most); };
     if (most <= 4 * kPick)
         pick(evict_pick<4>);
     else if (most <= 8 * kPick)
@@ -327,11 +331,11 @@ hipError_t launch_cache_evict(const EvictParams& p, int d, int page, hipStream_t
         pick(evict_pick<16>);
     else
         pick(evict_pick<0>);
-    hipError_t e = hipGetLastError();
+    e = hipGetLastError();
     if (e != hipSuccess)
         return e;
     auto go = [&](auto kern) {
-        hipLaunchKernelGGL(kern, dim3((unsigned)moves), dim3(256), 0, s, p);
+        hipLaunchKernelGGL(kern, dim3(moves), dim3(256), 0, s, p);
         return hipGetLastError();
     };
     if (d == 64)

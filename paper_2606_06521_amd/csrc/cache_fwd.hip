@@ -93,10 +93,10 @@ __global__ void __launch_bounds__(256) cache_merge(FwdParams p, int tile_rows)
 }
 
 template <int D, int PAGE>
-hipError_t fwd_go(const FwdParams& p, int rows, bool e4m3, int64_t grid, hipStream_t s)
+hipError_t fwd_go(const FwdParams& p, int rows, bool e4m3, unsigned grid, hipStream_t s)
 {
     auto go = [&](auto kern) {
-        hipLaunchKernelGGL(kern, dim3((unsigned)grid), dim3(256), 0, s, p);
+        hipLaunchKernelGGL(kern, dim3(grid), dim3(256), 0, s, p);
         return hipGetLastError();
     };
     if (rows == kTileRows)
@@ -141,27 +141,42 @@ FwdPlan cache_fwd_plan(int B, int Hkv, int G, int max_q, int max_len, int d, int
     return run > 16 && plan_time(tall, kTileRows, heads, run, visits, d, n_cu) < t_low ? tall : low;
 }
 
+bool cache_fwd_fits(int B, int Hkv, int G, int max_q)
+{
+    unsigned grid;
+    return grid_of((__int128)B * Hkv * (((int64_t)max_q * G + kTileRows - 1) / kTileRows), 256, grid) == hipSuccess;
+}
+
+hipError_t cache_fwd_grids(int B, int Hkv, int G, int max_q, int d, const FwdPlan& pl, FwdGrids& g)
+{
+    const int64_t heads = (int64_t)B * Hkv;
+    // whole rounds of the XCDs
+    const hipError_t e = grid_of(((__int128)heads * pl.tiles * pl.ranges + kNumXcd - 1) / kNumXcd * kNumXcd, 256, g.tiles);
+    // rows of a merging workgroup: one, or as many as have a thread per 16 bytes
+    g.merge_rows = pl.ranges > 8 ? 1 : 1024 / d;
+    g.merges = 0;
+    return e != hipSuccess || pl.ranges == 1
+               ? e
+               : grid_of((__int128)heads * (((int64_t)max_q * G + g.merge_rows - 1) / g.merge_rows), 256, g.merges);
+}
+
 hipError_t launch_cache_fwd(FwdParams p, const FwdPlan& pl, int d, int page, bool e4m3, hipStream_t s)
 {
     p.tiles = pl.tiles;
     p.chunk = pl.chunk;
     p.ranges = pl.ranges;
-    const int64_t units = (int64_t)p.bt.B * p.cache.Hkv * pl.tiles;
-    // (whole rounds of the XCDs)
-    const int64_t grid = (units * pl.ranges + kNumXcd - 1) / kNumXcd * kNumXcd;
-    // rows of a merging workgroup: one, or as many as have a thread per 16 bytes
-    const int rpw = pl.ranges > 8 ? 1 : 1024 / d;
-    const int64_t merges = (int64_t)p.bt.B * p.cache.Hkv * (((int64_t)p.bt.max_q * p.gr.G + rpw - 1) / rpw);
-    if (grid > 1 << 30 || merges > 1 << 30)
-        return hipErrorInvalidValue;
-    hipError_t e = d == 64 ? (page == 64 ? fwd_go<64, 64>(p, pl.rows, e4m3, grid, s) : fwd_go<64, 128>(p, pl.rows, e4m3, grid, s))
-                           : (page == 64 ? fwd_go<128, 64>(p, pl.rows, e4m3, grid, s) : fwd_go<128, 128>(p, pl.rows, e4m3, grid, s));
+    FwdGrids g;
+    hipError_t e = cache_fwd_grids(p.bt.B, p.cache.Hkv, p.gr.G, p.bt.max_q, d, pl, g);
+    if (e != hipSuccess)
+        return e;
+    e = d == 64 ? (page == 64 ? fwd_go<64, 64>(p, pl.rows, e4m3, g.tiles, s) : fwd_go<64, 128>(p, pl.rows, e4m3, g.tiles, s))
+                : (page == 64 ? fwd_go<128, 64>(p, pl.rows, e4m3, g.tiles, s) : fwd_go<128, 128>(p, pl.rows, e4m3, g.tiles, s));
     if (e == hipSuccess && pl.ranges > 1) {
-        auto merge = [&](auto kern) { hipLaunchKernelGGL(kern, dim3((unsigned)merges), dim3(256), 0, s, p, pl.rows); };
+        auto merge = [&](auto kern) { hipLaunchKernelGGL(kern, dim3(g.merges), dim3(256), 0, s, p, pl.rows); };
         if (d == 64)
-            rpw == 1 ? merge(cache_merge<64, 16>) : merge(cache_merge<64, 1>);
+            g.merge_rows == 1 ? merge(cache_merge<64, 16>) : merge(cache_merge<64, 1>);
         else
-            rpw == 1 ? merge(cache_merge<128, 8>) : merge(cache_merge<128, 1>);
+            g.merge_rows == 1 ? merge(cache_merge<128, 8>) : merge(cache_merge<128, 1>);
         e = hipGetLastError();
     }
     return e;

@@ -238,11 +238,14 @@ __global__ void __launch_bounds__(256) append_kernel(Batch bt, Cache cache, Head
 hipError_t launch_rope(const Heads& x, const Heads& out, int T, int H, int d, int type, const Rotation& r, hipStream_t s)
 {
     const int upt = d / 16;
-    const int64_t n = (int64_t)T * H * upt, grid = (n + 255) / 256;
-    if (grid > 1 << 30)
-        return hipErrorInvalidValue;
+    unsigned grid;
+    const __int128 units = (__int128)T * H * upt;
+    const hipError_t e = grid_of((units + 255) / 256, 256, grid);
+    if (e != hipSuccess)
+        return e;
+    const int64_t n = (int64_t)units;
     auto go = [&](auto kern) {
-        hipLaunchKernelGGL(kern, dim3((unsigned)grid), dim3(256), 0, s, x, out, n, H, upt, r);
+        hipLaunchKernelGGL(kern, dim3(grid), dim3(256), 0, s, x, out, n, H, upt, r);
         return hipGetLastError();
     };
     return type == kTypeF32 ? go(rope_kernel<kTypeF32>) : type == kTypeBf16 ? go(rope_kernel<kTypeBf16>) : go(rope_kernel<kTypeF16>);
@@ -253,13 +256,15 @@ hipError_t launch_append(const Batch& bt, const Cache& c, int d, int page, const
 {
     // blocks that max_q tokens can lie in
     const int most = (int)(((int64_t)bt.max_q + page - 2) / page + 1);
-    const int64_t blocks = (int64_t)bt.B * most * c.Hkv * 2;
+    const __int128 writes = (__int128)bt.B * most * c.Hkv * 2;
     const int64_t q_groups = q.data ? ((int64_t)bt.max_q * Hq * (d / 16) + 255) / 256 : 0;   // of a sequence
-    const int64_t grid = blocks + bt.B * q_groups;
-    if (grid > 1 << 30)
-        return hipErrorInvalidValue;
+    unsigned grid;
+    const hipError_t e = grid_of(writes + (__int128)bt.B * q_groups, 256, grid);
+    if (e != hipSuccess)
+        return e;
+    const int64_t blocks = (int64_t)writes;
     auto go = [&](auto kern) {
-        hipLaunchKernelGGL(kern, dim3((unsigned)grid), dim3(256), 0, s, bt, c, k, v, r, q, q_out, Hq, most, blocks, q_groups);
+        hipLaunchKernelGGL(kern, dim3(grid), dim3(256), 0, s, bt, c, k, v, r, q, q_out, Hq, most, blocks, q_groups);
         return hipGetLastError();
     };
     auto by_type = [&](auto ty) {

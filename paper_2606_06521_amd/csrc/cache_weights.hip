@@ -403,21 +403,22 @@ hipError_t launch_cache_weights(const WeightParams& p, int d, int page, bool e4m
     // 336 blocks: 82 and 83; 8 x 8 x 1024, 64 x 4 rows, 512 blocks: 12 and 16)
     const int keys = heads * visits < n_cu ? 32 : 128;
     const int blocks = (p.max_len + keys - 1) / keys;
-    const int64_t grid = heads * (tall ? blocks : ranges);
-    if (grid > 1 << 30)
-        return hipErrorInvalidValue;
+    unsigned grid;
+    const hipError_t e = grid_of((__int128)heads * (tall ? blocks : ranges), tall ? 256 : 512, grid);
+    if (e != hipSuccess)
+        return e;
     auto by_type = [&](auto dc, auto pc, auto ec) {
         constexpr int D = decltype(dc)::value, PAGE = decltype(pc)::value;
         constexpr bool E = decltype(ec)::value;
-        auto tall_of = [&](auto kern) { hipLaunchKernelGGL(kern, dim3((unsigned)grid), dim3(256), 0, s, p, blocks); };
+        auto tall_of = [&](auto kern) { hipLaunchKernelGGL(kern, dim3(grid), dim3(256), 0, s, p, blocks); };
         if (tall && keys == 128)
             tall_of(weights_tall_kernel<D, PAGE, E, 128>);
         else if (tall)
             tall_of(weights_tall_kernel<D, PAGE, E, 32>);
         else if (rows <= 16)
-            hipLaunchKernelGGL((weights_stream_kernel<D, PAGE, E, 1>), dim3((unsigned)grid), dim3(512), 0, s, p, chunk, ranges);
+            hipLaunchKernelGGL((weights_stream_kernel<D, PAGE, E, 1>), dim3(grid), dim3(512), 0, s, p, chunk, ranges);
         else
-            hipLaunchKernelGGL((weights_stream_kernel<D, PAGE, E, kStreamRows / 16>), dim3((unsigned)grid), dim3(512), 0, s, p, chunk,
+            hipLaunchKernelGGL((weights_stream_kernel<D, PAGE, E, kStreamRows / 16>), dim3(grid), dim3(512), 0, s, p, chunk,
                                ranges);
         return hipGetLastError();
     };

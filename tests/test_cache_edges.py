@@ -1,7 +1,10 @@
 """Refusals of the cache calls at their edges, on the host (no GPU needed): nothing is launched."""
+import ctypes
+
 import pytest
 
-from tests.test_cache_abi import batch, cache, heads
+from tests.cache_plan import fwd_plan
+from tests.test_cache_abi import batch, cache, heads, rotation
 
 MB = 1 << 20   # addresses are never dereferenced
 
@@ -58,3 +61,64 @@ def test_weights_takes_either_order_of_rows(A):
         pytest.skip("would launch on made-up addresses")
     for sb, sh, B, Hkv in ((1024, 512, 2, 2), (512, 1024, 2, 2), (512, 1536, 3, 2), (0, 512, 1, 2), (512, 512, 2, 1), (1 << 62, 1 << 40, 4, 2)):
         assert weights(A, sb, sh, B, Hkv) == A.ATTN_ERR_HIP, (sb, sh, B, Hkv)
+
+
+GB = 1 << 36
+
+
+def test_rope_of_too_many_threads_is_unsupported(A):
+    """16 channels a thread; a launch holds less than 2^32 threads."""
+    r = rotation(A)
+    big = lambda T, H, d: A.attn_fp8_rope(heads(A), heads(A), T, H, d, r, None)  # noqa: E731
+    for T, H, d in ((1 << 26, 64, 1024), (1 << 30, 32, 128), ((1 << 31) - 1, (1 << 31) - 16, 1024), (1 << 23, 128, 64)):
+        assert big(T, H, d) == A.ATTN_ERR_UNSUPPORTED, (T, H, d)
+
+
+@pytest.mark.parametrize("B,max_q,Hkv,Hq", [((1 << 31) - 1, 1 << 26, 1 << 16, 1 << 16), (1 << 12, 1 << 20, 8, 8), (1 << 18, 1, 32, 32),
+                                            (1 << 16, 1 << 16, 1, 1 << 8)])
+def test_append_of_too_many_threads_is_unsupported(A, B, max_q, Hkv, Hq):
+    """A workgroup per block that can get tokens, KV head, and K or V, and those of q: products that pass
+    64 bits in the first case."""
+    b, x = batch(A, B=B, max_q=max_q, cu=MB, T=64), heads(A)
+    q = x if Hq != Hkv else None
+    assert A.attn_fp8_cache_append(cache(A, Hkv=Hkv), b, x, x, rotation(A), q, q, Hq, None) == A.ATTN_ERR_UNSUPPORTED
+
+
+@pytest.mark.parametrize("B,max_q,Hkv,G", [((1 << 31) - 1, 1 << 24, 1 << 16, 1), (1 << 20, 1, 16, 4), (64, 1 << 22, 64, 4)])
+def test_attention_of_too_many_threads_is_unsupported(A, B, max_q, Hkv, G):
+    c, b, x = cache(A, Hkv=Hkv), batch(A, B=B, max_q=max_q, cu=MB, T=64), heads(A)
+    assert A.attn_fp8_cache_fwd(c, b, x, Hkv * G, MB, 1, MB, 1, 0.1, 1.0, 0, None, 0, None) == A.ATTN_ERR_UNSUPPORTED
+    assert A.attn_fp8_cache_workspace_bytes(c, b, Hkv * G, 0) == (A.ATTN_ERR_UNSUPPORTED, 0)
+    assert A.attn_fp8_cache_weights(c, b, x, Hkv * G, MB, 1, 0.1, 1.0, 0, 4 * MB, 1 << 40, 1 << 20, None) == A.ATTN_ERR_UNSUPPORTED
+
+
+def test_grids_of_a_plan(A):
+    """The tiles' and the merge's launches: whole rounds of 8 workgroups, a row or a thread per 16 bytes."""
+    class Grids(ctypes.Structure):
+        _fields_ = [("tiles", ctypes.c_uint), ("merges", ctypes.c_uint), ("merge_rows", ctypes.c_int)]
+
+    f = ctypes.CDLL(A.LIB_PATH)["_ZN4attn15cache_fwd_gridsEiiiiiRKNS_7FwdPlanERNS_8FwdGridsE"]
+    f.restype = ctypes.c_int
+
+    def grids(B, Hkv, G, max_q, n, d):
+        p, g = fwd_plan(B, Hkv, G, max_q, n, d), Grids()
+        return p, f(B, Hkv, G, max_q, d, ctypes.byref(p), ctypes.byref(g)), g
+
+    for B, Hkv, G, max_q, n, d in ((1, 2, 4, 1, 777, 64), (3, 2, 5, 1, 16500, 128), (2, 2, 4, 400, 2000, 128), (1, 8, 4, 2048, 16384, 128)):
+        p, st, g = grids(B, Hkv, G, max_q, n, d)
+        wgs = B * Hkv * p.tiles * p.ranges
+        rows = 1 if p.ranges > 8 else 1024 // d
+        assert st == 0 and g.tiles == -(-wgs // 8) * 8 and g.merge_rows == rows
+        assert g.merges == (0 if p.ranges == 1 else B * Hkv * -(-max_q * G // rows))
+    # 2^24 tiles; 2^25 rows to merge one by one
+    for a in ((1 << 18, 64, 1, 1, 128, 128), (64, 64, 4, 2048, 1 << 23, 128)):
+        p, st, _ = grids(*a)
+        assert st != 0, (a, p.rows, p.ranges)
+
+
+def test_evict_of_too_many_threads_is_unsupported(A):
+    def big(B, Hkv, budget):
+        c, b = cache(A, Hkv=Hkv), batch(A, B=B, pages=GB, lens=2 * GB)
+        return A.attn_fp8_cache_evict(c, b, c, 3 * GB, 4 * GB, 512, 512, budget, 4, 0, 1 << 61, 6 * GB, None, None)
+    for a in ((1 << 21, 2, 64), (1 << 10, 1 << 10, 1 << 14), (1 << 25, 1 << 7, 64)):
+        assert big(*a) == A.ATTN_ERR_UNSUPPORTED, a
