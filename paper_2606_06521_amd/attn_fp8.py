@@ -5,7 +5,8 @@ The C entry points are exposed under their C names; ``fwd`` and
 check their dtypes and shapes, allocate outputs with torch and pass the
 current torch stream; ``rope``, ``cache_append``, ``cache_fwd``, ``cache_weights``
 and ``cache_evict`` do the same for the KV cache, through a native module.  Every step of the computation
-runs in the HIP kernels; there is no fallback.  If the shared library is missing the import fails.
+runs in the HIP kernels; there is no fallback.  If the shared library is missing the import fails,
+if the native module is, the cache calls do.
 """
 from __future__ import annotations
 
@@ -37,7 +38,24 @@ if not os.path.exists(LIB_PATH):
     raise ImportError(f"{LIB_PATH} is not built; run __graft_entry__.build() "
                       "(hipcc --offload-arch=gfx950)")
 _lib = ctypes.CDLL(LIB_PATH)
-from . import _cache_binding as _binding  # noqa: E402  (its symbols are the library's)
+
+
+class _NoBinding:
+    """In the place of the native module where it cannot be loaded: every cache call raises;
+    the other calls do not need it."""
+
+    def __init__(self, why):
+        self._why = why
+
+    def __getattr__(self, name):
+        raise ImportError(f"the cache calls need _cache_binding.so ({self._why}); run "
+                          "__graft_entry__.build() (g++, with this torch)") from self._why
+
+
+try:
+    from . import _cache_binding as _binding  # its symbols are the library's
+except ImportError as e:
+    _binding = _NoBinding(e)
 
 _P, _I, _F, _Z = ctypes.c_void_p, ctypes.c_int, ctypes.c_float, ctypes.c_size_t
 _lib.attn_fp8_fwd.argtypes = [_P, _P, _P, _P, _P] + [_I] * 8 + [_F, _I, _P]

@@ -1,5 +1,9 @@
 """Refusals of the cache calls at their edges, on the host (no GPU needed): nothing is launched."""
 import ctypes
+import os
+import shutil
+import subprocess
+import sys
 
 import pytest
 
@@ -122,3 +126,38 @@ def test_evict_of_too_many_threads_is_unsupported(A):
         return A.attn_fp8_cache_evict(c, b, c, 3 * GB, 4 * GB, 512, 512, budget, 4, 0, 1 << 61, 6 * GB, None, None)
     for a in ((1 << 21, 2, 64), (1 << 10, 1 << 10, 1 << 14), (1 << 25, 1 << 7, 64)):
         assert big(*a) == A.ATTN_ERR_UNSUPPORTED, a
+
+
+@pytest.mark.parametrize("broken", [False, True])
+def test_the_other_calls_do_not_need_the_native_module(A, tmp_path, broken):
+    """Without _cache_binding.so (or with one that does not load) the package is there, and the cache calls
+    say what to do."""
+    package = tmp_path / "paper_2606_06521_amd"
+    package.mkdir()
+    here = os.path.dirname(A.__file__)
+    for name in ("__init__.py", "attn_fp8.py"):
+        shutil.copy(os.path.join(here, name), package / name)
+    os.symlink(A.LIB_PATH, package / os.path.basename(A.LIB_PATH))
+    if broken:
+        (package / "_cache_binding.so").write_bytes(b"not a library")
+    code = """
+import torch
+from paper_2606_06521_amd import attn_fp8 as A
+assert A.__file__.startswith({0!r}), A.__file__
+assert A.attn_fp8_version() > 0 and A.kv_cache(1, 1, 64, device="cpu").k.shape == (1, 1, 128, 64)
+x = torch.zeros((1, 1, 64))
+for call in (lambda: A.rope(x, x, x), lambda: A.cache_fwd(x, None, x, x), lambda: A.cache_append(None, x, x, x, x)):
+    try:
+        call()
+    except ImportError as e:
+        assert "__graft_entry__.build()" in str(e) and "_cache_binding" in str(e), e
+    else:
+        raise SystemExit("no error")
+try:
+    A.fwd(x, x, x)
+except ValueError:
+    print("fine")
+""".format(str(tmp_path))
+    r = subprocess.run([sys.executable, "-c", code], cwd=tmp_path, capture_output=True, text=True, timeout=120,
+                       env={**os.environ, "PYTHONPATH": str(tmp_path)})
+    assert r.stdout == "fine\n", r.stderr
