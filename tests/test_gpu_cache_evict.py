@@ -90,3 +90,40 @@ def test_blocks_beyond_fp32(A, d, page):
     wk, _, _ = R.evict(c, w, 128, 4, 0, to, to.pages)
     assert np.array_equal(kept.cpu().numpy(), wk)
     same_cache(gt, to)
+
+
+@pytest.mark.parametrize("room", [700, 5000, 20000])
+def test_captured_eviction_and_rotation_follow_their_inputs(A, room):
+    """An eviction and a rotation captured once and replayed while lengths, weights and positions change,
+    beside eager work, equal eager calls."""
+    rng = np.random.default_rng(room)
+    page, budget, lens0 = 64, 300, [room, room // 3]
+    c = R.make_cache(rng, 2, 2, page, 64, lens0)
+    spare = R.make_cache(rng, 2, 2, page, 64, [-(-budget // page) * page] * 2)
+    gc, pages, new_pages = dev_cache(A, c), dev(c.pages), dev(spare.pages)
+    table = A.rope_table(500, 64)
+    x = torch.randn((9, 3, 64), device="cuda").bfloat16()
+    steps = [(np.array(n, np.int32), hard_weights(rng, (2, 2, c.pages.shape[1] * page)), rng.integers(0, 500, 9).astype(np.int32))
+             for n in (lens0, [room - 1, 5], [299, 300], [0, 301])]
+    lens, w, pos, to = dev(steps[0][0]), dev(steps[0][1]), dev(steps[0][2]), dev_cache(A, spare)
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        got = A.cache_evict(gc, pages, lens, w, to, new_pages, budget, n_recent=20)
+        turned = A.rope(x, table, pos)
+    for i, (n, wi, p) in enumerate(steps):
+        log(f"replay {i} of {room}")
+        lens.copy_(dev(n))
+        w.copy_(dev(wi))
+        pos.copy_(dev(p))
+        before = [t.clone() for t in to]
+        graph.replay()
+        eager_to = A.KVCache(*before)
+        want = A.cache_evict(gc, pages, lens, w, eager_to, new_pages, budget, n_recent=20)
+        want_x = A.rope(x, table, pos)
+        torch.cuda.synchronize()
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+        assert torch.equal(got[2].view(torch.int32), want[2].view(torch.int32))
+        assert all(torch.equal(a.view(torch.uint8), b.view(torch.uint8)) for a, b in zip(to, eager_to))
+        assert torch.equal(turned, want_x)
+        assert got[1].tolist() == [min(int(v), budget) for v in n]

@@ -391,3 +391,32 @@ def test_tokens_before_position_0_see_nothing(A, lens, new, wide, d, page, G):
     A.cache_weights(R.torch_q(q, "bf16").cuda(), dev(lse), dev_cache(A, c), dev(c.pages), dev(c.lens), w, cu=dev(cu), max_q=max_q, causal=False)
     ww = R.weights(c, q, np.where(fin, lse, -np.inf), G, n_w, cu=cu, causal=False)
     within(w.cpu().double().numpy(), ww, 2.0 ** -17 * ww)
+
+
+@pytest.mark.parametrize("d,page,G,lens,new,max_q,first,rows", [
+    (64, 64, 2, [60, 300], [20, 3], 8, 0, 16), (128, 128, 4, [200, 9, 70], [60, 9, 1], 5, 3, 16),
+    (64, 128, 8, [1000, 40], [900, 40], 700, 5, 128), (128, 64, 8, [900, 3], [450, 1], 400, 0, 128)])
+def test_tokens_beyond_max_q_are_left_out(A, d, page, G, lens, new, max_q, first, rows):
+    """More new tokens than max_q says: the first max_q are done at their places, the rows of the others stay
+    as they were, and so do rows before the first sequence's."""
+    rng = np.random.default_rng(d + max_q)
+    c = R.make_cache(rng, len(lens), 2, page, d, lens)
+    n = c.pages.shape[1] * page
+    assert fwd_plan(len(lens), 2, G, max_q, n, d, n_cu()).rows == rows
+    q = R.make_queries(rng, first + sum(new) + 1, 2 * G, d)
+    cu = (cu_of(new) + first).astype(np.int32)
+    log(f"beyond max_q d={d} {lens} {new} max_q={max_q}")
+    out = torch.full(q.shape, 7.0, device="cuda")
+    lse = torch.full(q.shape[:2], 7.0, device="cuda")
+    gq, gc, pages, glens = R.torch_q(q, "bf16").cuda(), dev_cache(A, c), dev(c.pages), dev(c.lens)
+    A.cache_fwd(gq, gc, pages, glens, cu=dev(cu), max_q=max_q, out=out, lse=lse)
+    want, wl, bound, lb = R.attention(c, q, G, cu=cu, max_q=max_q)
+    o, l = out.cpu().double().numpy(), lse.cpu().double().numpy()
+    left = np.isnan(bound)
+    assert left.any() and np.all(o[left] == 7.0) and np.all(l[np.isnan(lb)] == 7.0)
+    within(o[~left], want[~left], bound[~left])
+    within(l[~np.isnan(lb)], wl[~np.isnan(lb)], lb[~np.isnan(lb)])
+    w = torch.zeros((len(lens), 2, n), device="cuda")
+    A.cache_weights(gq, lse, gc, pages, glens, w, cu=dev(cu), max_q=max_q)
+    ww = R.weights(c, q, l.astype(np.float32), G, n, cu=cu, max_q=max_q)
+    within(w.cpu().double().numpy(), ww, 2.0 ** -17 * ww)
