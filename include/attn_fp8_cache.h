@@ -10,7 +10,7 @@
  * The cache.  A page holds `page` = 64 or 128 tokens of all KV heads:
  *   k, v             [n_pages][Hkv][page][d]  E4M3 bytes, d = 64 or 128
  *   k_scale, v_scale [n_pages][Hkv]           E8M0 bytes: a code stands for
- *                                             code * 2^(byte - 127)
+ *                                             code * 2^(byte - 127), byte <= 254
  * The byte of a block (one page of one head) is the least for which no value of
  * the block exceeds 448 * 2^(byte - 127), and at least 0; powers of two keep
  * every rescaling exact and are what the matrix cores' block scales take.
@@ -95,8 +95,9 @@ int attn_fp8_rope(const attn_fp8_heads *x, const attn_fp8_heads *out, int T, int
  * rounded once to E4M3), v as it is.  A block that gets its first tokens takes
  * the scale they need; in a block that holds older ones the scale only grows,
  * and the older codes are rounded to the grown scale.  Values that are not
- * finite become NaN codes and do not count towards the scale.  Pages that are
- * written belong to one sequence alone.
+ * finite become NaN codes and do not count towards the scale; a rotated value past
+ * FP32's largest is one of them, one below 2^-126 is rounded to FP32's subnormals
+ * first.  Pages that are written belong to one sequence alone.
  *   k, v       [T][Hkv][d] of one type, F32, BF16 or F16.
  *   rotation   NULL: none.
  *   q, q_out   optional (both or neither): [T][Hq][d] of k's type, rotated like
@@ -118,9 +119,15 @@ int attn_fp8_cache_append(const attn_fp8_cache *cache, const attn_fp8_batch *bat
  * so no group underflows for another's maximum and neither the codes nor their
  * scales depend on the order in which the groups are visited:
  *   out = sum_g 2^(M_g - 8) sum_t code_t v_t / l,  l = sum_t 2^(x_t) before the cast,
- * sums in FP32 relative to a power of two per row; lse = ln l.  A query that
- * sees no key gets out = 0 and lse = -inf.
- *   q          [T][Hq][d], BF16 or E4M3; Hq / Hkv at most 256, times max_q at most 2^24
+ * sums in FP32 relative to a power of two per row (which may lie 2^16 below its
+ * largest: sums of values beyond 2^111 / lens[b] may pass FP32's range); lse = ln l.
+ * A query that sees no key gets out = 0 and lse = -inf.  The matrix cores add the
+ * products of P V in eights and drop what lies 13 bits below the largest of them: 6e-5
+ * of the result (relative norm), below a BF16 out's rounding, visible in an F32 one.
+ * The rounding of P itself is 1.7e-2 (777 keys) to 3.7e-2 (131001) of the softmax
+ * over the same codes.
+ *   q          [T][Hq][d], BF16 or E4M3 (F32 and F16 queries are the caller's to
+ *              round); Hq / Hkv at most 256, times max_q at most 2^24
  *              (beyond: ATTN_ERR_UNSUPPORTED).
  *   out        contiguous [T][Hq][d], BF16 or F32 by out_type, 16-byte aligned.
  *   lse        FP32 [T][Hq], or NULL.
@@ -165,7 +172,8 @@ int attn_fp8_cache_weights(const attn_fp8_cache *cache, const attn_fp8_batch *ba
  * to the lower token, NaN counts as the lowest.  Sequences of at most budget
  * tokens move whole.  The moved block's scale is that of its own values.
  *   from, batch    the cache, of at least one page; of batch pages, lens, B and W
- *                  are used.
+ *                  are used (T, max_q and cu are not, but have to be valid: T >= 0,
+ *                  max_q >= 1).
  *   to, new_pages  the cache that takes them (it may be the same arrays) and
  *                  int32 [B][ceil(budget / page)]: pages that hold none of the
  *                  batch's tokens.  Its slots that get no token are left alone.

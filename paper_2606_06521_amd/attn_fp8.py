@@ -449,7 +449,9 @@ def cache_append(cache, k, v, pages, lens, *, cu=None, max_q=None, table=None, p
     (with a table), both rounded to E4M3 on the scale of their block.  pages int32
     [B, W], lens int32 [B] (the new tokens included), cu int32 [B + 1] with max_q (None:
     T / B tokens each).  positions None: the tokens' places in their sequences.  With
-    q [T, Hq, d] its rotation is done in the same launch and returned."""
+    q [T, Hq, d] its rotation is done in the same launch and returned, in q's type: cache_fwd
+    takes bfloat16 (or float8_e4m3fn), so float32 and float16 ones are converted between.
+    Rows of the returned q that belong to no sequence's first max_q tokens are left unset."""
     return _call(stream, _binding.append, cache, k, v, pages, lens, cu, max_q, table, positions, LAYOUTS[layout], q,
                  q_out)
 
@@ -463,7 +465,9 @@ def cache_fwd(q, cache, pages, lens, *, cu=None, max_q=None, causal: bool = True
     at position lens[b] - n + i and sees the keys up to it (causal=False: all); before
     position 0, as the front of a padded batch, it sees none and gets out = 0, lse = -inf.
     pages, lens, cu, max_q as for cache_append.  sm_scale None: 1 / sqrt(d).
-    max_len: no sequence is longer (0: as long as pages allows)."""
+    max_len: no sequence is longer (0: as long as pages allows).  Rows that belong to no
+    sequence's first max_q tokens (behind cu[B], say) are not written: in outputs that the
+    call allocates they hold anything."""
     return _call(stream, _binding.fwd, q, cache, pages, lens, cu, max_q, causal, sm_scale, q_descale, max_len, out,
                  _OUT_TYPES[out_dtype], lse, want_lse)
 

@@ -12,9 +12,9 @@
 //
 // What bounds it is vector work: per key and row an exp2 (half of the rate), an FMA,
 // an add, half a maximum and half a convert, and the widening of K's codes to bf16,
-// which 32 rows share: 66 % of the time, beside 38 % of the matrix cores'.  8 heads x 2048 x 4
-// rows against 16384 keys, d = 128: 406 us, 1.27 PFLOP/s (2 % more or less from card to card); a large
-// bf16 product reaches 1.40.
+// which 32 rows share: 74 % of the cycles, beside 42 % of the matrix cores' (counted in a
+// run of 448 us).  8 heads x 2048 x 4 rows against 16384 keys, d = 128: 408 us, 1.26 PFLOP/s
+// (2 % more or less from card to card); a large bf16 product reaches 1.40.
 #pragma once
 
 #include "cache_fwd_kernel.hpp"

@@ -16,8 +16,8 @@
 // workgroup takes 128 keys, widens them to bf16 registers once (64 keys a wave) and runs over
 // the rows 64 at a time, the next 64 on their way into the other of two LDS stages,
 // each wave two 16-row tiles of them; what bounds that is the vector work of every
-// (row, key), at three waves a SIMD (37 % busy): 2 x 8 heads x 8192 keys x 1024 rows,
-// ragged, 43 us.  Where blocks of 128 keys do not fill the GPU they are of 32 keys, and
+// (row, key), at three waves a SIMD (39 % busy): 2 x 8 heads x 8192 keys x 1024 rows,
+// ragged, 42 us.  Where blocks of 128 keys do not fill the GPU they are of 32 keys, and
 // the waves share out the rows instead.
 #include "cache_common.hpp"
 
