@@ -183,7 +183,8 @@ int attn_fp8_cache_weights(const attn_fp8_cache *cache, const attn_fp8_batch *ba
  *   new_lens       int32 [B]: min(lens[b], budget).
  *   new_weights    FP32 [B][Hkv][budget]: the moved tokens' weights, then 0; or NULL.
  * kept, new_lens and new_weights overlap neither each other nor lens, pages,
- * new_pages or weights, else ATTN_ERR_INVALID_ARG.
+ * new_pages or weights (from its first row to the end of its last), else
+ * ATTN_ERR_INVALID_ARG.
  */
 int attn_fp8_cache_evict(const attn_fp8_cache *from, const attn_fp8_batch *batch,
                          const attn_fp8_cache *to, const int32_t *new_pages,

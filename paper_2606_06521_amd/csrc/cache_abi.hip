@@ -128,7 +128,8 @@ int check_attention(const attn_fp8_cache* c, const attn_fp8_batch* bt, int Hq, i
         return ATTN_ERR_INVALID_ARG;
     // (the row numbers of a sequence and KV head times the group stay below 2^32)
     const int G = Hq / c->Hkv;
-    if (G > 256 || (int64_t)G * bt->max_q > 1 << 24 || !attn::cache_fwd_fits(bt->B, c->Hkv, G, bt->max_q))
+    unsigned heads;
+    if (G > 256 || (int64_t)G * bt->max_q > 1 << 24 || attn::grid_of((__int128)bt->B * c->Hkv, 256, heads) != hipSuccess)
         return ATTN_ERR_UNSUPPORTED;
     return ATTN_OK;
 }
@@ -211,6 +212,8 @@ int attn_fp8_cache_workspace_bytes(const attn_fp8_cache* cache, const attn_fp8_b
     const int st = check_attention(cache, batch, Hq, 1, 1.f, 1.f, max_len);
     if (st != ATTN_OK || batch->B == 0 || batch->T == 0)
         return st;
+    if (!attn::cache_fwd_fits(batch->B, cache->Hkv, Hq / cache->Hkv, batch->max_q))
+        return ATTN_ERR_UNSUPPORTED;
     int n_cu = 0;
     if (device_cus(n_cu) != ATTN_OK)
         return ATTN_ERR_HIP;
@@ -239,6 +242,8 @@ int attn_fp8_cache_fwd(const attn_fp8_cache* cache, const attn_fp8_batch* batch,
     if ((q->type != ATTN_TYPE_BF16 && q->type != ATTN_TYPE_E4M3) || !out || misaligned(out, 16) || misaligned(lse, 4) ||
         misaligned(workspace, 256))
         return ATTN_ERR_INVALID_ARG;
+    if (!attn::cache_fwd_fits(batch->B, cache->Hkv, Hq / cache->Hkv, batch->max_q))
+        return ATTN_ERR_UNSUPPORTED;
     int n_cu = 0;
     if ((st = device_cus(n_cu)) != ATTN_OK)
         return st;

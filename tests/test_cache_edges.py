@@ -93,7 +93,13 @@ def test_attention_of_too_many_threads_is_unsupported(A, B, max_q, Hkv, G):
     c, b, x = cache(A, Hkv=Hkv), batch(A, B=B, max_q=max_q, cu=MB, T=64), heads(A)
     assert A.attn_fp8_cache_fwd(c, b, x, Hkv * G, MB, 1, MB, 1, 0.1, 1.0, 0, None, 0, None) == A.ATTN_ERR_UNSUPPORTED
     assert A.attn_fp8_cache_workspace_bytes(c, b, Hkv * G, 0) == (A.ATTN_ERR_UNSUPPORTED, 0)
-    assert A.attn_fp8_cache_weights(c, b, x, Hkv * G, MB, 1, 0.1, 1.0, 0, 4 * MB, 1 << 40, 1 << 20, None) == A.ATTN_ERR_UNSUPPORTED
+
+
+@pytest.mark.parametrize("B,Hkv", [((1 << 31) - 1, 1 << 16), (1 << 20, 16)])
+def test_weights_of_too_many_threads_are_unsupported(A, B, Hkv):
+    """A workgroup per (sequence, KV head) at least; the new tokens are not in its grid."""
+    c, b, x = cache(A, Hkv=Hkv), batch(A, B=B, cu=MB, T=64, max_q=1 << 22), heads(A)
+    assert A.attn_fp8_cache_weights(c, b, x, Hkv, MB, 1, 0.1, 1.0, 0, 4 * MB, 1 << 40, 1 << 20, None) == A.ATTN_ERR_UNSUPPORTED
 
 
 def test_grids_of_a_plan(A):

@@ -75,3 +75,20 @@ def test_bound_on_the_length(A, kernel):
                     max_len=cut)
     want = R.weights(c, q, lse, G, n_w, cu=cu)[:, :, :cut]
     within(w.cpu().double().numpy(), want, 2.0 ** -17 * want)
+
+
+@pytest.mark.parametrize("max_q", [1 << 16, 1 << 22])
+def test_a_loose_bound_on_the_new_tokens(A, max_q):
+    """The weights' launch does not grow with max_q."""
+    G, Hkv, B, d, page = 4, 8, 64, 64, 64
+    rng = np.random.default_rng(5)
+    lens, new = [int(n) for n in rng.integers(1, 100, B)], [1] * B
+    c = R.make_cache(rng, B, Hkv, page, d, lens)
+    q = R.make_queries(rng, B, G * Hkv, d)
+    lse = R.attention(c, q, G, cu=cu_of(new))[1].astype(np.float32)
+    n_w = c.pages.shape[1] * page
+    w = torch.zeros((B, Hkv, n_w), device="cuda")
+    log(f"weights max_q={max_q}")
+    A.cache_weights(R.torch_q(q, "bf16").cuda(), dev(lse), dev_cache(A, c), dev(c.pages), dev(c.lens), w, cu=dev(cu_of(new)), max_q=max_q)
+    want = R.weights(c, q, lse, G, n_w, cu=cu_of(new))
+    within(w.cpu().double().numpy(), want, 2.0 ** -17 * want)
