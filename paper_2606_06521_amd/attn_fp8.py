@@ -3,8 +3,9 @@
 The C entry points are exposed under their C names; ``fwd`` and
 ``p_underflow_count`` are thin conveniences that take torch tensors on the GPU,
 check their dtypes and shapes, allocate outputs with torch and pass the
-current torch stream; ``rope``, ``cache_append``, ``cache_fwd``, ``cache_weights``
-and ``cache_evict`` do the same for the KV cache, through a native module.  Every step of the computation
+current torch stream; ``rope``, ``cache_append``, ``cache_fwd``, ``cache_weights``,
+``cache_evict``, ``cache_bounds``, ``cache_select``, ``cache_fwd_blocks`` and ``cache_fwd_shared`` do the same for
+the KV cache, through a native module.  Every step of the computation
 runs in the HIP kernels; there is no fallback.  If the shared library is missing the import fails,
 if the native module is, the cache calls do.
 """
@@ -208,18 +209,49 @@ _lib.attn_fp8_cache_weights.argtypes = [_PC, _PB, _PH, _I, _P, _I, _F, _F, _I, _
 _lib.attn_fp8_cache_weights.restype = _I
 _lib.attn_fp8_cache_evict.argtypes = [_PC, _PB, _PC, _P, _P, _L, _L, _I, _I, _I, _P, _P, _P, _P]
 _lib.attn_fp8_cache_evict.restype = _I
+# include/attn_fp8_parts.h
+_lib.attn_fp8_cache_bounds.argtypes = [_PC, _PB, _P, _P]
+_lib.attn_fp8_cache_bounds.restype = _I
+_lib.attn_fp8_cache_select.argtypes = [_PC, _PB, _PH, _I, _P, _P] + [_I] * 6 + [_P]
+_lib.attn_fp8_cache_select.restype = _I
+_lib.attn_fp8_cache_fwd_blocks.argtypes = [_PC, _PB, _PH, _I, _P, _I, _I, _P, _I, _P, _I, _F, _F, _P, _Z, _P]
+_lib.attn_fp8_cache_fwd_blocks.restype = _I
+_lib.attn_fp8_cache_blocks_workspace_bytes.argtypes = [_PC, _PB, _I, _I, _I, ctypes.POINTER(_Z)]
+_lib.attn_fp8_cache_blocks_workspace_bytes.restype = _I
+_lib.attn_fp8_cache_fwd_shared.argtypes = [_PC, _PB, _I, _PH, _I, _P, _I, _P, _I, _F, _F, _I, _P, _Z, _P]
+_lib.attn_fp8_cache_fwd_shared.restype = _I
+_lib.attn_fp8_cache_shared_workspace_bytes.argtypes = [_PC, _PB, _I, _I, _I, ctypes.POINTER(_Z)]
+_lib.attn_fp8_cache_shared_workspace_bytes.restype = _I
 
 attn_fp8_rope = _lib.attn_fp8_rope
 attn_fp8_cache_append = _lib.attn_fp8_cache_append
 attn_fp8_cache_fwd = _lib.attn_fp8_cache_fwd
 attn_fp8_cache_weights = _lib.attn_fp8_cache_weights
 attn_fp8_cache_evict = _lib.attn_fp8_cache_evict
+attn_fp8_cache_bounds = _lib.attn_fp8_cache_bounds
+attn_fp8_cache_select = _lib.attn_fp8_cache_select
+attn_fp8_cache_fwd_blocks = _lib.attn_fp8_cache_fwd_blocks
+attn_fp8_cache_fwd_shared = _lib.attn_fp8_cache_fwd_shared
 
 
 def attn_fp8_cache_workspace_bytes(cache, batch, Hq, max_len):
     """Returns (status, bytes)."""
     n = _Z(0)
     st = _lib.attn_fp8_cache_workspace_bytes(cache, batch, Hq, max_len, ctypes.byref(n))
+    return st, n.value
+
+
+def attn_fp8_cache_blocks_workspace_bytes(cache, batch, Hq, take, run):
+    """Returns (status, bytes)."""
+    n = _Z(0)
+    st = _lib.attn_fp8_cache_blocks_workspace_bytes(cache, batch, Hq, take, run, ctypes.byref(n))
+    return st, n.value
+
+
+def attn_fp8_cache_shared_workspace_bytes(cache, batch, shared, Hq, max_len):
+    """Returns (status, bytes)."""
+    n = _Z(0)
+    st = _lib.attn_fp8_cache_shared_workspace_bytes(cache, batch, shared, Hq, max_len, ctypes.byref(n))
     return st, n.value
 
 
@@ -491,3 +523,50 @@ def cache_evict(cache, pages, lens, weights, to, new_pages, budget, *, n_sink: i
     new_weights [B, Hkv, budget] float32: theirs, then 0); given ones overlap no input."""
     return _call(stream, _binding.evict, cache, pages, lens, weights, to, new_pages, budget, n_sink, n_recent, kept,
                  new_lens, new_weights)
+
+
+# ---- attention over parts of the cache ----
+
+def key_bounds(n_pages, Hkv, d, *, device="cuda"):
+    """Room for the bounds of a cache's keys, float8_e4m3fn [pages, Hkv, 2, d] of zeros: the
+    least code of each channel of a page, and the largest."""
+    return torch.zeros((n_pages, Hkv, 2, d), dtype=torch.uint8, device=device).view(torch.float8_e4m3fn)
+
+
+def cache_bounds(cache, pages, lens, bounds, *, cu=None, max_q=None, stream=None):
+    """Writes the bounds (key_bounds) of the pages that hold the last max_q tokens of each
+    sequence (None: all of them), or with cu int32 [B + 1] the last cu[b + 1] - cu[b], of which the
+    first max_q count, as cache_append has written them; returns bounds.  To be called after each
+    append: a page's codes change when its scale grows."""
+    return _call(stream, _binding.bounds, cache, pages, lens, bounds, cu, max_q)
+
+
+def cache_select(q, cache, pages, lens, bounds, take, *, cu=None, max_q=None, run: int = 1, n_first: int = 1,
+                 n_last: int = 1, causal: bool = True, max_len: int = 0, blocks=None, stream=None):
+    """The `take` pages of each run of `run` new tokens and KV head whose bounds allow the largest
+    scores of the run's queries, as places in the sequence's row of pages: int32
+    [B, ceil(max_q / run), Hkv, take], ascending, then -1.  The first n_first and the last n_last
+    of the pages that the run sees are always among them; equal scores: the earlier page.
+    q and the others as for cache_fwd."""
+    return _call(stream, _binding.select, q, cache, pages, lens, bounds, take, cu, max_q, run, n_first, n_last, causal,
+                 max_len, blocks)
+
+
+def cache_fwd_blocks(q, cache, pages, lens, blocks, *, cu=None, max_q=None, run: int = 1, causal: bool = True,
+                     sm_scale=None, q_descale: float = 1.0, out=None, out_dtype=torch.bfloat16, lse=None,
+                     want_lse: bool = True, stream=None):
+    """cache_fwd over the pages of lists alone: blocks int32 [B, ceil(max_q / run), Hkv, take], one
+    list for each run of `run` new tokens and KV head, as cache_select gives them (any order; below
+    0: none; a page listed twice counts twice).  A query sees of them what it sees of the sequence."""
+    return _call(stream, _binding.fwd_blocks, q, cache, pages, lens, blocks, cu, max_q, run, causal, sm_scale, q_descale,
+                 out, _OUT_TYPES[out_dtype], lse, want_lse)
+
+
+def cache_fwd_shared(q, cache, pages, lens, n_shared, *, cu=None, max_q=None, causal: bool = True, sm_scale=None,
+                     q_descale: float = 1.0, max_len: int = 0, out=None, out_dtype=torch.bfloat16, lse=None,
+                     want_lse: bool = True, stream=None):
+    """cache_fwd for sequences that begin with the same n_shared pages (those of the first row of
+    pages; the other rows' first n_shared entries are not looked at): the same result, with these
+    pages read once for the queries of all sequences."""
+    return _call(stream, _binding.fwd_shared, q, cache, pages, lens, n_shared, cu, max_q, causal, sm_scale, q_descale,
+                 max_len, out, _OUT_TYPES[out_dtype], lse, want_lse)

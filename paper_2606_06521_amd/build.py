@@ -21,7 +21,8 @@ BINDING = os.path.join(HERE, "_cache_binding.so")
 SOURCES = ["attn_fp8_abi.hip", "attn_fast.hip", "attn_fast_pair.hip", "attn_fast_qk8.hip",
            "attn_fast_qk8_pair.hip", "attn_faithful.hip", "attn_prefill.hip", "attn_kv_bf16_16.hip",
            "attn_kv_bf16_32.hip", "attn_kv_qk8_16.hip", "attn_kv_qk8_32.hip", "cache_abi.hip",
-           "cache_rope.hip", "cache_fwd.hip", "cache_weights.hip", "cache_evict.hip"]
+           "cache_rope.hip", "cache_fwd.hip", "cache_weights.hip", "cache_evict.hip", "cache_bounds.hip",
+           "cache_select.hip", "cache_fwd_blocks.hip", "cache_fwd_shared.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 # -packed-fp32-ops: no packed FP32 VALU instructions anywhere in the device code

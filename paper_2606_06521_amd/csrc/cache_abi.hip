@@ -1,7 +1,8 @@
-// C ABI of the KV cache (declared in include/attn_fp8_cache.h): argument
+// C ABI of the KV cache (declared in include/attn_fp8_cache.h and attn_fp8_parts.h): argument
 // validation and launch on the caller's stream.  No state is kept and no memory
 // is allocated.
 #include "../../include/attn_fp8_cache.h"
+#include "../../include/attn_fp8_parts.h"
 #include "cache_common.hpp"
 
 #include <math.h>
@@ -149,6 +150,82 @@ int device_cus(int& n_cu)
     return ATTN_OK;
 }
 
+// What the attention calls share: pointers, types and the launch parameters.
+int check_fwd(const attn_fp8_cache* cache, const attn_fp8_batch* batch, const attn_fp8_heads* q, const void* out,
+              const float* lse, const void* workspace)
+{
+    int st;
+    if ((st = check_cache(cache)) != ATTN_OK || (st = check_batch(batch, true)) != ATTN_OK || (st = check_heads(q)) != ATTN_OK)
+        return st;
+    if ((q->type != ATTN_TYPE_BF16 && q->type != ATTN_TYPE_E4M3) || !out || misaligned(out, 16) || misaligned(lse, 4) ||
+        misaligned(workspace, 256))
+        return ATTN_ERR_INVALID_ARG;
+    return ATTN_OK;
+}
+
+void fill_fwd(attn::FwdParams& p, const attn_fp8_cache* cache, const attn_fp8_batch* batch, const attn_fp8_heads* q, int Hq,
+              void* out, int out_type, float* lse, int causal, float sm_scale, float q_descale, int max_len, void* workspace)
+{
+    p.bt = batch_of(batch);
+    p.cache = cache_of(cache);
+    p.q = heads_of(q);
+    p.out = out;
+    p.lse = lse;
+    p.ws = static_cast<float*>(workspace);
+    p.out_bf16 = out_type == ATTN_TYPE_BF16;
+    p.Hq = Hq;
+    p.gr = attn::group_of(Hq / cache->Hkv);
+    p.causal = causal;
+    p.max_len = longest(cache, batch, max_len);
+    p.c = factor_of(sm_scale, q_descale);
+}
+
+// Lists of `take` blocks for runs of new tokens: how many a KV head has.
+int check_lists(const attn_fp8_cache* c, const attn_fp8_batch* bt, int take, int most, int run, int64_t& runs)
+{
+    if (take < 1 || run < 1)
+        return ATTN_ERR_INVALID_ARG;
+    runs = ((int64_t)bt->max_q + run - 1) / run;
+    unsigned lists;
+    if (take > most || attn::grid_of((__int128)bt->B * c->Hkv * runs, 256, lists) != hipSuccess)
+        return ATTN_ERR_UNSUPPORTED;
+    return ATTN_OK;
+}
+
+// The plan of an attention over lists; ATTN_ERR_UNSUPPORTED if it cannot be launched.
+int plan_blocks(const attn_fp8_cache* c, const attn_fp8_batch* bt, int Hq, int take, int run, int64_t runs, attn::FwdPlan& pl)
+{
+    const int G = Hq / c->Hkv;
+    const int64_t lists = (int64_t)bt->B * c->Hkv * runs;
+    run = run < bt->max_q ? run : bt->max_q;
+    unsigned fewest;
+    if (attn::grid_of((__int128)lists * (((int64_t)run * G + 127) / 128), 256, fewest) != hipSuccess)
+        return ATTN_ERR_UNSUPPORTED;
+    int n_cu = 0;
+    if (device_cus(n_cu) != ATTN_OK)
+        return ATTN_ERR_HIP;
+    pl = attn::blocks_plan(lists, G, run, take, c->page, c->d, n_cu);
+    attn::FwdGrids g;
+    return attn::blocks_grids(lists, (int64_t)run * G, c->d, pl, g) == hipSuccess ? ATTN_OK : ATTN_ERR_UNSUPPORTED;
+}
+
+int plan_shared(const attn_fp8_cache* c, const attn_fp8_batch* bt, int shared, int Hq, int max_len, attn::SharedPlan& pl)
+{
+    const int G = Hq / c->Hkv;
+    if (shared < 0 || shared > bt->W)
+        return ATTN_ERR_INVALID_ARG;
+    if ((int64_t)G * bt->T > 1 << 24 || !attn::cache_fwd_fits(bt->B, c->Hkv, G, bt->max_q))
+        return ATTN_ERR_UNSUPPORTED;
+    if (bt->B == 0 || bt->T == 0)
+        return ATTN_OK;
+    int n_cu = 0;
+    if (device_cus(n_cu) != ATTN_OK)
+        return ATTN_ERR_HIP;
+    pl = attn::shared_plan(bt->B, c->Hkv, G, bt->T, bt->max_q, shared, longest(c, bt, max_len), c->page, c->d, n_cu);
+    attn::SharedGrids g;
+    return attn::shared_grids(bt->B, c->Hkv, G, bt->max_q, c->d, pl, g) == hipSuccess ? ATTN_OK : ATTN_ERR_UNSUPPORTED;
+}
+
 }  // namespace
 
 extern "C" {
@@ -237,29 +314,15 @@ int attn_fp8_cache_fwd(const attn_fp8_cache* cache, const attn_fp8_batch* batch,
         return ATTN_ERR_INVALID_ARG;
     if (batch->B == 0 || batch->T == 0)
         return ATTN_OK;
-    if ((st = check_cache(cache)) != ATTN_OK || (st = check_batch(batch, true)) != ATTN_OK || (st = check_heads(q)) != ATTN_OK)
+    if ((st = check_fwd(cache, batch, q, out, lse, workspace)) != ATTN_OK)
         return st;
-    if ((q->type != ATTN_TYPE_BF16 && q->type != ATTN_TYPE_E4M3) || !out || misaligned(out, 16) || misaligned(lse, 4) ||
-        misaligned(workspace, 256))
-        return ATTN_ERR_INVALID_ARG;
     if (!attn::cache_fwd_fits(batch->B, cache->Hkv, Hq / cache->Hkv, batch->max_q))
         return ATTN_ERR_UNSUPPORTED;
     int n_cu = 0;
     if ((st = device_cus(n_cu)) != ATTN_OK)
         return st;
     attn::FwdParams p{};
-    p.bt = batch_of(batch);
-    p.cache = cache_of(cache);
-    p.q = heads_of(q);
-    p.out = out;
-    p.lse = lse;
-    p.ws = static_cast<float*>(workspace);
-    p.out_bf16 = out_type == ATTN_TYPE_BF16;
-    p.Hq = Hq;
-    p.gr = attn::group_of(Hq / cache->Hkv);
-    p.causal = causal;
-    p.max_len = longest(cache, batch, max_len);
-    p.c = factor_of(sm_scale, q_descale);
+    fill_fwd(p, cache, batch, q, Hq, out, out_type, lse, causal, sm_scale, q_descale, max_len, workspace);
     const attn::FwdPlan pl = attn::cache_fwd_plan(batch->B, cache->Hkv, p.gr.G, batch->max_q, p.max_len, cache->d, n_cu);
     if (pl.bytes > 0 && (!workspace || workspace_bytes < pl.bytes))
         return ATTN_ERR_INVALID_ARG;
@@ -359,6 +422,156 @@ int attn_fp8_cache_evict(const attn_fp8_cache* from, const attn_fp8_batch* batch
     p.new_lens = new_lens;
     p.new_w = new_weights;
     return status(attn::launch_cache_evict(p, from->d, from->page, static_cast<hipStream_t>(stream)));
+}
+
+int attn_fp8_cache_bounds(const attn_fp8_cache* cache, const attn_fp8_batch* batch, void* bounds, void* stream)
+{
+    int st = check_sizes(cache, batch);
+    if (st != ATTN_OK || batch->B == 0)
+        return st;
+    if ((st = check_cache(cache)) != ATTN_OK || (st = check_batch(batch, true)) != ATTN_OK)
+        return st;
+    if (!bounds || misaligned(bounds, 16))
+        return ATTN_ERR_INVALID_ARG;
+    if (batch->T == 0 || batch->W == 0)
+        return ATTN_OK;
+    attn::BoundsParams p{};
+    p.bt = batch_of(batch);
+    p.cache = cache_of(cache);
+    p.bounds = static_cast<uint8_t*>(bounds);
+    // (n tokens lie in at most this many pages)
+    const int most = (batch->max_q + cache->page - 2) / cache->page + 1;
+    p.most = most < batch->W ? most : batch->W;
+    return status(attn::launch_cache_bounds(p, cache->d, cache->page, static_cast<hipStream_t>(stream)));
+}
+
+int attn_fp8_cache_select(const attn_fp8_cache* cache, const attn_fp8_batch* batch, const attn_fp8_heads* q, int Hq,
+                          const void* bounds, int32_t* blocks, int take, int run, int n_first, int n_last, int causal,
+                          int max_len, void* stream)
+{
+    int64_t runs;
+    int st = check_attention(cache, batch, Hq, causal, 1.f, 1.f, max_len);
+    if (st == ATTN_OK)
+        st = check_lists(cache, batch, take, attn::kMaxChoice, run, runs);
+    if (st != ATTN_OK)
+        return st;
+    if (!q || n_first < 0 || n_last < 0 || (int64_t)n_first + n_last > take)
+        return ATTN_ERR_INVALID_ARG;
+    const int most = longest(cache, batch, max_len);
+    if (most > attn::kMaxChoice * cache->page)
+        return ATTN_ERR_UNSUPPORTED;
+    if (batch->B == 0)
+        return ATTN_OK;
+    if ((st = check_cache(cache)) != ATTN_OK || (st = check_batch(batch, true)) != ATTN_OK ||
+        (batch->T > 0 && (st = check_heads(q)) != ATTN_OK))
+        return st;
+    if ((q->type != ATTN_TYPE_BF16 && q->type != ATTN_TYPE_E4M3) || !bounds || misaligned(bounds, 16) || !blocks || misaligned(blocks, 4))
+        return ATTN_ERR_INVALID_ARG;
+    attn::SelectParams p{};
+    p.bt = batch_of(batch);
+    p.cache = cache_of(cache);
+    p.q = heads_of(q);
+    p.bounds = static_cast<const uint8_t*>(bounds);
+    p.blocks = blocks;
+    p.take = take;
+    p.run = run < batch->max_q ? run : batch->max_q;
+    p.runs = (int)runs;
+    p.n_first = n_first;
+    p.n_last = n_last;
+    p.gr = attn::group_of(Hq / cache->Hkv);
+    p.causal = causal;
+    p.max_len = most;
+    return status(attn::launch_cache_select(p, cache->d, cache->page, q->type == ATTN_TYPE_E4M3, static_cast<hipStream_t>(stream)));
+}
+
+int attn_fp8_cache_blocks_workspace_bytes(const attn_fp8_cache* cache, const attn_fp8_batch* batch, int Hq, int take, int run,
+                                          size_t* bytes)
+{
+    if (!bytes)
+        return ATTN_ERR_INVALID_ARG;
+    *bytes = 0;
+    int64_t runs;
+    int st = check_attention(cache, batch, Hq, 1, 1.f, 1.f, 0);
+    if (st == ATTN_OK)
+        st = check_lists(cache, batch, take, 1 << 19, run, runs);
+    if (st != ATTN_OK || batch->B == 0 || batch->T == 0)
+        return st;
+    attn::FwdPlan pl;
+    st = plan_blocks(cache, batch, Hq, take, run, runs, pl);
+    if (st == ATTN_OK)
+        *bytes = pl.bytes;
+    return st;
+}
+
+int attn_fp8_cache_fwd_blocks(const attn_fp8_cache* cache, const attn_fp8_batch* batch, const attn_fp8_heads* q, int Hq,
+                              const int32_t* blocks, int take, int run, void* out, int out_type, float* lse, int causal,
+                              float sm_scale, float q_descale, void* workspace, size_t workspace_bytes, void* stream)
+{
+    int64_t runs;
+    int st = check_attention(cache, batch, Hq, causal, sm_scale, q_descale, 0);
+    if (st == ATTN_OK)
+        st = check_lists(cache, batch, take, 1 << 19, run, runs);
+    if (st != ATTN_OK)
+        return st;
+    if (!q || (out_type != ATTN_TYPE_BF16 && out_type != ATTN_TYPE_F32))
+        return ATTN_ERR_INVALID_ARG;
+    if (batch->B == 0 || batch->T == 0)
+        return ATTN_OK;
+    if ((st = check_fwd(cache, batch, q, out, lse, workspace)) != ATTN_OK)
+        return st;
+    if (!blocks || misaligned(blocks, 4))
+        return ATTN_ERR_INVALID_ARG;
+    attn::FwdPlan pl;
+    if ((st = plan_blocks(cache, batch, Hq, take, run, runs, pl)) != ATTN_OK)
+        return st;
+    if (pl.bytes > 0 && (!workspace || workspace_bytes < pl.bytes))
+        return ATTN_ERR_INVALID_ARG;
+    attn::BlocksParams p{};
+    fill_fwd(p, cache, batch, q, Hq, out, out_type, lse, causal, sm_scale, q_descale, 0, workspace);
+    p.blocks = blocks;
+    p.take = take;
+    p.run = run < batch->max_q ? run : batch->max_q;
+    p.runs = (int)runs;
+    return status(attn::launch_cache_fwd_blocks(p, pl, cache->d, cache->page, q->type == ATTN_TYPE_E4M3, static_cast<hipStream_t>(stream)));
+}
+
+int attn_fp8_cache_shared_workspace_bytes(const attn_fp8_cache* cache, const attn_fp8_batch* batch, int shared, int Hq,
+                                          int max_len, size_t* bytes)
+{
+    if (!bytes)
+        return ATTN_ERR_INVALID_ARG;
+    *bytes = 0;
+    int st = check_attention(cache, batch, Hq, 1, 1.f, 1.f, max_len);
+    attn::SharedPlan pl{};
+    if (st == ATTN_OK)
+        st = plan_shared(cache, batch, shared, Hq, max_len, pl);
+    if (st == ATTN_OK)
+        *bytes = pl.pre.bytes + pl.own.bytes;
+    return st;
+}
+
+int attn_fp8_cache_fwd_shared(const attn_fp8_cache* cache, const attn_fp8_batch* batch, int shared, const attn_fp8_heads* q, int Hq,
+                              void* out, int out_type, float* lse, int causal, float sm_scale, float q_descale, int max_len,
+                              void* workspace, size_t workspace_bytes, void* stream)
+{
+    int st = check_attention(cache, batch, Hq, causal, sm_scale, q_descale, max_len);
+    if (st != ATTN_OK)
+        return st;
+    if (!q || (out_type != ATTN_TYPE_BF16 && out_type != ATTN_TYPE_F32) || shared < 0 || shared > batch->W)
+        return ATTN_ERR_INVALID_ARG;
+    if (batch->B == 0 || batch->T == 0)
+        return ATTN_OK;
+    if ((st = check_fwd(cache, batch, q, out, lse, workspace)) != ATTN_OK)
+        return st;
+    attn::SharedPlan pl;
+    if ((st = plan_shared(cache, batch, shared, Hq, max_len, pl)) != ATTN_OK)
+        return st;
+    if (!workspace || workspace_bytes < pl.pre.bytes + pl.own.bytes)
+        return ATTN_ERR_INVALID_ARG;
+    attn::SharedParams p{};
+    fill_fwd(p, cache, batch, q, Hq, out, out_type, lse, causal, sm_scale, q_descale, max_len, workspace);
+    p.shared = shared;
+    return status(attn::launch_cache_fwd_shared(p, pl, cache->d, cache->page, q->type == ATTN_TYPE_E4M3, static_cast<hipStream_t>(stream)));
 }
 
 }  // extern "C"

@@ -1,4 +1,4 @@
-// Python module _cache_binding: the cache calls of attn_fp8_cache.h on torch
+// Python module _cache_binding: the cache calls of attn_fp8_cache.h and attn_fp8_parts.h on torch
 // tensors.  Checks the tensors' types, shapes and places, allocates outputs and the
 // workspace with torch, passes the current stream; everything else is the
 // library's.  Native because a short call is host time: the same in Python takes
@@ -16,6 +16,7 @@
 #include <string>
 
 #include "../../include/attn_fp8_cache.h"
+#include "../../include/attn_fp8_parts.h"
 
 namespace {
 
@@ -307,6 +308,47 @@ struct Queries {
     }
 };
 
+// Outputs and workspace of an attention call.
+struct Results {
+    at::Tensor out, lse, ws;
+    Results(const Queries& s, const at::Tensor& q, PyObject* given, PyObject* type, PyObject* given_lse, PyObject* want_lse)
+    {
+        if (given == Py_None) {
+            const int t = int_arg(type, "out_dtype");
+            out = s.at.empty({s.T, s.Hq, s.d}, t == ATTN_TYPE_F32 ? at::kFloat : at::kBFloat16);
+        } else {
+            out = tensor(given, "out");
+            if (out.sizes() != q.sizes() || !out.is_contiguous() || out.device() != s.at.device)
+                value_error("out must be a contiguous tensor of q's shape on its device");
+            if (out.scalar_type() != at::kBFloat16 && out.scalar_type() != at::kFloat)
+                type_error("out is bfloat16 or float32");
+        }
+        if (given_lse != Py_None) {
+            lse = tensor(given_lse, "lse");
+            dense<float>(lse, "lse", s.at, at::kFloat, {s.T, s.Hq});
+        } else if (truth(want_lse)) {
+            lse = s.at.empty({s.T, s.Hq}, at::kFloat);
+        }
+    }
+    void* workspace(const Place& at, size_t bytes)
+    {
+        if (bytes)
+            ws = at.empty({(int64_t)bytes}, at::kByte);
+        return bytes ? ws.data_ptr() : nullptr;
+    }
+    int out_type() const { return type_of(out.scalar_type()); }
+    float* lse_at() const { return lse.defined() ? static_cast<float*>(lse.data_ptr()) : nullptr; }
+    PyObject* pack() const
+    {
+        PyObject* o = wrap(out);
+        PyObject* l = lse.defined() ? wrap(lse) : Py_NewRef(Py_None);
+        PyObject* both = o && l ? PyTuple_Pack(2, o, l) : nullptr;
+        Py_XDECREF(o);
+        Py_XDECREF(l);
+        return both;
+    }
+};
+
 // fwd(q, cache, pages, lens, cu, max_q, causal, sm_scale, q_descale, max_len, out, out_type, lse, want_lse)
 PyObject* fwd(PyObject*, PyObject* const* a, Py_ssize_t n)
 {
@@ -315,40 +357,121 @@ PyObject* fwd(PyObject*, PyObject* const* a, Py_ssize_t n)
     const at::Tensor& q = tensor(a[0], "q");
     const Queries s(q, a[1], a[2], a[3], a[4], a[5], a[7]);
     const int max_len = int_arg(a[9], "max_len");
-    at::Tensor out, lse, ws;
-    if (a[10] == Py_None) {
-        const int type = int_arg(a[11], "out_dtype");
-        out = s.at.empty({s.T, s.Hq, s.d}, type == ATTN_TYPE_F32 ? at::kFloat : at::kBFloat16);
-    } else {
-        out = tensor(a[10], "out");
-        if (out.sizes() != q.sizes() || !out.is_contiguous() || out.device() != s.at.device)
-            value_error("out must be a contiguous tensor of q's shape on its device");
-        if (out.scalar_type() != at::kBFloat16 && out.scalar_type() != at::kFloat)
-            type_error("out is bfloat16 or float32");
-    }
-    if (a[12] != Py_None) {
-        lse = tensor(a[12], "lse");
-        dense<float>(lse, "lse", s.at, at::kFloat, {s.T, s.Hq});
-    } else if (truth(a[13])) {
-        lse = s.at.empty({s.T, s.Hq}, at::kFloat);
-    }
+    Results r(s, q, a[10], a[11], a[12], a[13]);
     size_t bytes = 0;
     int st = attn_fp8_cache_workspace_bytes(&s.c, &s.bt, (int)s.Hq, max_len, &bytes);
-    if (!st) {
-        if (bytes)
-            ws = s.at.empty({(int64_t)bytes}, at::kByte);
-        st = attn_fp8_cache_fwd(&s.c, &s.bt, &s.hq, (int)s.Hq, out.data_ptr(), type_of(out.scalar_type()),
-                                lse.defined() ? static_cast<float*>(lse.data_ptr()) : nullptr, truth(a[6]), s.sm_scale, real(a[8]),
-                                max_len, ws.defined() ? ws.data_ptr() : nullptr, bytes, s.at.stream);
-    }
-    if (st)
-        return PyLong_FromLong(st);
-    PyObject* o = wrap(out);
-    PyObject* l = lse.defined() ? wrap(lse) : Py_NewRef(Py_None);
-    PyObject* both = o && l ? PyTuple_Pack(2, o, l) : nullptr;
-    Py_XDECREF(o);
-    Py_XDECREF(l);
-    return both;
+    if (!st)
+        st = attn_fp8_cache_fwd(&s.c, &s.bt, &s.hq, (int)s.Hq, r.out.data_ptr(), r.out_type(), r.lse_at(), truth(a[6]), s.sm_scale,
+                                real(a[8]), max_len, r.workspace(s.at, bytes), bytes, s.at.stream);
+    return st ? PyLong_FromLong(st) : r.pack();
+    END_HANDLE_TH_ERRORS
+}
+
+// fwd_shared(q, cache, pages, lens, shared, cu, max_q, causal, sm_scale, q_descale, max_len, out, out_type, lse, want_lse)
+PyObject* fwd_shared(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    count_args(n, 15);
+    const at::Tensor& q = tensor(a[0], "q");
+    const Queries s(q, a[1], a[2], a[3], a[5], a[6], a[8]);
+    const int shared = int_arg(a[4], "n_shared"), max_len = int_arg(a[10], "max_len");
+    Results r(s, q, a[11], a[12], a[13], a[14]);
+    size_t bytes = 0;
+    int st = attn_fp8_cache_shared_workspace_bytes(&s.c, &s.bt, shared, (int)s.Hq, max_len, &bytes);
+    if (!st)
+        st = attn_fp8_cache_fwd_shared(&s.c, &s.bt, shared, &s.hq, (int)s.Hq, r.out.data_ptr(), r.out_type(), r.lse_at(), truth(a[7]),
+                                       s.sm_scale, real(a[9]), max_len, r.workspace(s.at, bytes), bytes, s.at.stream);
+    return st ? PyLong_FromLong(st) : r.pack();
+    END_HANDLE_TH_ERRORS
+}
+
+// Lists int32 [B][ceil(max_q / run)][Hkv][take]: its shape but for take.
+std::array<int64_t, 3> lists_of(const Queries& s, int run)
+{
+    if (run < 1)
+        value_error("run is at least 1");
+    return {s.bt.B, (s.bt.max_q + (int64_t)run - 1) / run, s.c.Hkv};
+}
+
+// fwd_blocks(q, cache, pages, lens, blocks, cu, max_q, run, causal, sm_scale, q_descale, out, out_type, lse, want_lse)
+PyObject* fwd_blocks(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    count_args(n, 15);
+    const at::Tensor& q = tensor(a[0], "q");
+    const Queries s(q, a[1], a[2], a[3], a[5], a[6], a[9]);
+    const int run = int_arg(a[7], "run");
+    const std::array<int64_t, 3> shape = lists_of(s, run);
+    const at::Tensor& lists = tensor(a[4], "blocks");
+    const int64_t take = lists.dim() == 4 ? lists.size(3) : 0;
+    const int32_t* blocks = dense<int32_t>(lists, "blocks", s.at, at::kInt, {shape[0], shape[1], shape[2], take});
+    const int per_list = narrow(take, "take");
+    Results r(s, q, a[11], a[12], a[13], a[14]);
+    size_t bytes = 0;
+    int st = attn_fp8_cache_blocks_workspace_bytes(&s.c, &s.bt, (int)s.Hq, per_list, run, &bytes);
+    if (!st)
+        st = attn_fp8_cache_fwd_blocks(&s.c, &s.bt, &s.hq, (int)s.Hq, blocks, per_list, run, r.out.data_ptr(), r.out_type(), r.lse_at(),
+                                       truth(a[8]), s.sm_scale, real(a[10]), r.workspace(s.at, bytes), bytes, s.at.stream);
+    return st ? PyLong_FromLong(st) : r.pack();
+    END_HANDLE_TH_ERRORS
+}
+
+// A cache's bounds, E4M3 [pages][Hkv][2][d].
+void* bounds_of(PyObject* o, const attn_fp8_cache& c, const Place& at)
+{
+    const at::Tensor& t = tensor(o, "bounds");
+    if (!is_codes(t) || t.sizes() != at::IntArrayRef({(int64_t)c.n_pages, (int64_t)c.Hkv, (int64_t)2, (int64_t)c.d}) || !t.is_contiguous() ||
+        t.device() != at.device)
+        value_error("bounds must be a contiguous float8_e4m3fn (or uint8) tensor " + shape_text({c.n_pages, c.Hkv, 2, c.d}) + " on " +
+                    at.device.str());
+    return t.data_ptr();
+}
+
+// select(q, cache, pages, lens, bounds, take, cu, max_q, run, n_first, n_last, causal, max_len, blocks)
+PyObject* select(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    count_args(n, 14);
+    const Queries s(tensor(a[0], "q"), a[1], a[2], a[3], a[6], a[7], Py_None);
+    const int take = int_arg(a[5], "take"), run = int_arg(a[8], "run");
+    const std::array<int64_t, 3> shape = lists_of(s, run);
+    if (take < 1)
+        value_error("take is at least 1");
+    const void* bounds = bounds_of(a[4], s.c, s.at);
+    const std::array<int64_t, 4> full = {shape[0], shape[1], shape[2], take};
+    const at::Tensor lists = a[13] == Py_None ? s.at.empty(full, at::kInt) : tensor(a[13], "blocks");
+    int32_t* blocks = dense<int32_t>(lists, "blocks", s.at, at::kInt, full);
+    const int st = attn_fp8_cache_select(&s.c, &s.bt, &s.hq, (int)s.Hq, bounds, blocks, take, run, int_arg(a[9], "n_first"),
+                                         int_arg(a[10], "n_last"), truth(a[11]), int_arg(a[12], "max_len"), s.at.stream);
+    return st ? PyLong_FromLong(st) : wrap(lists);
+    END_HANDLE_TH_ERRORS
+}
+
+// bounds(cache, pages, lens, bounds, cu, max_q)
+PyObject* bounds(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    count_args(n, 6);
+    const Place at(tensor(a[2], "lens"));
+    const attn_fp8_cache c = cache_of(a[0], at);
+    const at::Tensor& pages = tensor(a[1], "pages");
+    if (pages.dim() != 2)
+        value_error("pages must be [B, W]");
+    // (max_q tokens of each sequence, or by cu, whose entries may be any)
+    const int64_t most = a[5] == Py_None ? pages.size(1) * c.page : integer(a[5]);
+    if (most < 0 || most > INT32_MAX)
+        value_error("max_q is out of range");
+    attn_fp8_batch bt{};
+    bt.pages = ints(a[1], "pages", at, pages.sizes());
+    bt.B = narrow(pages.size(0), "B");
+    bt.W = narrow(pages.size(1), "W");
+    bt.lens = ints(a[2], "lens", at, {pages.size(0)});
+    bt.max_q = (int)(most < 1 ? 1 : most);
+    if (a[4] != Py_None)
+        bt.cu = ints(a[4], "cu", at, {pages.size(0) + 1});
+    bt.T = a[4] != Py_None ? 1 << 30 : narrow(pages.size(0) * most, "tokens");
+    const int st = attn_fp8_cache_bounds(&c, &bt, bounds_of(a[3], c, at), at.stream);
+    return st ? PyLong_FromLong(st) : Py_NewRef(a[3]);
     END_HANDLE_TH_ERRORS
 }
 
@@ -428,6 +551,10 @@ PyMethodDef methods[] = {
     {"rope", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(&rope)), METH_FASTCALL, nullptr},
     {"append", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(&append)), METH_FASTCALL, nullptr},
     {"fwd", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(&fwd)), METH_FASTCALL, nullptr},
+    {"fwd_shared", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(&fwd_shared)), METH_FASTCALL, nullptr},
+    {"fwd_blocks", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(&fwd_blocks)), METH_FASTCALL, nullptr},
+    {"select", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(&select)), METH_FASTCALL, nullptr},
+    {"bounds", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(&bounds)), METH_FASTCALL, nullptr},
     {"weights", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(&weights)), METH_FASTCALL, nullptr},
     {"evict", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(&evict)), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr},

@@ -41,6 +41,9 @@ struct Rotation {
     int n_pos, rot, layout;      // layout 0: halves, 1: interleaved
 };
 
+// Most blocks of a sequence that a choice of pages looks at (their scores are kept in LDS).
+constexpr int kMaxChoice = 16384;
+
 // Sequence b: the keys there are (its length, at most max_len), its new tokens
 // [first, first + n) of the call (at most max_q, inside [0, T)), the position of the
 // first of them (by its whole length: it may lie before 0 or past the keys).
@@ -93,7 +96,7 @@ inline Group group_of(int G) { return {G, G == 1 ? 0u : (uint32_t)((((uint64_t)1
 // Page of a sequence's block, -1 if there is none.
 __device__ inline int page_of(const Batch& bt, int n_pages, int b, int block)
 {
-    const int p = block < bt.W ? bt.pages[(size_t)b * bt.W + block] : -1;
+    const int p = (uint32_t)block < (uint32_t)bt.W ? bt.pages[(size_t)b * bt.W + block] : -1;
     return (uint32_t)p < (uint32_t)n_pages ? p : -1;
 }
 
@@ -349,6 +352,39 @@ struct FwdParams {
     int tiles, chunk, ranges;   // row tiles per (sequence, KV head); visits per range; most ranges
 };
 
+// Attention over lists of pages: FwdParams with one list for `run` new tokens and a KV head.
+struct BlocksParams : FwdParams {
+    const int32_t* blocks;  // [B][runs][Hkv][take]: places in the sequence's table, below 0: none
+    int take, run, runs;
+};
+
+// Attention of a batch whose tables begin with the same `shared` pages.  tiles, chunk, ranges
+// and ws are those of the sequences' own pages.
+struct SharedParams : FwdParams {
+    int shared;
+    int pre_tiles, pre_chunk, pre_ranges, pre_rows;     // the shared pages' row tiles and ranges, rows per tile
+    float* pre_ws;
+    unsigned pre_grid;      // workgroups of a launch that work on them; those behind work on the own pages
+};
+
+struct BoundsParams {
+    Batch bt;
+    Cache cache;
+    uint8_t* bounds;        // E4M3 [n_pages][Hkv][2][d]: the least codes, the largest
+    int most;               // pages per sequence that may hold new tokens
+};
+
+struct SelectParams {
+    Batch bt;
+    Cache cache;
+    Heads q;
+    const uint8_t* bounds;
+    int32_t* blocks;        // [B][runs][Hkv][take]
+    int take, run, runs, n_first, n_last;
+    Group gr;
+    int causal, max_len;
+};
+
 struct WeightParams {
     Batch bt;
     Cache cache;
@@ -382,21 +418,40 @@ struct FwdPlan {
     size_t bytes;           // workspace
 };
 FwdPlan cache_fwd_plan(int B, int Hkv, int G, int max_q, int max_len, int d, int n_cu);
+// (heads: units of `rows` query rows; visits: of 128 keys)
+FwdPlan cache_fwd_plan(int64_t heads, int64_t rows, int visits, int d, int n_cu);
 
 // Whether a call can be launched at all, by the fewest workgroups of a plan; the grids of
 // one plan's launches (hipErrorNotSupported: too large).
 bool cache_fwd_fits(int B, int Hkv, int G, int max_q);
+// Plans of the calls over lists and over a shared prefix.
+FwdPlan blocks_plan(int64_t lists, int G, int run, int take, int page, int d, int n_cu);
+struct SharedPlan {
+    FwdPlan pre, own;       // the shared pages and the sequences' own (bytes: of the partial results, also of one range)
+};
+SharedPlan shared_plan(int B, int Hkv, int G, int T, int max_q, int shared, int max_len, int page, int d, int n_cu);
+
 struct FwdGrids {
     unsigned tiles, merges;
     int merge_rows;         // rows of a merging workgroup
 };
 hipError_t cache_fwd_grids(int B, int Hkv, int G, int max_q, int d, const FwdPlan& plan, FwdGrids& g);
+hipError_t blocks_grids(int64_t lists, int64_t rows, int d, const FwdPlan& plan, FwdGrids& g);
+struct SharedGrids {
+    unsigned pre, own, merges;
+    int merge_rows;
+};
+hipError_t shared_grids(int B, int Hkv, int G, int max_q, int d, const SharedPlan& plan, SharedGrids& g);
 
 hipError_t launch_rope(const Heads& x, const Heads& out, int T, int H, int d, int type, const Rotation& r, hipStream_t s);
 hipError_t launch_append(const Batch& bt, const Cache& c, int d, int page, const Heads& k, const Heads& v, int type,
                          const Rotation& r, const Heads& q, const Heads& q_out, int Hq, hipStream_t s);
 // (the launches: hipErrorNotSupported if a grid is too large, before any of them)
 hipError_t launch_cache_fwd(FwdParams p, const FwdPlan& plan, int d, int page, bool e4m3, hipStream_t s);
+hipError_t launch_cache_bounds(const BoundsParams& p, int d, int page, hipStream_t s);
+hipError_t launch_cache_select(const SelectParams& p, int d, int page, bool e4m3, hipStream_t s);
+hipError_t launch_cache_fwd_blocks(BlocksParams p, const FwdPlan& plan, int d, int page, bool e4m3, hipStream_t s);
+hipError_t launch_cache_fwd_shared(SharedParams p, const SharedPlan& plan, int d, int page, bool e4m3, hipStream_t s);
 hipError_t launch_cache_weights(const WeightParams& p, int d, int page, bool e4m3, int n_cu, hipStream_t s);
 hipError_t launch_cache_evict(const EvictParams& p, int d, int page, hipStream_t s);
 

@@ -1,0 +1,35 @@
+// Attention over lists of pages: a list for `run` new tokens of a sequence and a KV head.
+// The rows of a run and its list take the place of a sequence's rows and keys in the
+// kernels of the whole cache; a page of the list is anywhere in the sequence, so its first
+// key is read beside its number.
+#include "cache_merge.hpp"
+
+namespace attn {
+
+FwdPlan blocks_plan(int64_t lists, int G, int run, int take, int page, int d, int n_cu)
+{
+    return cache_fwd_plan(lists, (int64_t)run * G, (take + kVisit / page - 1) / (kVisit / page), d, n_cu);
+}
+
+hipError_t blocks_grids(int64_t lists, int64_t rows, int d, const FwdPlan& pl, FwdGrids& g)
+{
+    const hipError_t e = grid_of(((__int128)lists * pl.tiles * pl.ranges + kNumXcd - 1) / kNumXcd * kNumXcd, 256, g.tiles);
+    g.merge_rows = pl.ranges > 8 ? 1 : 1024 / d;
+    g.merges = 0;
+    return e != hipSuccess || pl.ranges == 1 ? e : grid_of((__int128)lists * ((rows + g.merge_rows - 1) / g.merge_rows), 256, g.merges);
+}
+
+hipError_t launch_cache_fwd_blocks(BlocksParams p, const FwdPlan& pl, int d, int page, bool e4m3, hipStream_t s)
+{
+    p.tiles = pl.tiles;
+    p.chunk = pl.chunk;
+    p.ranges = pl.ranges;
+    FwdGrids g;
+    hipError_t e = blocks_grids((int64_t)p.bt.B * p.cache.Hkv * p.runs, (int64_t)p.run * p.gr.G, d, pl, g);
+    if (e != hipSuccess)
+        return e;
+    e = fwd_launch(p, pl.rows, d, page, e4m3, g.tiles, s);
+    return e == hipSuccess && pl.ranges > 1 ? merge_launch(p, pl.rows, d, page, g.merges, g.merge_rows, s) : e;
+}
+
+}  // namespace attn

@@ -30,35 +30,187 @@
 
 #include "cache_common.hpp"
 
+#include <type_traits>
+
 namespace attn {
 
 constexpr int kMaxChunk = 128;      // visits of a range (its page numbers are kept in LDS)
 constexpr float kSlack = 16.f;      // how far (log2) a group's maximum may exceed the row's reference
 
-// Visits of a tile: those that hold a key that its last row sees.
-__device__ inline int tile_visits(const FwdParams& p, const Seq& s, int tile, int tile_rows)
+// What a kernel works on, by its parameters: FwdParams, the whole cache of a sequence;
+// BlocksParams, the pages of a list; SharedParams, the pages a batch begins with or those
+// behind them.
+template <class P>
+constexpr bool kLists = std::is_same_v<P, BlocksParams>;
+template <class P>
+constexpr bool kShared = std::is_same_v<P, SharedParams>;
+
+// A (sequence, KV head), or a run of it that has a list; or the KV head of the shared pages,
+// whose rows are those of all tokens of the call.
+struct Unit {
+    Seq s;                  // its tokens, and the keys there are
+    int b, hk;
+    int base;               // first of its pages in the table
+    bool common;            // the shared pages
+    const int32_t* list;    // its pages, if it has a list
+};
+
+template <class P>
+__device__ inline Unit unit_of(const P& p, int u, bool common)
 {
-    const int last = min((tile + 1) * tile_rows, s.n * p.gr.G) - 1;       // last row
-    const int seen = p.causal ? min(max(s.pos0 + p.gr.token(last) + 1, 0), s.len) : s.len;
-    return (seen + kVisit - 1) / kVisit;
+    Unit t{};
+    if constexpr (kShared<P>)
+        if (common) {
+            t.hk = u;
+            t.common = true;
+            t.s = {p.max_len, 0, p.bt.T, 0};
+            return t;
+        }
+    int run = 0;
+    if constexpr (kLists<P>) {
+        run = u % p.runs;
+        u /= p.runs;
+    }
+    t.hk = u % p.cache.Hkv;
+    t.b = u / p.cache.Hkv;
+    t.s = sequence(p.bt, t.b, p.max_len);
+    if constexpr (kLists<P>) {
+        t.list = p.blocks + (((int64_t)t.b * p.runs + run) * p.cache.Hkv + t.hk) * p.take;
+        t.s.first += run * p.run;
+        t.s.pos0 += run * p.run;
+        t.s.n = min(max(t.s.n - run * p.run, 0), p.run);
+    }
+    if constexpr (kShared<P>)
+        t.base = p.shared;
+    return t;
 }
 
-// Workgroup -> tile, range, KV head and sequence.  Tiles run fastest and each XCD
-// takes a contiguous run: the tiles that read the same keys share an L2.
-__device__ inline bool workgroup_of(const FwdParams& p, int& tile, int& range, int& hk, int& b)
+// Keys that one of a tile's rows sees (the first ones of a unit without a list).
+__device__ inline int tile_seen(const FwdParams& p, const Seq& s, int tile, int tile_rows)
 {
-    const int total = p.bt.B * p.cache.Hkv * p.ranges * p.tiles;
+    const int last = min((tile + 1) * tile_rows, s.n * p.gr.G) - 1;       // last row
+    return p.causal ? min(max(s.pos0 + p.gr.token(last) + 1, 0), s.len) : s.len;
+}
+
+// Visits of a tile: those that hold a key that its last row sees; of a list, all; of the shared
+// pages, as many for every tile.
+template <class P>
+__device__ inline int tile_visits(const P& p, const Unit& t, int tile, int tile_rows, int page)
+{
+    if constexpr (kLists<P>)
+        return (p.take + kVisit / page - 1) / (kVisit / page);
+    int seen = t.common ? p.max_len : tile_seen(p, t.s, tile, tile_rows);
+    if constexpr (kShared<P>)
+        seen = t.common ? min(p.shared * page, seen) : seen - p.shared * page;
+    return (max(seen, 0) + kVisit - 1) / kVisit;
+}
+
+// Workgroup -> tile, range and unit.  Tiles run fastest and each XCD takes a
+// contiguous run: the tiles that read the same keys share an L2.
+__device__ inline bool workgroup_of(int wg, int units, int ranges, int tiles, int& tile, int& range, int& unit)
+{
+    const int total = units * ranges * tiles;
     const int per_xcd = (total + kNumXcd - 1) / kNumXcd;
-    const int slot = (int)(blockIdx.x / kNumXcd), L = (int)(blockIdx.x % kNumXcd) * per_xcd + slot;
+    const int slot = wg / kNumXcd, L = wg % kNumXcd * per_xcd + slot;
     if (slot >= per_xcd || L >= total)
         return false;
-    tile = p.tiles - 1 - L % p.tiles;           // (causal: the longest first)
-    int rest = L / p.tiles;
-    range = rest % p.ranges;
-    rest /= p.ranges;
-    hk = rest % p.cache.Hkv;
-    b = rest / p.cache.Hkv;
+    tile = tiles - 1 - L % tiles;           // (causal: the longest first)
+    const int rest = L / tiles;
+    range = rest % ranges;
+    unit = rest / ranges;
     return true;
+}
+
+// The workgroup's share of a launch: false if it has none.
+struct Share {
+    Unit u;
+    int tile, range, unit, visits, v0, v1;
+    bool whole;             // the only range of its tile: writes the result itself
+};
+
+template <class P>
+__device__ inline bool share_of(const P& p, int tile_rows, int page, Share& x)
+{
+    bool common = false;
+    int wg = (int)blockIdx.x, units = p.bt.B * p.cache.Hkv, ranges = p.ranges, tiles = p.tiles, chunk = p.chunk;
+    if constexpr (kLists<P>)
+        units *= p.runs;
+    if constexpr (kShared<P>) {
+        common = blockIdx.x < p.pre_grid;
+        if (common) {
+            units = p.cache.Hkv;
+            ranges = p.pre_ranges;
+            tiles = p.pre_tiles;
+            chunk = p.pre_chunk;
+        } else {
+            wg -= (int)p.pre_grid;
+        }
+    }
+    if (!workgroup_of(wg, units, ranges, tiles, x.tile, x.range, x.unit))
+        return false;
+    x.u = unit_of(p, x.unit, common);
+    x.u.s = uniform(x.u.s);
+    if (x.tile * tile_rows >= x.u.s.n * p.gr.G)
+        return false;
+    x.visits = tile_visits(p, x.u, x.tile, tile_rows, page);
+    x.v0 = x.range * chunk;
+    x.v1 = min(x.v0 + chunk, x.visits);
+    x.whole = !kShared<P> && (kLists<P> ? p.ranges == 1 : x.visits <= chunk);
+    return x.v0 < x.v1 || (!kShared<P> && x.range == 0) || (kLists<P> && !x.whole);
+}
+
+// Where the partial result of a workgroup goes.
+template <class P>
+__device__ inline float* part_of(const P& p, const Share& x, int tile_rows, int d)
+{
+    const size_t stride = (size_t)tile_rows * (d + 2);
+    if constexpr (kShared<P>)
+        if (x.u.common)
+            return p.pre_ws + (((size_t)x.unit * p.pre_tiles + x.tile) * p.pre_ranges + x.range) * stride;
+    return p.ws + (((size_t)x.unit * p.tiles + x.tile) * p.ranges + x.range) * stride;
+}
+
+constexpr int kSeesAll = 1 << 30;   // (past every key)
+
+// The last keys that the rows row0 .. row0 + rows - 1 of all tokens see, of the sequences that
+// they belong to; a token of none sees all (its row is not used).
+__device__ inline void common_last(const SharedParams& p, int row0, int rows, int* last)
+{
+    for (int r = threadIdx.x; r < rows; r += 256)
+        last[r] = kSeesAll;
+    __syncthreads();
+    const int from = p.gr.token(row0), to = p.gr.token(row0 + rows - 1);
+    for (int b = threadIdx.x; b < p.bt.B; b += 256) {
+        const Seq s = sequence(p.bt, b, p.max_len);
+        for (int i = max(s.first, from); i <= min(s.first + s.n - 1, to); ++i) {
+            const int key = last_key(s.pos0 + i - s.first, p.causal, s.len);
+            for (int r = max(i * p.gr.G - row0, 0); r < min((i + 1) * p.gr.G - row0, rows); ++r)
+                last[r] = key;
+        }
+    }
+    __syncthreads();
+}
+
+// The end of the visits of a range from v0 on that have a page (np pages of a list).
+template <int PPV>
+__device__ inline int listed_end(const int* pids, int v0, int np, int lane)
+{
+    int end = 0;
+    for (int i = 0; i < np; i += 64) {
+        const uint64_t some = __ballot(i + lane < np && pids[i + lane] >= 0);
+        end = some ? i + 64 - __builtin_clzll(some) : end;
+    }
+    return v0 + (end + PPV - 1) / PPV;
+}
+
+// Pages that the batch shares.
+template <class P>
+__device__ inline int shared_pages(const P& p)
+{
+    if constexpr (kShared<P>)
+        return p.shared;
+    else
+        return 0;
 }
 
 // Four channels of a row's result: acc / l (inv = 1 / l), in units of 2^m.
@@ -84,8 +236,8 @@ __device__ inline void write_row(const FwdParams& p, const Seq& s, int hk, int R
         p.lse[row] = m == -INFINITY ? -INFINITY : (m + __builtin_log2f(l)) * 0.6931471805599453f;
 }
 
-template <int D, int PAGE, bool E4M3>
-__global__ void __launch_bounds__(256, 1) cache_fwd_kernel(FwdParams p)
+template <int D, int PAGE, bool E4M3, class P>
+__global__ void __launch_bounds__(256, 1) cache_fwd_kernel(P p)
 {
     constexpr int NW = 4, TR = 16;
     constexpr int PPV = kVisit / PAGE;          // pages per visit
@@ -105,33 +257,59 @@ __global__ void __launch_bounds__(256, 1) cache_fwd_kernel(FwdParams p)
     __shared__ uint8_t kbyte[kMaxChunk * PPV], vbyte[kMaxChunk * PPV];
     __shared__ float lsh[NW][TR], msh[NW][TR];
 
-    int tile, range, hk, b;
-    if (!workgroup_of(p, tile, range, hk, b))
+    __shared__ int starts[kLists<P> ? kMaxChunk * PPV : 1];      // first keys of a list's pages
+    __shared__ int row_last[kShared<P> ? TR : 1];
+
+    Share x;
+    if (!share_of(p, TR, PAGE, x))
         return;
-    const Seq s = uniform(sequence(p.bt, b, p.max_len));
-    const int rows = s.n * p.gr.G;
-    const int row0 = tile * TR;
-    if (row0 >= rows)
-        return;
-    const int visits = tile_visits(p, s, tile, TR);
-    const int v0 = range * p.chunk, v1 = min(v0 + p.chunk, visits);
-    if (v0 >= v1 && range > 0)
-        return;
-    const bool whole = visits <= p.chunk;               // the only range of the tile
+    const Seq& s = x.u.s;
+    const int rows = s.n * p.gr.G, row0 = x.tile * TR, hk = x.u.hk;
+    const int v0 = x.v0;
+    int v1 = x.v1;
 
     const int tid = threadIdx.x, lane = tid & 63;
     const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int n = lane & 15, g = lane >> 4;
     const int row = row0 + n;
-    const int pos = row < rows ? last_key(s.pos0 + p.gr.token(row), p.causal, s.len) : -1;
-    const int pos_min = last_key(s.pos0 + p.gr.token(row0), p.causal, s.len);
-    const int seen = p.causal ? min(max(s.pos0 + p.gr.token(min(row0 + TR, rows) - 1) + 1, 0), s.len) : s.len;
+    int pos = row < rows ? last_key(s.pos0 + p.gr.token(row), p.causal, s.len) : -1;
+    int pos_min = last_key(s.pos0 + p.gr.token(row0), p.causal, s.len), seen = tile_seen(p, s, x.tile, TR);
+    if constexpr (kShared<P>)
+        if (x.u.common) {
+            common_last(p, row0, TR, row_last);
+            pos = row_last[n];
+            int lo = pos, hi = pos;
+#pragma unroll
+            for (int off = 8; off > 0; off >>= 1) {
+                lo = min(lo, __shfl_xor(lo, off, 64));
+                hi = max(hi, __shfl_xor(hi, off, 64));
+            }
+            pos_min = __builtin_amdgcn_readfirstlane(lo);
+            seen = min(p.shared * PAGE, min(__builtin_amdgcn_readfirstlane(hi), p.max_len - 1) + 1);
+        }
 
     // the range's page numbers, then their scales
     const int np = max(v1 - v0, 0) * PPV;
-    for (int i = tid; i < np; i += 256)
-        pids[i] = page_of(p.bt, p.cache.n_pages, b, v0 * PPV + i);
+    for (int i = tid; i < np; i += 256) {
+        const int at = v0 * PPV + i;
+        if constexpr (kLists<P>) {
+            const int block = at < p.take ? x.u.list[at] : -1;
+            pids[i] = page_of(p.bt, p.cache.n_pages, x.u.b, block);
+            starts[i] = pids[i] < 0 ? 0 : block * PAGE;
+        } else {
+            pids[i] = x.u.common && at >= shared_pages(p) ? -1 : page_of(p.bt, p.cache.n_pages, x.u.b, x.u.base + at);
+        }
+    }
     __syncthreads();
+    if constexpr (kLists<P>)
+        v1 = listed_end<PPV>(pids, v0, np, lane);
+    // first key of the range's page i
+    auto start = [&](int i) __attribute__((always_inline)) {
+        if constexpr (kLists<P>)
+            return i < np ? starts[i] : 0;
+        else
+            return (x.u.base + v0 * PPV + i) * PAGE;
+    };
 
     const size_t block_bytes = (size_t)PAGE * D;
     uint8_t* const kst = lds + w * 2 * STAGE;
@@ -148,7 +326,7 @@ __global__ void __launch_bounds__(256, 1) cache_fwd_kernel(FwdParams p)
     auto buffer = [&](const uint8_t* base, int v, int sub) __attribute__((always_inline)) {
         const int i = (v - v0) * PPV + sub;
         const int pid = v < v1 ? __builtin_amdgcn_readfirstlane(pids[i]) : -1;
-        const int left = min(max(seen - (v * kVisit + sub * PAGE), 0), PAGE);
+        const int left = min(max(seen - (kLists<P> ? __builtin_amdgcn_readfirstlane(start(i)) : start(i)), 0), PAGE);
         return bytes_buffer(base + ((size_t)(pid < 0 ? 0 : pid) * p.cache.Hkv + hk) * block_bytes, pid < 0 ? 0 : left * D);
     };
     auto issue_k = [&](int v) __attribute__((always_inline)) {
@@ -182,7 +360,7 @@ __global__ void __launch_bounds__(256, 1) cache_fwd_kernel(FwdParams p)
     for (int c = 0; c < (kMaxChunk * PPV + 255) / 256; ++c) {
         const int i = tid + 256 * c;
         // (a page behind the last key that a row sees may hold anything)
-        const int pid = i < np && (v0 * PPV + i) * PAGE < seen ? pids[i] : -1;
+        const int pid = i < np && start(i) < seen ? pids[i] : -1;
         const size_t at = (size_t)(pid < 0 ? 0 : pid) * p.cache.Hkv + hk;
         kb0[c] = pid < 0 ? 127 : p.cache.ks[at];
         vb0[c] = pid < 0 ? 127 : p.cache.vs[at];
@@ -249,18 +427,19 @@ __global__ void __launch_bounds__(256, 1) cache_fwd_kernel(FwdParams p)
             f32x4 acc = {};
 #pragma unroll
             for (int i = 0; i < KP; ++i) {
-                const i32x4 x = raw[kt][i];
-                acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen((uint32_t)x[0], (uint32_t)x[1]), qf[2 * i], acc, 0, 0, 0);
-                acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen((uint32_t)x[2], (uint32_t)x[3]), qf[2 * i + 1], acc, 0, 0, 0);
+                const i32x4 k = raw[kt][i];
+                acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen((uint32_t)k[0], (uint32_t)k[1]), qf[2 * i], acc, 0, 0, 0);
+                acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen((uint32_t)k[2], (uint32_t)k[3]), qf[2 * i + 1], acc, 0, 0, 0);
             }
             sc[kt] = acc;
         }
         // ---- keys the row does not see ----
-        const int t0 = v * kVisit;
-        if (t0 + kVisit - 1 > pos_min || !there[0] || !there[1]) {
+        const int t0[2] = {start(pi), PPV == 2 ? start(pi + 1) : start(pi) + 64};    // of its halves
+        const int t_end = kLists<P> ? max(t0[0], t0[1]) + 64 : t0[1] + 64;
+        if (t_end - 1 > pos_min || !there[0] || !there[1]) {
 #pragma unroll
             for (int kt = 0; kt < KT; ++kt) {
-                const int lim = there[kt / 4] ? pos - t0 - 64 * (kt / 4) - 16 * g : -1;
+                const int lim = there[kt / 4] ? pos - t0[kt / 4] - 16 * g : -1;
 #pragma unroll
                 for (int r = 0; r < 4; ++r)
                     sc[kt][r] = 4 * (kt % 4) + r <= lim ? sc[kt][r] : -INFINITY;
@@ -345,11 +524,11 @@ __global__ void __launch_bounds__(256, 1) cache_fwd_kernel(FwdParams p)
         };
         // Where some rows see keys that others do not, a NaN of V must not reach the others
         // by way of 0 times NaN: it makes NaN of the sums of the rows that see it, and goes.
-        if (t0 + kVisit - 1 > pos_min && pos_min + 1 < seen && holds_nan(vst, STAGE, lane)) {
+        if (t_end - 1 > pos_min && pos_min + 1 < seen && holds_nan(vst, STAGE, lane)) {
             i32x8 see;
 #pragma unroll
             for (int kt = 0; kt < KT; ++kt)
-                see[kt] = ones(pos - t0 - 64 * (kt / 4) - 16 * g - 4 * (kt % 4) + 1);
+                see[kt] = ones(pos - t0[kt / 4] - 16 * g - 4 * (kt % 4) + 1);
 #pragma unroll
             for (int dt = 0; dt < DT; ++dt) {
                 const f32x4 hits = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(nan_ones(v_read(dt)), see, f32x4{}, 0, 0, 0, 127, 0, 127);
@@ -387,17 +566,15 @@ __global__ void __launch_bounds__(256, 1) cache_fwd_kernel(FwdParams p)
     float* const mw = reinterpret_cast<float*>(lds) + (w * TR + n) * MS;
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) {
-        f32x4 x;
+        f32x4 y;
 #pragma unroll
         for (int r = 0; r < 4; ++r)
-            x[r] = __builtin_amdgcn_ldexpf(o[dt][r], down);
-        *reinterpret_cast<f32x4*>(mw + 16 * dt + 4 * g) = x;
+            y[r] = __builtin_amdgcn_ldexpf(o[dt][r], down);
+        *reinterpret_cast<f32x4*>(mw + 16 * dt + 4 * g) = y;
     }
     __syncthreads();
     const float* mb = reinterpret_cast<const float*>(lds);
-    const size_t stride = (size_t)TR * (D + 2);
-    float* const part = whole ? nullptr
-                              : p.ws + ((((size_t)b * p.cache.Hkv + hk) * p.tiles + tile) * p.ranges + range) * stride;
+    float* const part = x.whole ? nullptr : part_of(p, x, TR, D);
     for (int e = tid; e < TR * D / 4; e += 256) {
         const int rr = e / (D / 4), piece = e % (D / 4);
         if (row0 + rr >= rows)
@@ -418,7 +595,7 @@ __global__ void __launch_bounds__(256, 1) cache_fwd_kernel(FwdParams p)
             for (int c = 0; c < 4; ++c)
                 acc[c] += t[c];
         }
-        if (whole) {
+        if (x.whole) {
             write_row<D>(p, s, hk, row0 + rr, piece, acc, l, 1.f / l, mm);
         } else {
             *reinterpret_cast<f32x4*>(part + rr * D + 4 * piece) = acc;

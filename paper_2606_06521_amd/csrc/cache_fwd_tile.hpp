@@ -24,8 +24,8 @@ namespace attn {
 constexpr int kTileRows = 128;
 constexpr int kTileChunk = 512;     // visits of a range
 
-template <int D, int PAGE, bool E4M3>
-__global__ void __launch_bounds__(256, 2) cache_fwd_tile_kernel(FwdParams p)
+template <int D, int PAGE, bool E4M3, class P>
+__global__ void __launch_bounds__(256, 2) cache_fwd_tile_kernel(P p)
 {
     constexpr int NW = 4, TR = kTileRows;
     constexpr int PPV = kVisit / PAGE;          // pages per visit
@@ -42,34 +42,64 @@ __global__ void __launch_bounds__(256, 2) cache_fwd_tile_kernel(FwdParams p)
     __shared__ int pids[kTileChunk * PPV];
     __shared__ uint8_t kbyte[kTileChunk * PPV], vbyte[kTileChunk * PPV];
 
-    int tile, range, hk, b;
-    if (!workgroup_of(p, tile, range, hk, b))
+    __shared__ int starts[kLists<P> ? kTileChunk * PPV : 1];     // first keys of a list's pages
+    __shared__ int row_last[kShared<P> ? TR : 1];
+
+    Share x;
+    if (!share_of(p, TR, PAGE, x))
         return;
-    const Seq s = uniform(sequence(p.bt, b, p.max_len));
-    const int rows = s.n * p.gr.G;
-    const int row0 = tile * TR;
-    if (row0 >= rows)
-        return;
-    const int visits = tile_visits(p, s, tile, TR);
-    const int v0 = range * p.chunk, v1 = min(v0 + p.chunk, visits);
-    if (v0 >= v1 && range > 0)
-        return;
-    const bool whole = visits <= p.chunk;
+    const Seq& s = x.u.s;
+    const int rows = s.n * p.gr.G, row0 = x.tile * TR, hk = x.u.hk;
+    const int v0 = x.v0;
+    int v1 = x.v1;
 
     const int tid = threadIdx.x, lane = tid & 63;
     const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int n = lane & 31, h = lane >> 5;
     const int wrow0 = row0 + 32 * w;                    // the wave's first row
     const int row = wrow0 + n;
-    const int pos = row < rows ? last_key(s.pos0 + p.gr.token(row), p.causal, s.len) : -1;
-    const int pos_min = last_key(s.pos0 + p.gr.token(wrow0), p.causal, s.len);
-    const int tile_pos_min = last_key(s.pos0 + p.gr.token(row0), p.causal, s.len);
-    const int seen = p.causal ? min(max(s.pos0 + p.gr.token(min(row0 + TR, rows) - 1) + 1, 0), s.len) : s.len;
+    int pos = row < rows ? last_key(s.pos0 + p.gr.token(row), p.causal, s.len) : -1;
+    int pos_min = last_key(s.pos0 + p.gr.token(wrow0), p.causal, s.len);
+    int tile_pos_min = last_key(s.pos0 + p.gr.token(row0), p.causal, s.len), seen = tile_seen(p, s, x.tile, TR);
+    if constexpr (kShared<P>)
+        if (x.u.common) {
+            common_last(p, row0, TR, row_last);
+            pos = row_last[32 * w + n];
+            int lo = pos, all = min(row_last[lane], row_last[lane + 64]), hi = max(row_last[lane], row_last[lane + 64]);
+#pragma unroll
+            for (int off = 16; off > 0; off >>= 1)
+                lo = min(lo, __shfl_xor(lo, off, 64));
+#pragma unroll
+            for (int off = 32; off > 0; off >>= 1) {
+                all = min(all, __shfl_xor(all, off, 64));
+                hi = max(hi, __shfl_xor(hi, off, 64));
+            }
+            pos_min = __builtin_amdgcn_readfirstlane(lo);
+            tile_pos_min = __builtin_amdgcn_readfirstlane(all);
+            seen = min(p.shared * PAGE, min(__builtin_amdgcn_readfirstlane(hi), p.max_len - 1) + 1);
+        }
 
     const int np = max(v1 - v0, 0) * PPV;
-    for (int i = tid; i < np; i += 256)
-        pids[i] = page_of(p.bt, p.cache.n_pages, b, v0 * PPV + i);
+    for (int i = tid; i < np; i += 256) {
+        const int at = v0 * PPV + i;
+        if constexpr (kLists<P>) {
+            const int block = at < p.take ? x.u.list[at] : -1;
+            pids[i] = page_of(p.bt, p.cache.n_pages, x.u.b, block);
+            starts[i] = pids[i] < 0 ? 0 : block * PAGE;
+        } else {
+            pids[i] = x.u.common && at >= shared_pages(p) ? -1 : page_of(p.bt, p.cache.n_pages, x.u.b, x.u.base + at);
+        }
+    }
     __syncthreads();
+    if constexpr (kLists<P>)
+        v1 = listed_end<PPV>(pids, v0, np, lane);
+    // first key of the range's page i
+    auto start = [&](int i) __attribute__((always_inline)) {
+        if constexpr (kLists<P>)
+            return i < np ? starts[i] : 0;
+        else
+            return (x.u.base + v0 * PPV + i) * PAGE;
+    };
 
     const size_t block_bytes = (size_t)PAGE * D;
     const int lr = lane / CPR, lc = lane % CPR;
@@ -82,8 +112,10 @@ __global__ void __launch_bounds__(256, 2) cache_fwd_tile_kernel(FwdParams p)
     // the wave's rows 32 w .. 32 w + 31 of the visit's K and V, into stage pair v & 1
     auto issue = [&](int v) __attribute__((always_inline)) {
         const int sub = PPV == 2 ? w >> 1 : 0;
-        const int pid = v < v1 ? __builtin_amdgcn_readfirstlane(pids[(v - v0) * PPV + sub]) : -1;
-        const int left = pid < 0 ? 0 : min(max(seen - (v * kVisit + sub * PAGE), 0), PAGE) * D;
+        const int i = (v - v0) * PPV + sub;
+        const int pid = v < v1 ? __builtin_amdgcn_readfirstlane(pids[i]) : -1;
+        const int from = kLists<P> ? __builtin_amdgcn_readfirstlane(start(i)) : start(i);
+        const int left = pid < 0 ? 0 : min(max(seen - from, 0), PAGE) * D;
         const size_t at = ((size_t)(pid < 0 ? 0 : pid) * p.cache.Hkv + hk) * block_bytes;
         const i32x4 kb = bytes_buffer(p.cache.k + at, left), vb = bytes_buffer(p.cache.v + at, left);
         const uint8_t* const st = lds + (v & 1) * 2 * STAGE + w * (32 * D);
@@ -99,7 +131,7 @@ __global__ void __launch_bounds__(256, 2) cache_fwd_tile_kernel(FwdParams p)
     issue(v0);
     for (int i = tid; i < np; i += 256) {
         // (a page behind the last key that a row sees may hold anything)
-        const int pid = (v0 * PPV + i) * PAGE < seen ? pids[i] : -1;
+        const int pid = start(i) < seen ? pids[i] : -1;
         const size_t at = (size_t)(pid < 0 ? 0 : pid) * p.cache.Hkv + hk;
         kbyte[i] = pid < 0 ? 127 : p.cache.ks[at];
         vbyte[i] = pid < 0 ? 127 : p.cache.vs[at];
@@ -137,7 +169,9 @@ __global__ void __launch_bounds__(256, 2) cache_fwd_tile_kernel(FwdParams p)
         issue(v + 1);
         uint8_t* const kst = lds + (v & 1) * 2 * STAGE;
         uint8_t* const vst = kst + STAGE;
-        const int t0 = v * kVisit;
+        const int pi = (v - v0) * PPV;
+        const int t0[2] = {start(pi), PPV == 2 ? start(pi + 1) : start(pi) + 64};    // of its halves
+        const int t_end = kLists<P> ? max(t0[0], t0[1]) + 64 : t0[1] + 64;
         auto v_read = [&](int js, int dt) __attribute__((always_inline)) {
             i32x8 av;
 #pragma unroll
@@ -151,13 +185,13 @@ __global__ void __launch_bounds__(256, 2) cache_fwd_tile_kernel(FwdParams p)
         // Where some rows see keys that others do not, a NaN of V must not reach the others
         // by way of 0 times NaN: it makes NaN of the sums of the rows that see it, and goes
         // (every wave looks at the whole stage, so all take the same way).
-        if (t0 + kVisit - 1 > tile_pos_min && holds_nan(vst, STAGE, lane)) {
+        if (t_end - 1 > tile_pos_min && holds_nan(vst, STAGE, lane)) {
 #pragma unroll
             for (int js = 0; js < KT / 2; ++js) {
                 i32x8 see;
 #pragma unroll
                 for (int q = 0; q < 8; ++q)
-                    see[q] = ones(pos - t0 - 64 * js - 32 * (q / 4) - 16 * h - 4 * (q % 4) + 1);
+                    see[q] = ones(pos - t0[js] - 32 * (q / 4) - 16 * h - 4 * (q % 4) + 1);
 #pragma unroll
                 for (int dt = 0; dt < DT; ++dt) {
                     const f32x16 hits = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(nan_ones(v_read(js, dt)), see, f32x16{}, 0, 0, 0, 127, 0, 127);
@@ -172,7 +206,6 @@ __global__ void __launch_bounds__(256, 2) cache_fwd_tile_kernel(FwdParams p)
         }
         if (wrow0 >= rows)
             continue;
-        const int pi = (v - v0) * PPV;
         float c[2] = {score_factor(p.c, kbyte[pi]), score_factor(p.c, kbyte[pi + PPV - 1])};
         const int lent[2] = {lent_scale(vbyte[pi]), lent_scale(vbyte[pi + PPV - 1])};
         const int sa[2] = {vbyte[pi] - lent[0], vbyte[pi + PPV - 1] - lent[1]};
@@ -185,18 +218,18 @@ __global__ void __launch_bounds__(256, 2) cache_fwd_tile_kernel(FwdParams p)
             f32x16 acc = {};
 #pragma unroll
             for (int i = 0; i < KP; ++i) {
-                const i32x4 x = *reinterpret_cast<const i32x4*>(kst + r * D + 16 * ((2 * i + h) ^ kswz(r)));
-                acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(widen((uint32_t)x[0], (uint32_t)x[1]), qf[2 * i], acc, 0, 0, 0);
-                acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(widen((uint32_t)x[2], (uint32_t)x[3]), qf[2 * i + 1], acc, 0, 0, 0);
+                const i32x4 k = *reinterpret_cast<const i32x4*>(kst + r * D + 16 * ((2 * i + h) ^ kswz(r)));
+                acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(widen((uint32_t)k[0], (uint32_t)k[1]), qf[2 * i], acc, 0, 0, 0);
+                acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(widen((uint32_t)k[2], (uint32_t)k[3]), qf[2 * i + 1], acc, 0, 0, 0);
             }
             sc[kt] = acc;
         }
         __builtin_amdgcn_s_setprio(0);
         // ---- keys the row does not see ----
-        if (t0 + kVisit - 1 > pos_min || !there[0] || !there[1]) {
+        if (t_end - 1 > pos_min || !there[0] || !there[1]) {
 #pragma unroll
             for (int kt = 0; kt < KT; ++kt) {
-                const int lim = there[kt / 2] ? pos - t0 - 32 * kt - 16 * h : -1;
+                const int lim = there[kt / 2] ? pos - t0[kt / 2] - 32 * (kt % 2) - 16 * h : -1;
 #pragma unroll
                 for (int r = 0; r < 16; ++r)
                     sc[kt][r] = r <= lim ? sc[kt][r] : -INFINITY;
@@ -279,7 +312,7 @@ __global__ void __launch_bounds__(256, 2) cache_fwd_tile_kernel(FwdParams p)
     if (row >= rows)
         return;
     const float l = halves_sum(ell);
-    if (whole) {
+    if (x.whole) {
         const float inv = 1.f / l;
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt)
@@ -289,7 +322,7 @@ __global__ void __launch_bounds__(256, 2) cache_fwd_tile_kernel(FwdParams p)
                              l, inv, ref);
         return;
     }
-    float* const part = p.ws + ((((size_t)b * p.cache.Hkv + hk) * p.tiles + tile) * p.ranges + range) * ((size_t)TR * (D + 2));
+    float* const part = part_of(p, x, TR, D);
     const int rr = 32 * w + n;
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt)

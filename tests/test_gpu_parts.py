@@ -1,0 +1,517 @@
+"""Attention over parts of the KV cache on the GPU against 64-bit results (tests/parts_ref.py): bounds
+of pages, choice of pages, attention over lists and behind a shared prefix, and a run of them."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from tests import cache_ref as R
+from tests import parts_ref as P
+from tests.gpu_helpers import log
+from tests.test_gpu_cache import cu_of, dev, dev_cache, within
+
+pytestmark = pytest.mark.gpu
+
+E4M3 = torch.float8_e4m3fn
+
+
+@pytest.fixture(scope="module")
+def A():
+    from paper_2606_06521_amd import attn_fp8
+    return attn_fp8
+
+
+def n_cu():
+    return torch.cuda.get_device_properties(0).multi_processor_count
+
+
+def dev_bounds(x):
+    """float64 E4M3 values -> codes on the GPU."""
+    return dev(R.encode(x)).view(E4M3)
+
+
+def values(t):
+    return R.decode(t.view(torch.uint8).cpu().numpy())
+
+
+# ---- bounds ----
+
+CASES_BOUNDS = [([1], [1]), ([64, 65, 129, 300], [1, 1, 1, 1]), ([200, 129, 64, 0], [3, 129, 64, 0]), ([700, 257], [700, 130]),
+                ([60, 10], [70, 10])]
+
+
+@pytest.mark.parametrize("d,page", [(64, 64), (64, 128), (128, 64), (128, 128)])
+@pytest.mark.parametrize("case", range(len(CASES_BOUNDS)))
+def test_bounds(A, case, d, page):
+    lens, new = CASES_BOUNDS[case]
+    log(f"bounds {lens} {new} d={d} page={page}")
+    rng = np.random.default_rng(case * 5 + d + page)
+    c = R.make_cache(rng, len(lens), 3, page, d, lens)
+    # any codes, NaN and both zeros among them
+    c.k = rng.integers(0, 256, c.k.shape, dtype=np.uint8)
+    given = R.decode(rng.integers(0, 120, (c.n_pages, 3, 2, d), dtype=np.uint8))
+    got = dev_bounds(given)
+    r = A.cache_bounds(dev_cache(A, c), dev(c.pages), dev(c.lens), got, cu=dev(cu_of(new)), max_q=max(new))
+    assert r is got
+    want = P.bounds(c, given, cu=cu_of(new), max_q=max(new))
+    assert np.array_equal(values(got), want)
+    assert not (got.view(torch.uint8).cpu().numpy() == 0x80).any()
+
+
+@pytest.mark.parametrize("max_q", [None, 1, 5, 128, 129])
+def test_bounds_of_the_last_tokens(A, max_q):
+    rng = np.random.default_rng(3)
+    lens = [300, 2, 128, 0, 257]
+    c = R.make_cache(rng, 5, 2, 64, 128, lens)
+    given = np.full((c.n_pages, 2, 2, 128), 1.5)
+    got = dev_bounds(given)
+    A.cache_bounds(dev_cache(A, c), dev(c.pages), dev(c.lens), got, max_q=max_q)
+    # (a sequence shorter than max_q begins before position 0)
+    n = c.pages.shape[1] * 64 if max_q is None else max_q
+    assert np.array_equal(values(got), P.bounds(c, given, max_q=n))
+
+
+def test_bounds_of_small_and_large_codes(A):
+    """Every code by itself: rounded outwards to halves."""
+    c = R.make_cache(np.random.default_rng(4), 1, 2, 64, 128, [64])
+    codes = np.array([x for x in range(256) if x & 127 != 127], dtype=np.uint8)
+    c.k[c.pages[0, 0]] = codes[:128][None, None]
+    c.k[c.pages[0, 0], 1] = codes[126:][None]
+    got = A.key_bounds(c.n_pages, 2, 128)
+    A.cache_bounds(dev_cache(A, c), dev(c.pages), dev(c.lens), got)
+    x = R.decode(np.stack([codes[:128], codes[126:]]))
+    v = values(got)[c.pages[0, 0]]
+    assert np.array_equal(v[:, 0], np.floor(2 * x) / 2) and np.array_equal(v[:, 1], np.ceil(2 * x) / 2)
+
+
+def test_bounds_leave_out_what_has_no_place(A):
+    rng = np.random.default_rng(5)
+    c = R.make_cache(rng, 4, 2, 64, 64, [200, 100, 64, 90])
+    c.pages[0, 1], c.pages[1, 0], c.pages[2, 0] = -1, c.n_pages, 1 << 30
+    c.lens = np.array([200, 100, -5, 1 << 30], dtype=np.int32)
+    given = np.full((c.n_pages, 2, 2, 64), 2.0)
+    got = dev_bounds(given)
+    A.cache_bounds(dev_cache(A, c), dev(c.pages), dev(c.lens), got)
+    n = c.pages.shape[1] * 64
+    c.lens = np.array([200, 100, 0, 1 << 30], dtype=np.int32)
+    assert np.array_equal(values(got), P.bounds(c, given, max_q=n))
+
+
+# ---- choice ----
+
+def choose(A, c, q, G, take, kind="bf16", bnds=None, new=None, check=True, **kw):
+    """The lists of the call, equal to those of the definition."""
+    cu = None if new is None else cu_of(new)
+    max_q = q.shape[0] // len(c.lens) if new is None else max(max(new), 1)
+    bnds = P.bounds(c, np.zeros((c.n_pages, c.Hkv, 2, c.d)), max_q=c.pages.shape[1] * c.page) if bnds is None else bnds
+    got = A.cache_select(R.torch_q(q, kind).cuda(), dev_cache(A, c), dev(c.pages), dev(c.lens), dev_bounds(bnds), take,
+                         cu=None if cu is None else dev(cu), max_q=max_q, **kw).cpu().numpy()
+    if check:
+        want = P.select(c, q, bnds, G, take, cu=cu, max_q=max_q, **kw)
+        bad = np.argwhere((got != want).any(-1))
+        assert bad.size == 0, (bad[:3].tolist(), got[tuple(bad[0])].tolist(), want[tuple(bad[0])].tolist())
+    return got
+
+
+def any_queries(rng, T, Hq, d, kind):
+    """Queries of the type's whole precision, rows of different sizes."""
+    x = rng.standard_normal((T, Hq, d)) * np.exp2(rng.integers(-3, 3, (T, Hq, 1)))
+    return R.torch_q(x, kind).double().numpy()
+
+
+@pytest.mark.parametrize("kind", ["bf16", "e4m3"])
+@pytest.mark.parametrize("d,page", [(64, 64), (64, 128), (128, 64), (128, 128)])
+@pytest.mark.parametrize("lens,take", [([1], 1), ([127, 128, 129, 0], 2), ([5000, 31, 700], 5), ([2100, 2048, 2049], 16)])
+def test_select_for_single_tokens(A, lens, take, d, page, kind):
+    log(f"select {lens} take={take} d={d} page={page} {kind}")
+    rng = np.random.default_rng(sum(lens) + d)
+    c = R.make_cache(rng, len(lens), 2, page, d, lens)
+    choose(A, c, any_queries(rng, len(lens), 8, d, kind), 4, take, kind, n_first=min(1, take - 1), n_last=1)
+
+
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("d,page,G,run", [(64, 128, 1, 16), (64, 64, 3, 7), (128, 64, 8, 32), (128, 128, 4, 64)])
+@pytest.mark.parametrize("lens,new,take", [([40], [40], 1), ([900, 429, 5], [17, 129, 5], 3), ([1500, 0, 1260, 128], [1, 0, 33, 100], 4),
+                                           ([3000, 190], [200, 3], 9)])
+def test_select_for_runs(A, lens, new, take, d, page, G, run, causal):
+    log(f"select {lens} {new} take={take} d={d} page={page} G={G} run={run} causal={causal}")
+    rng = np.random.default_rng(sum(lens) + d + G)
+    c = R.make_cache(rng, len(lens), 2, page, d, lens)
+    q = any_queries(rng, sum(new) + 2, G * 2, d, "bf16")
+    choose(A, c, q, G, take, new=new, run=run, causal=causal, n_first=take // 3, n_last=take // 4)
+
+
+@pytest.mark.parametrize("n,page,take", [(70000, 64, 100), (300000, 64, 1000), (140000, 128, 7), (1 << 20, 64, 16384), (1 << 20, 64, 300)])
+def test_select_among_many(A, n, page, take):
+    """Up to 16384 pages; all of them one page of the cache but for some."""
+    log(f"select among many n={n} page={page} take={take}")
+    rng = np.random.default_rng(n)
+    c = R.make_cache(rng, 1, 1, page, 64, [page * 40])
+    W = n // page
+    c.pages = np.concatenate([c.pages, rng.choice(c.pages[0], (1, W - 40))], 1).astype(np.int32)
+    c.lens = np.array([n], dtype=np.int32)
+    got = choose(A, c, any_queries(rng, 1, 4, 64, "bf16"), 4, take)
+    assert (got >= 0).sum() == min(take, W)
+
+
+def test_select_takes_the_earlier_of_equals(A):
+    rng = np.random.default_rng(8)
+    c = R.make_cache(rng, 2, 2, 64, 64, [64 * 30, 64 * 30])
+    c.pages[0] = c.pages[0, 3]
+    c.pages[1, 5:25] = c.pages[1, 7]
+    q = any_queries(rng, 2, 4, 64, "bf16")
+    for take in (1, 3, 11, 29, 30, 40):
+        got = choose(A, c, q, 2, take, n_first=0, n_last=1)
+        m = min(take, 30)
+        assert np.array_equal(got[0, 0, 0, :m], [*range(m - 1), 29])
+
+
+def test_select_sums_are_exact(A):
+    """Sums next to 2^24 halves: the largest codes and 127s, one channel a half apart."""
+    d, page = 128, 64
+    c = R.make_cache(np.random.default_rng(9), 1, 1, page, d, [page * 12])
+    b = np.zeros((c.n_pages, 1, 2, d))
+    c.ks[:] = 127
+    for j in range(12):
+        b[c.pages[0, j], 0, 1] = 448.0
+        b[c.pages[0, j], 0, 1, 5] = 3.5 if j in (4, 9) else 3.0        # 127 a half apart in a sum of 7.2 million
+        b[c.pages[0, j], 0, 0] = -448.0
+        b[c.pages[0, j], 0, 1, 6] = 1.5 if j == 6 else 1.0
+    q = np.full((1, 2, d), 127.0)
+    q[0, 0, 6] = 1.0                                                   # one half of the smallest step
+    q[0, 1] = 0.0
+    choose(A, c, q, 2, 3, bnds=b, n_first=0, n_last=0)
+    q[0, 0, 5] = 1.0                                                   # (both channels as small as they get)
+    choose(A, c, q, 2, 3, bnds=b, n_first=0, n_last=0)
+    q[0, 0] = np.where(np.arange(d) % 2, 127.0, -127.0)
+    choose(A, c, q, 2, 5, bnds=b, n_first=0, n_last=0)
+    rng = np.random.default_rng(10)
+    for _ in range(8):
+        lo = R.decode(rng.integers(0, 127, (c.n_pages, 1, d), dtype=np.uint8) | 128)
+        hi = R.decode(rng.integers(0, 127, (c.n_pages, 1, d), dtype=np.uint8))
+        b = np.stack((np.floor(2 * lo) / 2, np.ceil(2 * hi) / 2), 2)
+        q = rng.integers(-127, 128, (1, 2, d)).astype(np.float64)
+        q[:, :, 0] = 127
+        choose(A, c, q, 2, 4, bnds=b, n_first=0, n_last=0)
+
+
+def test_select_far_scales_and_queries_that_are_not_finite(A):
+    rng = np.random.default_rng(12)
+    c = R.make_cache(rng, 3, 2, 64, 64, [64 * 9, 64 * 7 + 5, 64 * 8])
+    c.ks = rng.integers(0, 255, c.ks.shape).astype(np.uint8)
+    q = any_queries(rng, 3 * 4, 4, 64, "bf16") * np.exp2(rng.integers(-100, 100, (12, 4, 1)).astype(np.float64))
+    q = R.torch_q(q, "bf16").double().numpy()
+    q[0, 1, 5], q[5, 0, 0], q[5, 1, 63] = np.inf, np.nan, -np.inf
+    q[8:] = np.nan                                          # no row of the last sequence takes part
+    got = choose(A, c, q, 2, 3, run=2)
+    assert np.array_equal(got[2, 0, 0], [0, 1, 7])
+    q[:] = 0.0
+    choose(A, c, q, 2, 4, run=4)
+    q[:] = 2.0 ** -133                                      # bf16's least number
+    choose(A, c, q, 2, 4, run=4)
+
+
+def test_select_pages_that_are_none_and_lengths(A):
+    rng = np.random.default_rng(13)
+    c = R.make_cache(rng, 4, 2, 64, 64, [600, 300, 200, 640])
+    c.pages[0, 2], c.pages[0, 9], c.pages[1, :] = -1, c.n_pages, -3
+    q = any_queries(rng, 4, 4, 64, "bf16")
+    got = choose(A, c, q, 2, 9)
+    assert (got[1] == -1).all()
+    choose(A, c, q, 2, 3, max_len=333)
+    c.lens = np.array([-3, 1 << 20, 0, 641], dtype=np.int32)
+    choose(A, c, q, 2, 3, n_first=0)
+    # tokens before position 0 see nothing, those beyond max_q have no list
+    c.lens = np.array([5, 40, 70, 300], dtype=np.int32)
+    q = any_queries(rng, 40, 4, 64, "bf16")
+    choose(A, c, q, 2, 3, new=[10, 10, 10, 10], run=4)
+
+
+# ---- attention over lists ----
+
+def over_blocks(A, c, q, blocks, G, kind="bf16", new=None, run=1, check=True, out_dtype=torch.float32, max_q=None, **kw):
+    T, Hq, d = q.shape
+    cu = None if new is None else cu_of(new)
+    max_q = (T // len(c.lens) if new is None else max(max(new), 1)) if max_q is None else max_q
+    out = torch.full((T, Hq, d), 7.0, dtype=out_dtype, device="cuda")
+    lse = torch.full((T, Hq), 7.0, device="cuda")
+    A.cache_fwd_blocks(R.torch_q(q, kind).cuda(), dev_cache(A, c), dev(c.pages), dev(c.lens), dev(blocks),
+                       cu=None if cu is None else dev(cu), max_q=max_q, run=run, out=out, lse=lse, **kw)
+    o, l = out.cpu().double().numpy(), lse.cpu().double().numpy()
+    if check:
+        compare(o, l, P.attention(c, q, blocks, G, run=run, cu=cu, max_q=max_q, **kw), out_dtype)
+    return o, l
+
+
+def compare(o, l, want, out_dtype):
+    w, wl, bound, lb = want
+    left = np.isnan(bound)
+    assert np.all(o[left] == 7.0) and np.all(l[np.isnan(lb)] == 7.0)
+    assert np.array_equal(np.isnan(o[~left]), np.isnan(w[~left]))
+    fine = ~left & ~np.isnan(w)
+    within(o[fine], w[fine], bound[fine] + (np.abs(w[fine]) * 2.0 ** -8 if out_dtype == torch.bfloat16 else 0.0))
+    there = ~np.isnan(lb)
+    assert np.array_equal(np.isinf(l[there]), np.isinf(wl[there])) and np.array_equal(np.isnan(l[there]), np.isnan(wl[there]))
+    there &= np.isfinite(wl)
+    if there.any():
+        within(l[there], wl[there], lb[there])
+
+
+def random_lists(rng, c, runs, take):
+    """Blocks in any order, some twice, some none or outside the table."""
+    W = c.pages.shape[1]
+    x = rng.integers(0, max(-(-int(c.lens.max()) // c.page), 1), (len(c.lens), runs, c.Hkv, take))
+    odd = rng.random(x.shape)
+    x = np.where(odd < 0.1, -1, np.where(odd < 0.15, W + rng.integers(0, 1 << 30, x.shape), x))
+    return np.where((odd > 0.15) & (odd < 0.18), -(1 << 31), x).astype(np.int32)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "e4m3"])
+@pytest.mark.parametrize("d,page", [(64, 64), (64, 128), (128, 64), (128, 128)])
+@pytest.mark.parametrize("lens,take", [([1], 1), ([127, 128, 129, 0], 3), ([2000, 31, 700], 7), ([4000, 65, 3000, 33], 20)])
+def test_blocks_for_single_tokens(A, lens, take, d, page, kind):
+    log(f"blocks {lens} take={take} d={d} page={page} {kind}")
+    rng = np.random.default_rng(len(lens) + d + take)
+    c = R.make_cache(rng, len(lens), 2, page, d, lens)
+    q = R.make_queries(rng, len(lens), 8, d)
+    over_blocks(A, c, q, random_lists(rng, c, 1, take), 4, kind, out_dtype=torch.bfloat16 if take == 7 else torch.float32)
+
+
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("d,page,G,run,kind", [(64, 128, 1, 16, "bf16"), (64, 64, 3, 7, "e4m3"), (128, 64, 8, 16, "e4m3"),
+                                               (128, 128, 4, 64, "bf16"), (128, 64, 4, 40, "bf16"), (64, 64, 8, 300, "bf16"),
+                                               (64, 128, 4, 33, "e4m3"), (128, 128, 4, 32, "e4m3")])
+@pytest.mark.parametrize("lens,new,take", [([40], [40], 2), ([900, 429, 5], [17, 129, 5], 4), ([1500, 0, 1260, 128], [1, 0, 33, 100], 6),
+                                           ([1000, 290], [200, 3], 9)])
+def test_blocks_for_runs(A, lens, new, take, d, page, G, run, kind, causal):
+    log(f"blocks {lens} {new} take={take} d={d} page={page} G={G} run={run} {kind} causal={causal}")
+    rng = np.random.default_rng(sum(lens) + d + G)
+    c = R.make_cache(rng, len(lens), 2, page, d, lens)
+    q = R.make_queries(rng, sum(new) + 2, G * 2, d)       # two rows behind the last sequence
+    lists = random_lists(rng, c, -(-max(new) // run), take)
+    over_blocks(A, c, q, lists, G, kind, new=new, run=run, causal=causal)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "e4m3"])
+@pytest.mark.parametrize("G,take,page,d", [(4, 200, 64, 64), (4, 40, 128, 128), (4, 150, 64, 128), (8, 300, 128, 64)])
+@pytest.mark.parametrize("rows", [16, 128])
+def test_blocks_in_ranges(A, rows, G, take, page, d, kind):
+    """Lists that are split, some of them short, one empty; a loose bound on the tokens of a run makes tall tiles."""
+    run = next(r for r in (1, 50, 200, 400, 800, 1600, 3200) if P.blocks_plan(4, G, r, take, page, d, n_cu()).rows == rows)
+    plan = P.blocks_plan(4, G, run, take, page, d, n_cu())
+    assert plan.rows == rows and plan.ranges > 1
+    log(f"blocks in ranges rows={rows} G={G} run={run} take={take} page={page} d={d} {kind} ranges={plan.ranges}")
+    rng = np.random.default_rng(take)
+    c = R.make_cache(rng, 2, 2, page, d, [1700, 900])
+    new = [min(run, 40), min(run, 37)]
+    blocks = random_lists(rng, c, 1, take)
+    blocks[1, 0, 0] = -1
+    blocks[0, 0, 1, 3:] = -1
+    over_blocks(A, c, R.make_queries(rng, sum(new), G * 2, d), blocks, G, kind, new=new, run=run, max_q=run)
+
+
+@pytest.mark.parametrize("d,page,G,run", [(64, 64, 4, 1), (128, 128, 4, 1), (128, 64, 8, 40), (64, 128, 4, 100)])
+def test_blocks_all_listed_is_the_whole_cache(A, d, page, G, run):
+    rng = np.random.default_rng(21)
+    lens = [1000, 130]
+    new = [min(run, 100), 1]
+    c = R.make_cache(rng, 2, 2, page, d, lens)
+    W = c.pages.shape[1]
+    blocks = np.broadcast_to(np.arange(W, dtype=np.int32), (2, 1, 2, W))
+    q = R.make_queries(rng, sum(new), 2 * G, d)
+    o, l = over_blocks(A, c, q, np.ascontiguousarray(blocks), G, new=new, run=run)
+    a, b = A.cache_fwd(R.torch_q(q, "bf16").cuda(), dev_cache(A, c), dev(c.pages), dev(c.lens), cu=dev(cu_of(new)), max_q=max(new),
+                       out_dtype=torch.float32)
+    # FP32 sums of another order, the core's groups of eight as they are
+    a, b = a.cpu().double().numpy(), b.cpu().double().numpy()
+    within(o, a, 2.0 ** -9 * np.abs(a).max())
+    within(l, b, 2.0 ** -17 + 2.0 ** -20 * np.abs(b))
+
+
+@pytest.mark.parametrize("d,page,G,new", [(64, 64, 2, 6), (128, 128, 4, 20), (128, 64, 1, 130), (64, 128, 8, 40)])
+def test_blocks_nan_values_reach_the_rows_that_see_them(A, d, page, G, new):
+    """NaN codes in a listed page: rows before them are as without; in a page that is not listed they reach none."""
+    rng = np.random.default_rng(d + new)
+    n = 350 + new
+    c = R.make_cache(rng, 1, 1, page, d, [n])
+    q = R.make_queries(rng, new, G, d)
+    t = n - new // 2                                   # a key that the first half of the rows does not see
+    pid, slot = int(c.pages[0, t // page]), t % page
+    nb = -(-n // page)
+    log(f"blocks nan d={d} page={page} G={G} new={new}")
+    with_it = np.array([nb - 1, 0, t // page] if t // page < nb - 1 else [t // page, 0, 1], dtype=np.int32).reshape(1, 1, 1, 3)
+    without = np.array([0, 1, -1], dtype=np.int32).reshape(1, 1, 1, 3)
+    want, wl, bound, lb = P.attention(c, q, with_it, G, run=new)
+    ref = over_blocks(A, c, q, without, G, run=new)
+    first = t - (n - new)
+    c.v[pid, 0, slot, 5] = 0x7F
+    c.v[pid, 0, slot, d - 1] = 0xFF
+    o, l = over_blocks(A, c, q, with_it, G, run=new, check=False)
+    hit = np.zeros(o.shape, dtype=bool)
+    hit[first:, :, [5, d - 1]] = True
+    assert np.array_equal(np.isnan(o), hit)
+    within(np.where(hit, 0, o), np.where(hit, 0, want), bound)
+    within(l, wl, lb)
+    c.k[pid, 0, slot, 3] = 0x7F
+    o, l = over_blocks(A, c, q, with_it, G, run=new, check=False)
+    assert np.isnan(o[first:]).all() and np.isnan(l[first:]).all()
+    within(o[:first], want[:first], bound[:first])
+    within(l[:first], wl[:first], lb[:first])
+    o, l = over_blocks(A, c, q, without, G, run=new, check=False)
+    assert np.array_equal(o, ref[0]) and np.array_equal(l, ref[1])
+
+
+@pytest.mark.parametrize("d,page,run", [(64, 64, 1), (128, 128, 1), (128, 64, 64), (64, 128, 64)])
+def test_blocks_pages_that_are_none_and_tokens_before_position_0(A, d, page, run):
+    rng = np.random.default_rng(23)
+    c = R.make_cache(rng, 3, 2, page, d, [500, 300, 200])
+    c.pages[0, 1], c.pages[2, 0] = -1, c.n_pages
+    c.ks[rng.permutation(c.n_pages)[0]] = 127
+    new = [64, 64, 64]
+    c.lens = np.array([500, 40, 10], dtype=np.int32)
+    lists = random_lists(rng, c, 64 // run, 4)
+    o, l = over_blocks(A, c, R.make_queries(rng, 192, 8, d), lists, 4, new=new, run=run)
+    assert np.isinf(l[64:88]).all() and (o[64:88] == 0).all()
+
+
+def test_blocks_queries_with_strides_and_descales(A):
+    rng = np.random.default_rng(24)
+    c = R.make_cache(rng, 2, 2, 64, 64, [300, 200])
+    q = R.make_queries(rng, 2, 8, 64)
+    wide = torch.zeros((2, 12, 64), dtype=torch.bfloat16, device="cuda")
+    wide[:, 2:10] = R.torch_q(q, "bf16").cuda()
+    lists = random_lists(rng, c, 1, 4)
+    out, lse = A.cache_fwd_blocks(wide[:, 2:10], dev_cache(A, c), dev(c.pages), dev(c.lens), dev(lists), sm_scale=0.3, q_descale=0.5,
+                                  out_dtype=torch.float32)
+    want = P.attention(c, q, lists, 4, sm_scale=0.3, q_descale=0.5)
+    compare(out.cpu().double().numpy(), lse.cpu().double().numpy(), want, torch.float32)
+    none = A.cache_fwd_blocks(wide[:, 2:10], dev_cache(A, c), dev(c.pages), dev(c.lens), dev(lists), sm_scale=0.3, q_descale=0.5,
+                              out_dtype=torch.float32, want_lse=False)
+    assert none[1] is None and torch.equal(none[0], out)
+
+
+# ---- a shared prefix ----
+
+def over_shared(A, c, q, n_shared, G, kind="bf16", new=None, check=True, out_dtype=torch.float32, max_q=None, max_len=0, **kw):
+    T, Hq, d = q.shape
+    cu = None if new is None else cu_of(new)
+    max_q = (T // len(c.lens) if new is None else max(max(new), 1)) if max_q is None else max_q
+    out = torch.full((T, Hq, d), 7.0, dtype=out_dtype, device="cuda")
+    lse = torch.full((T, Hq), 7.0, device="cuda")
+    pages = c.pages.copy()
+    if n_shared < pages.shape[1]:
+        pages[1:, :n_shared] = -9                          # not looked at
+    A.cache_fwd_shared(R.torch_q(q, kind).cuda(), dev_cache(A, c), dev(pages), dev(c.lens), n_shared,
+                       cu=None if cu is None else dev(cu), max_q=max_q, out=out, lse=lse, max_len=max_len, **kw)
+    o, l = out.cpu().double().numpy(), lse.cpu().double().numpy()
+    if check:
+        compare(o, l, P.attention(c, q, None, G, run=max_q, cu=cu, max_q=max_q, **kw), out_dtype)
+    return o, l
+
+
+@pytest.mark.parametrize("kind", ["bf16", "e4m3"])
+@pytest.mark.parametrize("d,page", [(64, 64), (64, 128), (128, 64), (128, 128)])
+@pytest.mark.parametrize("lens,shared", [([130], 1), ([300, 257, 256, 10, 0], 2), ([900] + [770 + i for i in range(9)], 6),
+                                         ([600, 400], 0), ([640, 640, 640], 5)])
+def test_shared_for_single_tokens(A, lens, shared, d, page, kind):
+    log(f"shared {lens} {shared} d={d} page={page} {kind}")
+    rng = np.random.default_rng(len(lens) + d + shared)
+    c = P.share(R.make_cache(rng, len(lens), 2, page, d, lens), shared)
+    over_shared(A, c, R.make_queries(rng, len(lens), 8, d), shared, 4, kind,
+                out_dtype=torch.bfloat16 if shared == 2 else torch.float32)
+
+
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("d,page,G,kind", [(64, 128, 1, "bf16"), (64, 64, 3, "e4m3"), (128, 64, 8, "e4m3"), (128, 128, 4, "bf16")])
+@pytest.mark.parametrize("lens,new,shared", [([300], [40], 2), ([900, 829, 805], [17, 129, 5], 6), ([500, 0, 400, 128], [1, 0, 33, 100], 3),
+                                             ([700, 690], [200, 3], 4), ([400, 380, 200], [150, 140, 200], 2)])
+def test_shared_for_chunks(A, lens, new, shared, d, page, G, kind, causal):
+    """The last two: tokens whose own keys lie among the shared pages, a sequence that ends in them."""
+    log(f"shared {lens} {new} {shared} d={d} page={page} G={G} {kind} causal={causal}")
+    rng = np.random.default_rng(sum(lens) + d + G)
+    c = P.share(R.make_cache(rng, len(lens), 2, page, d, lens), shared)
+    q = R.make_queries(rng, sum(new) + 2, G * 2, d)       # two rows behind the last sequence
+    over_shared(A, c, q, shared, G, kind, new=new, causal=causal)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "e4m3"])
+@pytest.mark.parametrize("G,shared,n,page,d", [(4, 20, 2700, 128, 128), (4, 40, 2700, 64, 64), (8, 10, 1500, 128, 64), (8, 21, 1500, 64, 128),
+                                               (2, 300, 40000, 128, 64)])
+@pytest.mark.parametrize("pre_rows,own_rows", [(16, 16), (128, 16), (16, 128), (128, 128)])
+def test_shared_on_each_kernel(A, pre_rows, own_rows, G, shared, n, page, d, kind):
+    """Loose bounds on the tokens (of the call, of a sequence) make tall tiles."""
+    B, W, base = 4, -(-n // page), shared * page
+    T, max_q = next((t, m) for t in (30, 300, 600, 1000, 2000, 4000, 8000) for m in (9, 100, 200, 400, 800, 1600)
+                    for p in [P.shared_plan(B, 2, G, t, m, shared, W * page, page, d, n_cu())] if (p.pre.rows, p.own.rows) == (pre_rows, own_rows))
+    plan = P.shared_plan(B, 2, G, T, max_q, shared, W * page, page, d, n_cu())
+    log(f"shared rows {pre_rows} {own_rows} G={G} shared={shared} n={n} page={page} d={d} {kind} T={T} max_q={max_q} ranges {plan.pre.ranges} {plan.own.ranges}")
+    rng = np.random.default_rng(n + d)
+    c = R.make_cache(rng, 1, 2, page, d, [n], extra=B * (W - shared) + 2)
+    c.k[c.k & 127 == 127], c.v[c.v & 127 == 127] = 0x30, 0x31
+    spare = np.array([p for p in range(c.n_pages) if p not in c.pages[0]])[:(B - 1) * (W - shared)].reshape(B - 1, -1)
+    pages = np.concatenate([c.pages, np.concatenate([c.pages[[0] * (B - 1), :shared], spare], 1)]).astype(np.int32)
+    lens = [n, *(int(x) for x in rng.integers(base + 1, n, B - 1))]
+    c = R.Pages(c.k, c.v, c.ks, c.vs, pages, np.array(lens, dtype=np.int32))
+    new = [9, 8, 1, 7]
+    over_shared(A, c, R.make_queries(rng, T, 2 * G, d), shared, G, kind, new=new, max_q=max_q)
+
+
+@pytest.mark.parametrize("B,G,new", [(5, 4, 1), (3, 8, 40), (40, 4, 1)])
+@pytest.mark.parametrize("d,page", [(64, 64), (128, 128)])
+def test_shared_pages_that_are_none_and_lengths(A, d, page, B, G, new):
+    rng = np.random.default_rng(31)
+    c = P.share(R.make_cache(rng, B, 2, page, d, [700] * B), 4)
+    c.pages[:, 2], c.pages[0, 5] = -1, c.n_pages
+    c.lens = rng.integers(-20, 900, B).astype(np.int32)
+    q = R.make_queries(rng, B * new, 2 * G, d)
+    over_shared(A, c, q, 4, G)
+    # a bound inside and before the shared pages' end
+    for max_len in (4 * page + 70, 4 * page, 2 * page + 9, 1):
+        cut = R.Pages(c.k, c.v, c.ks, c.vs, c.pages, c.lens)
+        o, l = over_shared(A, c, q, 4, G, max_len=max_len, check=False)
+        a, b = A.cache_fwd(R.torch_q(q, "bf16").cuda(), dev_cache(A, cut), dev(c.pages), dev(c.lens), max_len=max_len, out_dtype=torch.float32)
+        a, b = a.cpu().double().numpy(), b.cpu().double().numpy()
+        assert np.array_equal(np.isnan(o), np.isnan(a)) and np.array_equal(np.isnan(l), np.isnan(b)) and np.array_equal(np.isinf(l), np.isinf(b))
+        top = np.abs(np.nan_to_num(a)).max()
+        within(np.nan_to_num(o), np.nan_to_num(a), 2.0 ** -9 * max(top, 1e-30))
+        fine = np.isfinite(b)
+        within(l[fine], b[fine], 2.0 ** -17 + 2.0 ** -20 * np.abs(b[fine])) if fine.any() else None
+
+
+@pytest.mark.parametrize("d,page,G,new", [(64, 64, 2, 6), (128, 128, 4, 20), (128, 64, 1, 60), (64, 128, 8, 40)])
+def test_shared_nan_values_reach_the_rows_that_see_them(A, d, page, G, new):
+    """A NaN in a shared page reaches the sequences whose tokens see it; the second ends before it."""
+    rng = np.random.default_rng(d + new)
+    base = 3 * page
+    lens = [base + new + 9, base - 20, base + 2 * new]
+    c = P.share(R.make_cache(rng, 3, 1, page, d, lens), 3)
+    q = R.make_queries(rng, 3 * new, G, d)
+    log(f"shared nan d={d} page={page} G={G} new={new}")
+    want, wl, bound, lb = R.attention(c, q, G)
+    pid = int(c.pages[0, 2])
+    c.v[pid, 0, page - 3, 5] = 0x7F
+    c.v[pid, 0, page - 3, d - 1] = 0xFF
+    o, l = over_shared(A, c, q, 3, G, check=False)
+    hit = np.zeros(o.shape, dtype=bool)
+    for rows in (slice(0, new), slice(2 * new, 3 * new)):
+        hit[rows][:, :, [5, d - 1]] = True
+    assert np.array_equal(np.isnan(o), hit)
+    within(np.where(hit, 0, o), np.where(hit, 0, want), bound)
+    within(l, wl, lb)
+    c.k[pid, 0, page - 3, 3] = 0x7F
+    o, l = over_shared(A, c, q, 3, G, check=False)
+    assert np.isnan(o[:new]).all() and np.isnan(l[2 * new:]).all()
+    within(o[new:2 * new], want[new:2 * new], bound[new:2 * new])
+
+
+def test_shared_far_scales_and_values(A):
+    """Blocks of far apart scales on both sides of the prefix's end, a far maximum in either."""
+    for seed in range(6):
+        rng = np.random.default_rng(40 + seed)
+        B = 2 if seed % 2 else 40
+        c = P.share(R.make_cache(rng, B, 2, 64, 64, [640] * B, spread=6), 5)
+        far = c.pages[0, 2] if seed % 3 else c.pages[0, 7]
+        c.ks[far] = 131
+        c.vs[c.pages[0, 3]] = 127 + (80 if seed < 3 else -80)
+        over_shared(A, c, R.make_queries(rng, B, 8, 64), 5, 4)
