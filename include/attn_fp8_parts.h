@@ -53,12 +53,17 @@ int attn_fp8_cache_bounds(const attn_fp8_cache *cache, const attn_fp8_batch *bat
  *   take       1 .. 16384; n_first, n_last >= 0, together at most take.
  *   run        >= 1.
  *   max_len    no lens[b] is larger (keys from max_len on are not seen); 0: W * page.  More than
- *              16384 blocks are ATTN_ERR_UNSUPPORTED.
+ *              16384 blocks are ATTN_ERR_UNSUPPORTED.  The plan goes by it.
+ *   workspace  256-byte aligned device memory of workspace_bytes, scratch of this call alone; at
+ *              least what attn_fp8_cache_select_workspace_bytes gives, else ATTN_ERR_INVALID_ARG.
+ *              NULL where that is 0.
  * Of the cache only k_scale is read.
  */
 int attn_fp8_cache_select(const attn_fp8_cache *cache, const attn_fp8_batch *batch, const attn_fp8_heads *q, int Hq,
                           const void *bounds, int32_t *blocks, int take, int run, int n_first, int n_last, int causal,
-                          int max_len, void *stream);
+                          int max_len, void *workspace, size_t workspace_bytes, void *stream);
+int attn_fp8_cache_select_workspace_bytes(const attn_fp8_cache *cache, const attn_fp8_batch *batch, int Hq, int take,
+                                          int run, int max_len, size_t *bytes);
 
 /*
  * attn_fp8_cache_fwd with the keys of a run's list in the place of all (of them those that a

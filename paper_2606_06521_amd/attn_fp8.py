@@ -212,8 +212,10 @@ _lib.attn_fp8_cache_evict.restype = _I
 # include/attn_fp8_parts.h
 _lib.attn_fp8_cache_bounds.argtypes = [_PC, _PB, _P, _P]
 _lib.attn_fp8_cache_bounds.restype = _I
-_lib.attn_fp8_cache_select.argtypes = [_PC, _PB, _PH, _I, _P, _P] + [_I] * 6 + [_P]
+_lib.attn_fp8_cache_select.argtypes = [_PC, _PB, _PH, _I, _P, _P] + [_I] * 6 + [_P, _Z, _P]
 _lib.attn_fp8_cache_select.restype = _I
+_lib.attn_fp8_cache_select_workspace_bytes.argtypes = [_PC, _PB, _I, _I, _I, _I, ctypes.POINTER(_Z)]
+_lib.attn_fp8_cache_select_workspace_bytes.restype = _I
 _lib.attn_fp8_cache_fwd_blocks.argtypes = [_PC, _PB, _PH, _I, _P, _I, _I, _P, _I, _P, _I, _F, _F, _P, _Z, _P]
 _lib.attn_fp8_cache_fwd_blocks.restype = _I
 _lib.attn_fp8_cache_blocks_workspace_bytes.argtypes = [_PC, _PB, _I, _I, _I, ctypes.POINTER(_Z)]
@@ -238,6 +240,13 @@ def attn_fp8_cache_workspace_bytes(cache, batch, Hq, max_len):
     """Returns (status, bytes)."""
     n = _Z(0)
     st = _lib.attn_fp8_cache_workspace_bytes(cache, batch, Hq, max_len, ctypes.byref(n))
+    return st, n.value
+
+
+def attn_fp8_cache_select_workspace_bytes(cache, batch, Hq, take, run, max_len):
+    """Returns (status, bytes)."""
+    n = _Z(0)
+    st = _lib.attn_fp8_cache_select_workspace_bytes(cache, batch, Hq, take, run, max_len, ctypes.byref(n))
     return st, n.value
 
 

@@ -447,7 +447,7 @@ int attn_fp8_cache_bounds(const attn_fp8_cache* cache, const attn_fp8_batch* bat
 
 int attn_fp8_cache_select(const attn_fp8_cache* cache, const attn_fp8_batch* batch, const attn_fp8_heads* q, int Hq,
                           const void* bounds, int32_t* blocks, int take, int run, int n_first, int n_last, int causal,
-                          int max_len, void* stream)
+                          int max_len, void* workspace, size_t workspace_bytes, void* stream)
 {
     int64_t runs;
     int st = check_attention(cache, batch, Hq, causal, 1.f, 1.f, max_len);
@@ -465,7 +465,11 @@ int attn_fp8_cache_select(const attn_fp8_cache* cache, const attn_fp8_batch* bat
     if ((st = check_cache(cache)) != ATTN_OK || (st = check_batch(batch, true)) != ATTN_OK ||
         (batch->T > 0 && (st = check_heads(q)) != ATTN_OK))
         return st;
-    if ((q->type != ATTN_TYPE_BF16 && q->type != ATTN_TYPE_E4M3) || !bounds || misaligned(bounds, 16) || !blocks || misaligned(blocks, 4))
+    if ((q->type != ATTN_TYPE_BF16 && q->type != ATTN_TYPE_E4M3) || !bounds || misaligned(bounds, 16) || !blocks || misaligned(blocks, 4) ||
+        misaligned(workspace, 256))
+        return ATTN_ERR_INVALID_ARG;
+    const attn::SelectPlan pl = attn::select_plan((int64_t)batch->B * cache->Hkv * runs, (most + cache->page - 1) / cache->page);
+    if (pl.bytes > 0 && (!workspace || workspace_bytes < pl.bytes))
         return ATTN_ERR_INVALID_ARG;
     attn::SelectParams p{};
     p.bt = batch_of(batch);
@@ -481,7 +485,27 @@ int attn_fp8_cache_select(const attn_fp8_cache* cache, const attn_fp8_batch* bat
     p.gr = attn::group_of(Hq / cache->Hkv);
     p.causal = causal;
     p.max_len = most;
-    return status(attn::launch_cache_select(p, cache->d, cache->page, q->type == ATTN_TYPE_E4M3, static_cast<hipStream_t>(stream)));
+    p.keys = static_cast<uint32_t*>(workspace);
+    return status(attn::launch_cache_select(p, pl, cache->d, cache->page, q->type == ATTN_TYPE_E4M3, static_cast<hipStream_t>(stream)));
+}
+
+int attn_fp8_cache_select_workspace_bytes(const attn_fp8_cache* cache, const attn_fp8_batch* batch, int Hq, int take, int run,
+                                          int max_len, size_t* bytes)
+{
+    if (!bytes)
+        return ATTN_ERR_INVALID_ARG;
+    *bytes = 0;
+    int64_t runs;
+    int st = check_attention(cache, batch, Hq, 1, 1.f, 1.f, max_len);
+    if (st == ATTN_OK)
+        st = check_lists(cache, batch, take, attn::kMaxChoice, run, runs);
+    if (st != ATTN_OK)
+        return st;
+    const int most = longest(cache, batch, max_len);
+    if (most > attn::kMaxChoice * cache->page)
+        return ATTN_ERR_UNSUPPORTED;
+    *bytes = attn::select_plan((int64_t)batch->B * cache->Hkv * runs, (most + cache->page - 1) / cache->page).bytes;
+    return ATTN_OK;
 }
 
 int attn_fp8_cache_blocks_workspace_bytes(const attn_fp8_cache* cache, const attn_fp8_batch* batch, int Hq, int take, int run,

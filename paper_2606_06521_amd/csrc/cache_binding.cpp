@@ -441,8 +441,16 @@ PyObject* select(PyObject*, PyObject* const* a, Py_ssize_t n)
     const std::array<int64_t, 4> full = {shape[0], shape[1], shape[2], take};
     const at::Tensor lists = a[13] == Py_None ? s.at.empty(full, at::kInt) : tensor(a[13], "blocks");
     int32_t* blocks = dense<int32_t>(lists, "blocks", s.at, at::kInt, full);
-    const int st = attn_fp8_cache_select(&s.c, &s.bt, &s.hq, (int)s.Hq, bounds, blocks, take, run, int_arg(a[9], "n_first"),
-                                         int_arg(a[10], "n_last"), truth(a[11]), int_arg(a[12], "max_len"), s.at.stream);
+    const int max_len = int_arg(a[12], "max_len");
+    size_t bytes = 0;
+    at::Tensor ws;
+    int st = attn_fp8_cache_select_workspace_bytes(&s.c, &s.bt, (int)s.Hq, take, run, max_len, &bytes);
+    if (!st) {
+        if (bytes)
+            ws = s.at.empty({(int64_t)bytes}, at::kByte);
+        st = attn_fp8_cache_select(&s.c, &s.bt, &s.hq, (int)s.Hq, bounds, blocks, take, run, int_arg(a[9], "n_first"),
+                                   int_arg(a[10], "n_last"), truth(a[11]), max_len, bytes ? ws.data_ptr() : nullptr, bytes, s.at.stream);
+    }
     return st ? PyLong_FromLong(st) : wrap(lists);
     END_HANDLE_TH_ERRORS
 }

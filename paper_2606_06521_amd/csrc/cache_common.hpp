@@ -383,7 +383,15 @@ struct SelectParams {
     int take, run, runs, n_first, n_last;
     Group gr;
     int causal, max_len;
+    uint32_t* keys;         // of a split call: the scores' keys [lists][most]
+    int parts, part, most;
 };
+
+struct SelectPlan {
+    int parts, part;        // workgroups that score a list's pages, pages of one
+    size_t bytes;           // workspace (0: one workgroup a list, one launch)
+};
+SelectPlan select_plan(int64_t lists, int most);
 
 struct WeightParams {
     Batch bt;
@@ -449,7 +457,7 @@ hipError_t launch_append(const Batch& bt, const Cache& c, int d, int page, const
 // (the launches: hipErrorNotSupported if a grid is too large, before any of them)
 hipError_t launch_cache_fwd(FwdParams p, const FwdPlan& plan, int d, int page, bool e4m3, hipStream_t s);
 hipError_t launch_cache_bounds(const BoundsParams& p, int d, int page, hipStream_t s);
-hipError_t launch_cache_select(const SelectParams& p, int d, int page, bool e4m3, hipStream_t s);
+hipError_t launch_cache_select(SelectParams p, const SelectPlan& plan, int d, int page, bool e4m3, hipStream_t s);
 hipError_t launch_cache_fwd_blocks(BlocksParams p, const FwdPlan& plan, int d, int page, bool e4m3, hipStream_t s);
 hipError_t launch_cache_fwd_shared(SharedParams p, const SharedPlan& plan, int d, int page, bool e4m3, hipStream_t s);
 hipError_t launch_cache_weights(const WeightParams& p, int d, int page, bool e4m3, int n_cu, hipStream_t s);

@@ -155,6 +155,22 @@ def test_select_among_many(A, n, page, take):
     assert (got >= 0).sum() == min(take, W)
 
 
+@pytest.mark.parametrize("d,G,run", [(64, 2, 1), (128, 8, 3)])
+@pytest.mark.parametrize("B,long", [(70, 3000), (140, 400), (140, 2100), (300, 400), (300, 5000), (300, 1500)])
+def test_select_of_many_lists(A, B, long, d, G, run):
+    """More lists than a split takes: one workgroup a list, of either size, with 16-row and 32-row tiles; a few
+    of the sequences are long."""
+    log(f"select of many lists B={B} long={long} d={d} G={G} run={run}")
+    rng = np.random.default_rng(B + long)
+    c = R.make_cache(rng, 1, 1, 64, d, [64 * 50])
+    lens = rng.integers(1, 64 * 12, B)
+    lens[[0, B // 2]] = 64 * long - 5, 64 * long - 900
+    pages = rng.choice(c.pages[0], (B, long)).astype(np.int32)
+    c = R.Pages(c.k, c.v, c.ks, c.vs, pages, lens.astype(np.int32))
+    new = [int(min(n, run)) for n in lens]
+    choose(A, c, any_queries(rng, sum(new), G, d, "bf16"), G, 17, new=new, run=run)
+
+
 def test_select_takes_the_earlier_of_equals(A):
     rng = np.random.default_rng(8)
     c = R.make_cache(rng, 2, 2, 64, 64, [64 * 30, 64 * 30])
@@ -165,6 +181,13 @@ def test_select_takes_the_earlier_of_equals(A):
         got = choose(A, c, q, 2, take, n_first=0, n_last=1)
         m = min(take, 30)
         assert np.array_equal(got[0, 0, 0, :m], [*range(m - 1), 29])
+    # as many of them that a histogram does not tell them apart: one workgroup a list, and split
+    for W, B in ((700, 1), (700, 300), (3000, 1)):
+        c.pages = np.broadcast_to(c.pages[:1, :1], (B, W)).copy()
+        c.pages[:, 5::7] = c.pages[0, 0] ^ 1
+        c.lens = np.full(B, 64 * W, dtype=np.int32)
+        c.lens[1:] = 64 * 3
+        choose(A, c, any_queries(rng, B, 4, 64, "bf16"), 2, 131, n_first=0, n_last=1)
 
 
 def test_select_sums_are_exact(A):

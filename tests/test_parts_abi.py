@@ -26,7 +26,8 @@ def test_exports_every_declared_symbol(A):
     text = re.sub(r"/\*.*?\*/", "", open(HEADER).read(), flags=re.S)
     names = sorted(set(re.findall(r"^int (attn_fp8_\w+)\(", text, flags=re.M)))
     assert names == ["attn_fp8_cache_blocks_workspace_bytes", "attn_fp8_cache_bounds", "attn_fp8_cache_fwd_blocks",
-                     "attn_fp8_cache_fwd_shared", "attn_fp8_cache_select", "attn_fp8_cache_shared_workspace_bytes"]
+                     "attn_fp8_cache_fwd_shared", "attn_fp8_cache_select", "attn_fp8_cache_select_workspace_bytes",
+                     "attn_fp8_cache_shared_workspace_bytes"]
     lib = ctypes.CDLL(A.LIB_PATH)
     for n in names:
         assert hasattr(lib, n) and hasattr(A, n), n
@@ -73,13 +74,13 @@ LISTS = [("a", dict(blocks=None), -1), ("a", dict(blocks=FAKE + 2), -1), ("a", d
 @pytest.mark.parametrize("kind,kw,status", SIZES + TOKENS + QUERIES + ATTENTION + LISTS + [
     ("a", dict(bounds=None), -1), ("a", dict(bounds=FAKE + 4), -1), ("a", dict(n_first=-1), -1), ("a", dict(n_last=-1), -1),
     ("a", dict(n_first=2, n_last=2), -1), ("a", dict(n_first=(1 << 31) - 1, n_last=(1 << 31) - 1), -1), ("a", dict(take=16385), -2),
-    ("a", dict(max_len=-1), -1), ("b", dict(W=16385), -2)])
+    ("a", dict(max_len=-1), -1), ("b", dict(W=16385), -2), ("a", dict(ws=FAKE + 16), -1), ("b", dict(W=5000), -1)])
 def test_select_refuses(A, kind, kw, status):
     c, b, q, _ = changed(A, kind, kw)
-    a = dict(Hq=4, bounds=FAKE, blocks=FAKE, take=3, run=1, n_first=1, n_last=1, causal=1, max_len=0)
+    a = dict(Hq=4, bounds=FAKE, blocks=FAKE, take=3, run=1, n_first=1, n_last=1, causal=1, max_len=0, ws=None)
     a.update(kw if kind == "a" else {})
     assert A.attn_fp8_cache_select(c, b, q, a["Hq"], a["bounds"], a["blocks"], a["take"], a["run"], a["n_first"], a["n_last"], a["causal"],
-                                   a["max_len"], None) == status
+                                   a["max_len"], a["ws"], 0, None) == status
 
 
 @pytest.mark.parametrize("kind,kw,status", SIZES + TOKENS + QUERIES + ATTENTION + OUTPUTS + LISTS + [("a", dict(take=(1 << 19) + 1), -2)])
@@ -106,6 +107,10 @@ def test_workspace_queries_refuse(A):
     assert A._lib.attn_fp8_cache_blocks_workspace_bytes(c, b, 4, 3, 1, None) == -1
     assert A._lib.attn_fp8_cache_shared_workspace_bytes(c, b, 2, 4, 0, None) == -1
     assert A.attn_fp8_cache_blocks_workspace_bytes(c, b, 4, 0, 1) == (-1, 0)
+    assert A._lib.attn_fp8_cache_select_workspace_bytes(c, b, 4, 3, 1, 0, None) == -1
+    assert A.attn_fp8_cache_select_workspace_bytes(c, b, 4, 0, 1, 0) == (-1, 0)
+    assert A.attn_fp8_cache_select_workspace_bytes(c, batch(A, W=16385), 4, 3, 1, 0) == (-2, 0)
+    assert A.attn_fp8_cache_select_workspace_bytes(c, b, 4, 3, 1, 0) == (0, 0)
     assert A.attn_fp8_cache_blocks_workspace_bytes(c, b, 5, 3, 1) == (-1, 0)
     assert A.attn_fp8_cache_shared_workspace_bytes(c, b, 5, 4, 0) == (-1, 0)
     assert A.attn_fp8_cache_shared_workspace_bytes(c, b, -1, 4, 0) == (-1, 0)
@@ -120,13 +125,13 @@ def test_empty_batches_are_fine(A):
         assert A.attn_fp8_cache_blocks_workspace_bytes(c, b, 4, 3, 1) == (0, 0)
         assert A.attn_fp8_cache_shared_workspace_bytes(c, b, 2, 4, 0) == (0, 0)
     # (a batch of sequences without new tokens still gets its lists, of -1)
-    assert A.attn_fp8_cache_select(c, batch(A, B=0, T=0), q, 4, FAKE, FAKE, 3, 1, 1, 1, 1, 0, None) == 0
+    assert A.attn_fp8_cache_select(c, batch(A, B=0, T=0), q, 4, FAKE, FAKE, 3, 1, 1, 1, 1, 0, None, 0, None) == 0
 
 
 @pytest.mark.parametrize("B,max_q,Hkv,G,run", [((1 << 31) - 1, 1, 1 << 16, 1, 1), (1 << 12, 1 << 20, 8, 1, 1), (1 << 18, 64, 8, 4, 8)])
 def test_lists_of_too_many_threads_are_unsupported(A, B, max_q, Hkv, G, run):
     c, b, q = cache(A, Hkv=Hkv), batch(A, B=B, T=1 << 30, cu=FAKE, max_q=max_q), heads(A)
-    assert A.attn_fp8_cache_select(c, b, q, Hkv * G, FAKE, FAKE, 3, run, 1, 1, 1, 0, None) == -2
+    assert A.attn_fp8_cache_select(c, b, q, Hkv * G, FAKE, FAKE, 3, run, 1, 1, 1, 0, None, 0, None) == -2
     assert A.attn_fp8_cache_fwd_blocks(c, b, q, Hkv * G, FAKE, 3, run, FAKE, 1, FAKE, 1, 0.1, 1.0, None, 0, None) == -2
     assert A.attn_fp8_cache_blocks_workspace_bytes(c, b, Hkv * G, 3, run) == (-2, 0)
 
@@ -162,3 +167,13 @@ def test_binding_refuses_tensors_on_the_host(A):
               lambda: A.cache_select(q, c, pages, lens, bounds, 1, n_last=0), lambda: A.cache_bounds(c, pages, lens, bounds)):
         with pytest.raises(ValueError, match="on the GPU"):
             f()
+
+
+def test_workspace_of_a_choice_holds_its_keys(A):
+    """A split choice (few lists of many pages) keeps four bytes for each page of each list."""
+    split = 0
+    for B, W, max_q, run in ((1, 2047, 1, 1), (1, 16384, 40, 8), (2, 600, 1, 1), (64, 4000, 1, 1), (4, 300, 1, 1)):
+        st, n = A.attn_fp8_cache_select_workspace_bytes(cache(A, page=64), batch(A, B=B, W=W, T=B, max_q=max_q, cu=FAKE), 4, 3, run, 0)
+        assert st == 0 and n in (0, B * 2 * -(-max_q // run) * W * 4)
+        split += n > 0
+    assert 0 < split < 5
