@@ -4,6 +4,8 @@
 
 #include "attn_common.hpp"
 
+#include <type_traits>
+
 namespace attn {
 
 // element types (the values of ATTN_TYPE_*)
@@ -246,16 +248,29 @@ __device__ inline bf16x8 widen(uint32_t a, uint32_t b)
     return bf16x8{x0[0], x0[1], x1[0], x1[1], x2[0], x2[1], x3[0], x3[1]};
 }
 
-// Eight channels of a query row as bf16.
+// Eight channels of a query row: as they lie in memory, and as bf16.
+template <bool E4M3>
+using Q8 = std::conditional_t<E4M3, i32x2, i32x4>;
+
+template <bool E4M3>
+__device__ inline Q8<E4M3> fetch_q8(const void* q, int64_t at)
+{
+    return *reinterpret_cast<const Q8<E4M3>*>(static_cast<const uint8_t*>(q) + at * (E4M3 ? 1 : 2));
+}
+
+template <bool E4M3>
+__device__ inline bf16x8 widen_q8(const Q8<E4M3>& w)
+{
+    if constexpr (E4M3)
+        return widen((uint32_t)w[0], (uint32_t)w[1]);
+    else
+        return __builtin_bit_cast(bf16x8, w);
+}
+
 template <bool E4M3>
 __device__ inline bf16x8 load_q8(const void* q, int64_t at)
 {
-    if constexpr (E4M3) {
-        const i32x2 w = *reinterpret_cast<const i32x2*>(static_cast<const uint8_t*>(q) + at);
-        return widen((uint32_t)w[0], (uint32_t)w[1]);
-    } else {
-        return __builtin_bit_cast(bf16x8, *reinterpret_cast<const i32x4*>(static_cast<const uint16_t*>(q) + at));
-    }
+    return widen_q8<E4M3>(fetch_q8<E4M3>(q, at));
 }
 
 }  // namespace

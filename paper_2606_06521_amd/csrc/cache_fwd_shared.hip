@@ -10,6 +10,23 @@
 
 namespace attn {
 
+namespace {
+
+hipError_t both_launch(const SharedParams& p, int d, int page, bool e4m3, unsigned grid, hipStream_t s)
+{
+    auto go = [&](auto kern) {
+        hipLaunchKernelGGL(kern, dim3(grid), dim3(256), 0, s, p);
+        return hipGetLastError();
+    };
+    if (d == 64)
+        return page == 64 ? (e4m3 ? go(cache_fwd_both_kernel<64, 64, true>) : go(cache_fwd_both_kernel<64, 64, false>))
+                          : (e4m3 ? go(cache_fwd_both_kernel<64, 128, true>) : go(cache_fwd_both_kernel<64, 128, false>));
+    return page == 64 ? (e4m3 ? go(cache_fwd_both_kernel<128, 64, true>) : go(cache_fwd_both_kernel<128, 64, false>))
+                      : (e4m3 ? go(cache_fwd_both_kernel<128, 128, true>) : go(cache_fwd_both_kernel<128, 128, false>));
+}
+
+}  // namespace
+
 SharedPlan shared_plan(int B, int Hkv, int G, int T, int max_q, int shared, int max_len, int page, int d, int n_cu)
 {
     const int base = (int)std::min<int64_t>((int64_t)shared * page, max_len);
@@ -54,6 +71,8 @@ hipError_t launch_cache_fwd_shared(SharedParams p, const SharedPlan& pl, int d, 
     p.pre_grid = g.pre;
     if (pl.pre.rows == pl.own.rows) {
         e = fwd_launch(p, pl.pre.rows, d, page, e4m3, g.pre + g.own, s);
+    } else if (pl.pre.rows == kTileRows) {
+        e = both_launch(p, d, page, e4m3, g.pre + g.own, s);
     } else {
         e = fwd_launch(p, pl.pre.rows, d, page, e4m3, g.pre, s);
         p.pre_grid = 0;
