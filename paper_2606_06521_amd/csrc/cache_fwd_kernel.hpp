@@ -148,12 +148,12 @@ __device__ inline bool share_of(const P& p, int tile_rows, int page, Share& x)
     }
     if (!workgroup_of(wg, units, ranges, tiles, x.tile, x.range, x.unit))
         return false;
+    x.v0 = x.range * chunk;
     x.u = unit_of(p, x.unit, common);
     x.u.s = uniform(x.u.s);
     if (x.tile * tile_rows >= x.u.s.n * p.gr.G)
         return false;
     x.visits = tile_visits(p, x.u, x.tile, tile_rows, page);
-    x.v0 = x.range * chunk;
     x.v1 = min(x.v0 + chunk, x.visits);
     x.whole = !kShared<P> && (kLists<P> ? p.ranges == 1 : x.visits <= chunk);
     return x.v0 < x.v1 || (!kShared<P> && x.range == 0) || (kLists<P> && !x.whole);

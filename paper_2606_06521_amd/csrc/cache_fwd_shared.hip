@@ -7,6 +7,7 @@
 #include "cache_merge.hpp"
 
 #include <algorithm>
+#include <cmath>
 
 namespace attn {
 
@@ -25,14 +26,57 @@ hipError_t both_launch(const SharedParams& p, int d, int page, bool e4m3, unsign
                       : (e4m3 ? go(cache_fwd_both_kernel<128, 128, true>) : go(cache_fwd_both_kernel<128, 128, false>));
 }
 
+// Plan of the shared pages where the sequences' own take 16-row tiles, by modelled time in microseconds:
+//   16-row tiles, a workgroup per CU (two at d = 64): 11.5 (9.2 at d = 64), 0.48 for each visit of a workgroup (0.62 where
+//     they fill the GPU) and 0.15 for each range that a row's merge adds up; for each further round of
+//     workgroups 6 and 0.75 for each visit of the own pages;
+//   128-row tiles in the same launch: 8.5, 2.0 for each visit (more where there is more than one
+//     workgroup for each CU), 0.1 for each range and for each MB of partial results, and the own
+//     pages' workgroups beside them, 0.012 and 0.0045 for each of their visits
+// (0.7 of a visit at d = 64).  Measured with 300 own tokens and 32/8 heads at d = 128: 4 sequences x 16384
+// shared keys 18.9 (16-row tiles) against 20.4, 16 x 16384 27.3 against 23.1, 64 x 16384 58 against 37;
+// 32 x 2048 19.6 against 18.8; 16 x 16/2 heads x 8192 15.4 against 17.5.
+FwdPlan shared_pages_plan(int Hkv, int64_t rows, int visits, int64_t own_wgs, int own_visits, int d, int n_cu)
+{
+    const double f = d == 64 ? 0.7 : 1.0;
+    FwdPlan best{};
+    double t_best = 0;
+    for (const int tile : {16, kTileRows}) {
+        const bool tall = tile == kTileRows;
+        const int64_t tiles = (rows + tile - 1) / tile;
+        for (int chunk = tall ? 2 : 8;; chunk *= 2) {
+            chunk = std::min(chunk, tall ? kTileChunk : kMaxChunk);
+            const int ranges = std::max(1, (visits + chunk - 1) / chunk);
+            const double wgs = (double)Hkv * tiles * ranges, each = std::min(chunk, visits);
+            const double mb = 1e-6 * wgs * tile * (d + 2) * sizeof(float);
+            const double slots = n_cu * (d == 64 ? 2.0 : 1.0);
+            const double t = tall ? 8.5 + 2.0 * f * each * std::max(1.0, 0.85 * wgs / n_cu) + 0.1 * (ranges + mb) +
+                                        own_wgs * (0.012 + 0.0045 * f * own_visits)
+                                  : (d == 64 ? 9.2 : 11.5) + f * each * (wgs < 0.75 * slots ? 0.48 : 0.62 * std::max(1.0, std::floor(wgs / slots))) + 0.15 * ranges +
+                                        (6 + 0.75 * f * own_visits) * (std::ceil((wgs + own_wgs) / slots) - 1);
+            if (!best.rows || t < t_best) {
+                t_best = t;
+                best = {tile, (int)tiles, chunk, ranges, 0};
+            }
+            if (chunk >= visits || chunk == (tall ? kTileChunk : kMaxChunk))
+                break;
+        }
+    }
+    return best;
+}
+
 }  // namespace
 
 SharedPlan shared_plan(int B, int Hkv, int G, int T, int max_q, int shared, int max_len, int page, int d, int n_cu)
 {
-    const int base = (int)std::min<int64_t>((int64_t)shared * page, max_len);
+    const int base = (int)std::min<int64_t>((int64_t)shared * page, max_len), visits = (base + kVisit - 1) / kVisit;
+    const int own_visits = (max_len - base + kVisit - 1) / kVisit;
+    const int64_t rows = (int64_t)T * G;
     SharedPlan pl;
-    pl.pre = cache_fwd_plan(Hkv, (int64_t)T * G, (base + kVisit - 1) / kVisit, d, n_cu);
-    pl.own = cache_fwd_plan((int64_t)B * Hkv, (int64_t)max_q * G, (max_len - base + kVisit - 1) / kVisit, d, n_cu);
+    pl.own = cache_fwd_plan((int64_t)B * Hkv, (int64_t)max_q * G, own_visits, d, n_cu);
+    pl.pre = pl.own.rows == kTileRows
+                 ? cache_fwd_plan(Hkv, rows, visits, d, n_cu)
+                 : shared_pages_plan(Hkv, rows, visits, (int64_t)B * Hkv * pl.own.tiles * pl.own.ranges, std::min(pl.own.chunk, own_visits), d, n_cu);
     pl.pre.bytes = (size_t)Hkv * pl.pre.tiles * pl.pre.ranges * pl.pre.rows * (d + 2) * sizeof(float);
     pl.own.bytes = (size_t)B * Hkv * pl.own.tiles * pl.own.ranges * pl.own.rows * (d + 2) * sizeof(float);
     return pl;

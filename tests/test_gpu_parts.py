@@ -460,13 +460,17 @@ def test_shared_for_chunks(A, lens, new, shared, d, page, G, kind, causal):
 
 @pytest.mark.parametrize("kind", ["bf16", "e4m3"])
 @pytest.mark.parametrize("G,shared,n,page,d", [(4, 20, 2700, 128, 128), (4, 40, 2700, 64, 64), (8, 10, 1500, 128, 64), (8, 21, 1500, 64, 128),
-                                               (2, 300, 40000, 128, 64)])
+                                               (2, 300, 40000, 128, 64), (2, 300, 20000, 64, 128)])
 @pytest.mark.parametrize("pre_rows,own_rows", [(16, 16), (128, 16), (16, 128), (128, 128)])
 def test_shared_on_each_kernel(A, pre_rows, own_rows, G, shared, n, page, d, kind):
     """Loose bounds on the tokens (of the call, of a sequence) make tall tiles."""
     B, W, base = 4, -(-n // page), shared * page
-    T, max_q = next((t, m) for t in (30, 300, 600, 1000, 2000, 4000, 8000) for m in (9, 100, 200, 400, 800, 1600)
-                    for p in [P.shared_plan(B, 2, G, t, m, shared, W * page, page, d, n_cu())] if (p.pre.rows, p.own.rows) == (pre_rows, own_rows))
+    found = [(t, m) for t in (4, 30, 300, 600, 1000, 2000, 4000, 8000) for m in (1, 9, 100, 200, 400, 800, 1600) if t == 4 or m > 1
+             for p in [P.shared_plan(B, 2, G, t, m, shared, W * page, page, d, n_cu())] if (p.pre.rows, p.own.rows) == (pre_rows, own_rows)]
+    if not found:
+        assert (pre_rows, own_rows, d) == (16, 16, 128)     # (128-row tiles are faster there)
+        pytest.skip("no call of these sizes takes these tiles")
+    T, max_q = found[0]
     plan = P.shared_plan(B, 2, G, T, max_q, shared, W * page, page, d, n_cu())
     log(f"shared rows {pre_rows} {own_rows} G={G} shared={shared} n={n} page={page} d={d} {kind} T={T} max_q={max_q} ranges {plan.pre.ranges} {plan.own.ranges}")
     rng = np.random.default_rng(n + d)
@@ -476,7 +480,7 @@ def test_shared_on_each_kernel(A, pre_rows, own_rows, G, shared, n, page, d, kin
     pages = np.concatenate([c.pages, np.concatenate([c.pages[[0] * (B - 1), :shared], spare], 1)]).astype(np.int32)
     lens = [n, *(int(x) for x in rng.integers(base + 1, n, B - 1))]
     c = R.Pages(c.k, c.v, c.ks, c.vs, pages, np.array(lens, dtype=np.int32))
-    new = [9, 8, 1, 7]
+    new = [9, 8, 1, 7] if T > 4 else [1, 1, 1, 1]
     over_shared(A, c, R.make_queries(rng, T, 2 * G, d), shared, G, kind, new=new, max_q=max_q)
 
 
