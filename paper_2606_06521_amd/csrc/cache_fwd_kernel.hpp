@@ -179,14 +179,14 @@ __device__ inline void common_last(const SharedParams& p, int row0, int rows, in
     for (int r = threadIdx.x; r < rows; r += 256)
         last[r] = kSeesAll;
     __syncthreads();
-    const int from = p.gr.token(row0), to = p.gr.token(row0 + rows - 1);
-    for (int b = threadIdx.x; b < p.bt.B; b += 256) {
+    // (the threads shared out among the sequences, as a chunk may hold all rows: one each takes 28.3 us in the place of
+    // 20.5 for 3 chunks of up to 64 tokens behind 14592 keys, 128-row tiles)
+    const int bits = max(8 - (p.bt.B > 1 ? 32 - __builtin_clz((unsigned)p.bt.B - 1) : 0), 0);
+    for (int b = (int)threadIdx.x >> bits; b < p.bt.B; b += 256 >> bits) {
         const Seq s = sequence(p.bt, b, p.max_len);
-        for (int i = max(s.first, from); i <= min(s.first + s.n - 1, to); ++i) {
-            const int key = last_key(s.pos0 + i - s.first, p.causal, s.len);
-            for (int r = max(i * p.gr.G - row0, 0); r < min((i + 1) * p.gr.G - row0, rows); ++r)
-                last[r] = key;
-        }
+        const int end = min((s.first + s.n) * p.gr.G - row0, rows);
+        for (int r = max(s.first * p.gr.G - row0, 0) + ((int)threadIdx.x & ((1 << bits) - 1)); r < end; r += 1 << bits)
+            last[r] = last_key(s.pos0 + p.gr.token(row0 + r) - s.first, p.causal, s.len);
     }
     __syncthreads();
 }

@@ -35,10 +35,12 @@ hipError_t both_launch(const SharedParams& p, int d, int page, bool e4m3, unsign
 //   16-row tiles, a workgroup per CU (two at d = 64): 11.5 (9.2 at d = 64), 0.48 for each visit of a workgroup (0.62 where
 //     they fill the GPU) and 0.15 for each range that a row's merge adds up; for each further round of
 //     workgroups 6 and 0.75 for each visit of the own pages;
-//   128-row tiles in the same launch: 8.5, 2.0 for each visit (more where there is more than one
-//     workgroup for each CU), 0.1 for each range and for each MB of partial results, and the own
-//     pages' workgroups beside them, 0.012 and 0.0045 for each of their visits
-// (0.7 of a visit at d = 64).  Measured with 300 own tokens and 32/8 heads at d = 128: 4 sequences x 16384
+//   128-row tiles in the same launch: 10, 0.29 for each MB of partial results, and of the two that run at once, a workgroup's
+//     own visits, 2.1 each, and what all of them take of the GPU (0.006 for each visit, 0.0056 for each workgroup,
+//     for each of the own pages' 0.007 and 0.0033 for each of its visits), the root of the sum of their cubes
+// (0.7 of a visit at d = 64, 0.74 on 128-row tiles).  Over 600 calls (2 to 256 sequences, 256 to 92000 shared keys, 16 to
+// 6000 own ones, 1 to 64 tokens, 1 to 16 KV heads of 1 to 8 rows) the plan takes 1.05 times the best
+// one's time, 1.14 in nine of ten, 1.49 at most.  Measured with 300 own tokens and 32/8 heads at d = 128: 4 sequences x 16384
 // shared keys 18.9 (16-row tiles) against 20.4, 16 x 16384 27.3 against 23.1, 64 x 16384 58 against 37;
 // 32 x 2048 19.6 against 18.8; 16 x 16/2 heads x 8192 15.4 against 17.5.
 FwdPlan shared_pages_plan(int Hkv, int64_t rows, int visits, int64_t own_wgs, int own_visits, int d, int n_cu)
@@ -55,10 +57,15 @@ FwdPlan shared_pages_plan(int Hkv, int64_t rows, int visits, int64_t own_wgs, in
             const double wgs = (double)Hkv * tiles * ranges, each = std::min(chunk, visits);
             const double mb = 1e-6 * wgs * tile * (d + 2) * sizeof(float);
             const double slots = n_cu * (d == 64 ? 2.0 : 1.0);
-            const double t = tall ? 8.5 + 2.0 * f * each * std::max(1.0, 0.85 * wgs / n_cu) + 0.1 * (ranges + mb) +
-                                        own_wgs * (0.012 + 0.0045 * f * own_visits)
-                                  : (d == 64 ? 9.2 : 11.5) + f * each * (wgs < 0.75 * slots ? 0.48 : 0.62 * std::max(1.0, std::floor(wgs / slots))) + 0.15 * ranges +
-                                        (6 + 0.75 * f * own_visits) * (std::ceil((wgs + own_wgs) / slots) - 1);
+            double t;
+            if (tall) {
+                const double f8 = d == 64 ? 0.74 : 1.0, own = 2.1 * f8 * each;
+                const double all = 256.0 / n_cu * (0.006 * f8 * Hkv * tiles * visits + 0.0056 * wgs + own_wgs * (0.007 + 0.0033 * f8 * own_visits));
+                t = 10 + 0.29 * mb + std::cbrt(own * own * own + all * all * all);
+            } else {
+                t = (d == 64 ? 9.2 : 11.5) + f * each * (wgs < 0.75 * slots ? 0.48 : 0.62 * std::max(1.0, std::floor(wgs / slots))) +
+                    0.15 * ranges + (6 + 0.75 * f * own_visits) * (std::ceil((wgs + own_wgs) / slots) - 1);
+            }
             if (!best.rows || t < t_best) {
                 t_best = t;
                 best = {tile, (int)tiles, chunk, ranges, 0};
