@@ -441,8 +441,8 @@ struct FwdPlan {
     size_t bytes;           // workspace
 };
 FwdPlan cache_fwd_plan(int B, int Hkv, int G, int max_q, int max_len, int d, int n_cu);
-// (heads: units of `rows` query rows; visits: of 128 keys)
-FwdPlan cache_fwd_plan(int64_t heads, int64_t rows, int visits, int d, int n_cu);
+// (heads: units of `rows` query rows; visits: of 128 keys; lists: units have lists of pages)
+FwdPlan cache_fwd_plan(int64_t heads, int64_t rows, int visits, int d, int n_cu, bool lists = false);
 
 // Whether a call can be launched at all, by the fewest workgroups of a plan; the grids of
 // one plan's launches (hipErrorNotSupported: too large).

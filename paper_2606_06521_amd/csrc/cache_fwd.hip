@@ -16,7 +16,11 @@ namespace {
 // merge: a launch, and the partial sums written and read.  Measured at 16 x 8 heads x
 // 8192 keys: 32 rows 51 (16-row tiles) against 82, 96 rows 149 against 113; one
 // sequence x 8 heads x 32768 keys: 64 rows 33 against 46, 256 rows 94 against 61.
-double plan_time(FwdPlan& pl, int rows, int64_t heads, int64_t run, int visits, int d, int n_cu)
+// Lists of neighbouring runs share pages, so their 128-row tiles wait less for memory: a visit takes 2.3 (at
+// d = 64 0.6 of 2.8) where one wave has rows, 3.0 where two have, and partial sums are read back from the caches.
+// d = 128: 2560 lists x 32 rows x 15 visits 213 against 328 on 16-row tiles, 512 x 32 x 121 301 against 293;
+// d = 64: 448 x 32 x 43 82 against 56.
+double plan_time(FwdPlan& pl, int rows, int64_t heads, int64_t run, int visits, int d, int n_cu, bool lists)
 {
     const bool tall = rows == kTileRows;
     pl.rows = rows;
@@ -30,17 +34,18 @@ double plan_time(FwdPlan& pl, int rows, int64_t heads, int64_t run, int visits, 
     pl.ranges = std::max(1, (visits + pl.chunk - 1) / pl.chunk);
     pl.bytes = pl.ranges > 1 ? (size_t)units * pl.ranges * rows * (d + 2) * sizeof(float) : 0;
     const double wgs = (double)units * pl.ranges, rounds = std::ceil(wgs / slots), each = std::min(pl.chunk, visits);
-    const double visit = (d == 64 ? 0.6 : 1.0) * (tall ? (wgs > n_cu ? 4.1 : 2.5) : 3.0 * (slots > n_cu && wgs > n_cu ? 1.5 : 1.0) / 4);
-    return 2 + rounds * ((tall ? 9 : 6) + each * visit) + (pl.ranges > 1 ? 5 + 2e-6 * pl.bytes / 2.5 : 0);
+    const double beside = !lists || run > 64 ? 4.1 : run > 32 ? 3.0 : d == 64 ? 2.8 : 2.3;
+    const double visit = (d == 64 ? 0.6 : 1.0) * (tall ? (wgs > n_cu ? beside : std::min(beside, 2.5)) : 3.0 * (slots > n_cu && wgs > n_cu ? 1.5 : 1.0) / 4);
+    return 2 + rounds * ((tall ? 9 : 6) + each * visit) + (pl.ranges > 1 ? 5 + (lists ? 0.29e-6 : 0.8e-6) * pl.bytes : 0);
 }
 
 }  // namespace
 
-FwdPlan cache_fwd_plan(int64_t heads, int64_t rows, int visits, int d, int n_cu)
+FwdPlan cache_fwd_plan(int64_t heads, int64_t rows, int visits, int d, int n_cu, bool lists)
 {
     FwdPlan low, tall;
-    const double t_low = plan_time(low, 16, heads, rows, visits, d, n_cu);
-    return rows > 16 && plan_time(tall, kTileRows, heads, rows, visits, d, n_cu) < t_low ? tall : low;
+    const double t_low = plan_time(low, 16, heads, rows, visits, d, n_cu, lists);
+    return rows > 16 && plan_time(tall, kTileRows, heads, rows, visits, d, n_cu, lists) < t_low ? tall : low;
 }
 
 FwdPlan cache_fwd_plan(int B, int Hkv, int G, int max_q, int max_len, int d, int n_cu)

@@ -13,14 +13,21 @@ namespace attn {
 FwdPlan blocks_plan(int64_t lists, int G, int run, int take, int page, int d, int n_cu)
 {
     const int visits = (take + kVisit / page - 1) / (kVisit / page);
-    FwdPlan pl = cache_fwd_plan(lists, (int64_t)run * G, visits, d, n_cu);
-    // few lists: a visit for each wave, where that leaves every second CU free all the same (8 lists x 64 visits
-    // 18.0 -> 14.7 us, 8 x 32 14.6 -> 13.6; not so 32 x 32, 17.3 -> 18.9)
+    FwdPlan pl = cache_fwd_plan(lists, (int64_t)run * G, visits, d, n_cu, true);
+    // few lists: a visit for each wave, where that leaves CUs free all the same (8 lists x 64 visits
+    // 18.0 -> 14.7 us, 26 x 33 18.8 -> 17.3, 28 x 26 at d = 64 14.1 -> 13.9; not so 32 x 32, 17.3 -> 18.9)
     const int64_t units = lists * pl.tiles, ranges = (visits + 3) / 4;
-    if (pl.rows == 16 && pl.ranges > 1 && pl.chunk == 8 && units * ranges <= n_cu / 2) {
+    if (pl.rows == 16 && pl.ranges > 1 && pl.chunk == 8 && units * ranges < n_cu) {
         pl.chunk = 4;
         pl.ranges = (int)ranges;
         pl.bytes = (size_t)units * ranges * pl.rows * (d + 2) * sizeof(float);
+    } else if (pl.ranges == 2 && (pl.rows == 16 ? visits <= (d == 64 ? 24 : 16) : visits <= 16 && (int64_t)run * G > 64)) {
+        // short lists: no merge (16-row tiles: 160 lists x 10 visits at d = 64 17.1 -> 13.7 us, 208 x 21 21.5 -> 18.6; at
+        // d = 128 96 x 9 17.4 -> 16.2, 112 x 16 18.9 -> 18.2; 128-row tiles: 256 lists x 128 rows x 5 38.6 -> 23.1, 224 x 128 x 14
+        // 49.3 -> 45.9; not so 216 x 64 x 8, 32.3 -> 32.5)
+        pl.chunk = visits;
+        pl.ranges = 1;
+        pl.bytes = 0;
     }
     return pl;
 }
