@@ -6,8 +6,8 @@
 // B G n rows instead of G n.  What follows in each sequence is the other part.
 //
 // Measured at d = 128, 32/8 heads: single tokens of 32 sequences behind 16384 common keys and up to 1024 of their own
-// 28.8 us (72 MB read; 23.8 for both kinds of tile in one launch, 6 for the merge); chunks of 192
-// tokens of 8 such sequences 221 us, 1.03 PFLOP/s (205 in the tiles, 15 for the merge, which
+// 28.7 us (72 MB read; 23 for both kinds of tile in one launch, 6 for the merge); chunks of up to 192
+// tokens of 8 such sequences 208 us, 1.10 PFLOP/s (194 in the tiles, 13 for the merge, which
 // reads 44 MB).
 #include "cache_merge.hpp"
 

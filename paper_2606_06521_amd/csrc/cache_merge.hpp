@@ -83,6 +83,35 @@ __global__ void __launch_bounds__(256) cache_merge(P p, int tile_rows, int page)
         return;                                  // (the range wrote the row itself)
     const int piece = threadIdx.x % PIECES, part = threadIdx.x / PIECES % PARTS;
     float m = -INFINITY;
+    // few parts: all of them on their way at once (references first and then the sums: 4.0 us in the place of 3.2 for 32
+    // rows of two parts, 15.9 in the place of 13.8 for 27200 of three)
+    constexpr int FEW = 4;
+    if (PARTS == 1 && n <= FEW) {
+        f32x4 x[FEW], acc = {};
+        float lc[FEW], mc[FEW], l = 0.f;
+#pragma unroll
+        for (int c = 0; c < FEW; ++c) {
+            const RowParts::One r = a.at(max(min(c, n - 1), 0));
+            x[c] = *reinterpret_cast<const f32x4*>(r.o + 4 * piece);
+            lc[c] = *r.l;
+            mc[c] = *r.m;
+        }
+#pragma unroll
+        for (int c = 0; c < FEW; ++c)
+            m = c < n ? fmax_f(m, mc[c]) : m;
+#pragma unroll
+        for (int c = 0; c < FEW; ++c) {
+            if (c >= n)
+                continue;
+            const int down = shift_of(mc[c], m);
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                acc[e] += __builtin_amdgcn_ldexpf(x[c][e], down);
+            l += __builtin_amdgcn_ldexpf(lc[c], down);
+        }
+        write_row<D>(p, s, u.hk, R, piece, acc, l, 1.f / l, m);
+        return;
+    }
     if constexpr (PARTS > 1) {
         for (int c = threadIdx.x; c < n; c += 256) {
             const float x = *a.at(c).m;
