@@ -3,9 +3,9 @@
 // kernels of the whole cache; a page of the list is anywhere in the sequence, so its first
 // key is read beside its number.
 //
-// Measured at d = 128, 32/8 heads: single tokens of 16 sequences on lists of 32 pages of 128 keys 32.9 us
-// (28.5 for 134 MB of K and V, 4.7 TB/s, and 4.5 for the merge); of one sequence on 128 pages of 64, E4M3
-// queries, 13.8; 2048 tokens in runs of 32 on 32 pages each 117 us, 1.17 PFLOP/s.
+// Measured at d = 128, 32/8 heads: single tokens of 16 sequences on lists of 32 pages of 128 keys 31.7 us
+// (28.5 for 134 MB of K and V, 4.7 TB/s, and 4 for the merge); of one sequence on 128 pages of 64, E4M3
+// queries, 13.9; 2048 tokens in runs of 32 on 32 pages each 114 to 124 us, 1.11 to 1.20 PFLOP/s.
 #include "cache_merge.hpp"
 
 namespace attn {
