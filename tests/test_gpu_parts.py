@@ -460,7 +460,7 @@ def test_shared_for_chunks(A, lens, new, shared, d, page, G, kind, causal):
 
 @pytest.mark.parametrize("kind", ["bf16", "e4m3"])
 @pytest.mark.parametrize("G,shared,n,page,d", [(4, 20, 2700, 128, 128), (4, 40, 2700, 64, 64), (8, 10, 1500, 128, 64), (8, 21, 1500, 64, 128),
-                                               (2, 300, 40000, 128, 64), (2, 300, 20000, 64, 128)])
+                                               (2, 300, 40000, 128, 64), (2, 300, 20000, 64, 128), (1, 40, 6000, 64, 128), (4, 120, 17000, 128, 128)])
 @pytest.mark.parametrize("pre_rows,own_rows", [(16, 16), (128, 16), (16, 128), (128, 128)])
 def test_shared_on_each_kernel(A, pre_rows, own_rows, G, shared, n, page, d, kind):
     """Loose bounds on the tokens (of the call, of a sequence) make tall tiles."""
