@@ -504,6 +504,8 @@ int attn_fp8_cache_select_workspace_bytes(const attn_fp8_cache* cache, const att
     const int most = longest(cache, batch, max_len);
     if (most > attn::kMaxChoice * cache->page)
         return ATTN_ERR_UNSUPPORTED;
+    if (batch->B == 0)
+        return ATTN_OK;
     *bytes = attn::select_plan((int64_t)batch->B * cache->Hkv * runs, (most + cache->page - 1) / cache->page).bytes;
     return ATTN_OK;
 }

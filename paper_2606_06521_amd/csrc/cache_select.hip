@@ -541,7 +541,7 @@ __global__ void __launch_bounds__(64 * NW) pick_kernel(SelectParams p, int page)
 SelectPlan select_plan(int64_t lists, int most)
 {
     SelectPlan pl{1, most, 0};
-    if (most > (lists > 64 ? 512 : 256) && lists <= 128) {
+    if (lists > 0 && most > (lists > 64 ? 512 : 256) && lists <= 128) {
         const int64_t want = std::min<int64_t>(512 / lists, (most + 127) / 128);
         pl.part = (int)std::min<int64_t>(((most + want - 1) / want + 127) / 128 * 128, kPartPages);
         pl.parts = (most + pl.part - 1) / pl.part;

@@ -811,3 +811,25 @@ def test_calls_without_tokens(A):
     assert (A.cache_select(one, *narrow, b, 3) == -1).all()
     for o, l in (A.cache_fwd_blocks(one, *narrow, lists), A.cache_fwd_shared(one, *narrow, 0)):
         assert (o == 0).all() and torch.isinf(l).all()
+
+
+@pytest.mark.parametrize("page", [64, 128])
+def test_calls_of_no_sequences_with_wide_tables(A, page):
+    """Tables of more pages than one workgroup's waves choose among, of no sequence."""
+    c = A.kv_cache(3, 2, 64, page=page)
+    b = A.key_bounds(3, 2, 64)
+    q = torch.zeros((0, 4, 64), dtype=torch.bfloat16, device="cuda")
+    lens = torch.zeros((0,), dtype=torch.int32, device="cuda")
+    for W in (257, 600, 16384):
+        log(f"no sequences page={page} W={W}")
+        pages = torch.zeros((0, W), dtype=torch.int32, device="cuda")
+        lists = A.cache_select(q, c, pages, lens, b, 3)
+        assert lists.shape == (0, 1, 2, 3)
+        assert A.cache_fwd_blocks(q, c, pages, lens, lists)[0].shape == (0, 4, 64)
+        assert A.cache_fwd_shared(q, c, pages, lens, 2)[0].shape == (0, 4, 64)
+        assert A.cache_bounds(c, pages, lens, b) is b
+        # sequences without new tokens beside it: empty lists
+        some = torch.zeros((2, W), dtype=torch.int32, device="cuda")
+        lists = A.cache_select(q, c, some, torch.full((2,), W * page, dtype=torch.int32, device="cuda"), b, 3,
+                               blocks=torch.full((2, 1, 2, 3), 9, dtype=torch.int32, device="cuda"))
+        assert (lists == -1).all()

@@ -5,6 +5,7 @@ import os
 import re
 import shutil
 import subprocess
+import sys
 
 import pytest
 import torch
@@ -177,3 +178,24 @@ def test_workspace_of_a_choice_holds_its_keys(A):
         assert st == 0 and n in (0, B * 2 * -(-max_q // run) * W * 4)
         split += n > 0
     assert split == 5           # (not: more than 128 lists; pages that one workgroup's waves hold)
+
+
+def test_workspace_of_a_choice_for_an_empty_batch():
+    """No sequences, tables on both sides of the split's thresholds: no workspace and no division by the
+    number of lists, and the call itself is a no-op.  In a process of its own, which such a division would end."""
+    code = """
+from paper_2606_06521_amd import attn_fp8 as A
+from tests.test_cache_abi import FAKE, batch, cache, heads
+for W in (0, 4, 256, 257, 512, 513, 600, 16384):
+    for page in (64, 128):
+        c = cache(A, page=page)
+        for b in (batch(A, B=0, T=0, W=W), batch(A, B=0, T=0, W=W, cu=FAKE, max_q=40)):
+            assert A.attn_fp8_cache_select_workspace_bytes(c, b, 4, 3, 8, 0) == (0, 0), (W, page)
+            assert A.attn_fp8_cache_select(c, b, heads(A), 4, FAKE, FAKE, 3, 8, 1, 1, 1, 0, None, 0, None) == 0
+        # (sequences without new tokens have lists, so their choice keeps its keys)
+        st, n = A.attn_fp8_cache_select_workspace_bytes(c, batch(A, T=0, W=W), 4, 3, 1, 0)
+        assert st == 0 and n == (2 * 2 * W * 4 if W > 256 else 0), (W, page, st, n)
+print("done")
+"""
+    r = subprocess.run([sys.executable, "-c", code], cwd=ROOT, capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0 and r.stdout.split() == ["done"], (r.returncode, r.stdout, r.stderr[-2000:])
