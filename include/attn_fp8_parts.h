@@ -31,8 +31,9 @@ extern "C" {
  * taken again after each append to it.
  *   bounds   E4M3 [n_pages][Hkv][2][d] (least, largest), 16-byte aligned; on the K scale of
  *            the page.
- * The batch's T bounds the entries of cu and is otherwise not looked at.  Pages that two
- * sequences hold have to be full in both.
+ * T is looked at for the bound on the entries of cu, or with cu = NULL for the T / B new tokens
+ * of each sequence.  B * Hkv is below 2^24 here (else ATTN_ERR_UNSUPPORTED), W as wide as a
+ * table may be.  Pages that two sequences hold have to be full in both.
  */
 int attn_fp8_cache_bounds(const attn_fp8_cache *cache, const attn_fp8_batch *batch, void *bounds, void *stream);
 

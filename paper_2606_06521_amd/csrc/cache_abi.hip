@@ -441,8 +441,7 @@ int attn_fp8_cache_bounds(const attn_fp8_cache* cache, const attn_fp8_batch* bat
     p.bounds = static_cast<uint8_t*>(bounds);
     // (n tokens lie in at most this many pages)
     const int most = (batch->max_q + cache->page - 2) / cache->page + 1;
-    p.most = most < batch->W ? most : batch->W;
-    return status(attn::launch_cache_bounds(p, cache->d, cache->page, static_cast<hipStream_t>(stream)));
+    return status(attn::launch_cache_bounds(p, most < batch->W ? most : batch->W, cache->d, cache->page, static_cast<hipStream_t>(stream)));
 }
 
 int attn_fp8_cache_select(const attn_fp8_cache* cache, const attn_fp8_batch* batch, const attn_fp8_heads* q, int Hq,

@@ -11,6 +11,7 @@
 #include <ATen/ATen.h>
 #include <c10/hip/HIPStream.h>
 
+#include <algorithm>
 #include <array>
 #include <cmath>
 #include <string>
@@ -469,17 +470,30 @@ PyObject* bounds(PyObject*, PyObject* const* a, Py_ssize_t n)
     const int64_t most = a[5] == Py_None ? pages.size(1) * c.page : integer(a[5]);
     if (most < 0 || most > INT32_MAX)
         value_error("max_q is out of range");
+    const int B = narrow(pages.size(0), "B");
     attn_fp8_batch bt{};
     bt.pages = ints(a[1], "pages", at, pages.sizes());
-    bt.B = narrow(pages.size(0), "B");
     bt.W = narrow(pages.size(1), "W");
-    bt.lens = ints(a[2], "lens", at, {pages.size(0)});
+    bt.lens = ints(a[2], "lens", at, {B});
     bt.max_q = (int)(most < 1 ? 1 : most);
     if (a[4] != Py_None)
-        bt.cu = ints(a[4], "cu", at, {pages.size(0) + 1});
-    bt.T = a[4] != Py_None ? 1 << 30 : narrow(pages.size(0) * most, "tokens");
-    const int st = attn_fp8_cache_bounds(&c, &bt, bounds_of(a[3], c, at), at.stream);
-    return st ? PyLong_FromLong(st) : Py_NewRef(a[3]);
+        bt.cu = ints(a[4], "cu", at, {(int64_t)B + 1});
+    void* const to = bounds_of(a[3], c, at);
+    // (without cu a call has B max_q tokens, and the tables may have room for more than the 2^30 that it may
+    // have: as many sequences to a call as that allows)
+    const int64_t most_tokens = 1 << 30, each = bt.cu || most < 1 ? B : std::max<int64_t>(most_tokens / most, 1);
+    int64_t b = 0;
+    do {
+        bt.B = (int)std::min<int64_t>(each, B - b);
+        bt.T = (int)(bt.cu ? most_tokens : bt.B * most);
+        const int st = attn_fp8_cache_bounds(&c, &bt, to, at.stream);
+        if (st)
+            return PyLong_FromLong(st);
+        b += bt.B;
+        bt.lens += bt.B;
+        bt.pages += (int64_t)bt.B * bt.W;
+    } while (b < B);
+    return Py_NewRef(a[3]);
     END_HANDLE_TH_ERRORS
 }
 

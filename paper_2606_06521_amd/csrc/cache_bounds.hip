@@ -9,6 +9,8 @@
 // chain and then 4 us of the stream: all workgroups start at once and each has its whole page on the way.
 #include "cache_common.hpp"
 
+#include <algorithm>
+
 namespace attn {
 
 namespace {
@@ -18,19 +20,11 @@ typedef int16_t s16x2_t __attribute__((ext_vector_type(2)));
 // The codes of a word as signed bytes of the same order (it is its own inverse).
 __device__ inline uint32_t ordered(uint32_t w) { return w ^ (((w >> 7) & 0x01010101u) * 0x7Fu); }
 
+// Bounds of page `block` of sequence b, of its keys before `to`; by all threads of the workgroup.
 template <int D, int PAGE>
-__global__ void __launch_bounds__(256) bounds_kernel(BoundsParams p)
+__device__ inline void page_bounds(const BoundsParams& p, int b, int hk, int block, int to, int (&lo_sh)[4][D / 2], int (&hi_sh)[4][D / 2])
 {
     constexpr int CPR = D / 16, RPP = 256 / CPR, NL = (PAGE + RPP - 1) / RPP;       // chunks of a row, rows of a pass
-    __shared__ int lo_sh[4][D / 2], hi_sh[4][D / 2];
-    const int hk = (int)(blockIdx.x % p.cache.Hkv);
-    const int rest = (int)(blockIdx.x / p.cache.Hkv);
-    const int b = rest / p.most;
-    const Seq s = uniform(sequence(p.bt, b, p.bt.W * PAGE));
-    const int from = max(s.pos0, 0), to = min(s.pos0 + s.n, s.len);
-    const int block = from / PAGE + rest % p.most;
-    if (block * PAGE >= to || from >= to)
-        return;
     const int pid = __builtin_amdgcn_readfirstlane(page_of(p.bt, p.cache.n_pages, b, block));
     if (pid < 0)
         return;
@@ -103,12 +97,37 @@ __global__ void __launch_bounds__(256) bounds_kernel(BoundsParams p)
     }
 }
 
+template <int D, int PAGE>
+__global__ void __launch_bounds__(256) bounds_kernel(BoundsParams p)
+{
+    __shared__ int lo_sh[4][D / 2], hi_sh[4][D / 2];
+    const int hk = (int)(blockIdx.x % p.cache.Hkv);
+    const int rest = (int)(blockIdx.x / p.cache.Hkv);
+    const int b = rest / p.step;
+    const Seq s = uniform(sequence(p.bt, b, p.bt.W * PAGE));
+    const int from = max(s.pos0, 0), to = min(s.pos0 + s.n, s.len);
+    if (from >= to)
+        return;
+    for (int block = from / PAGE + rest % p.step; block * PAGE < to; block += p.step) {
+        page_bounds<D, PAGE>(p, b, hk, block, to, lo_sh, hi_sh);
+        if ((block + p.step) * PAGE < to)
+            __syncthreads();            // (the next page's bounds go to the same LDS)
+    }
+}
+
 }  // namespace
 
-hipError_t launch_cache_bounds(const BoundsParams& p, int d, int page, hipStream_t s)
+// (most: pages of a sequence that may hold new tokens)
+hipError_t launch_cache_bounds(BoundsParams p, int most, int d, int page, hipStream_t s)
 {
+    // One workgroup per page and head.  Tables with room for more than a launch has workgroups for hold
+    // far fewer tokens: 2^20 workgroups then take the pages that there are in turns.
+    const int64_t heads = (int64_t)p.bt.B * p.cache.Hkv;
     unsigned grid;
-    const hipError_t e = grid_of((__int128)p.bt.B * p.most * p.cache.Hkv, 256, grid);
+    p.step = most;
+    if (grid_of((__int128)heads * most, 256, grid) != hipSuccess)
+        p.step = (int)std::max<int64_t>((1 << 20) / heads, 1);
+    const hipError_t e = grid_of((__int128)heads * p.step, 256, grid);
     if (e != hipSuccess)
         return e;
     auto go = [&](auto kern) {

@@ -386,7 +386,7 @@ struct BoundsParams {
     Batch bt;
     Cache cache;
     uint8_t* bounds;        // E4M3 [n_pages][Hkv][2][d]: the least codes, the largest
-    int most;               // pages per sequence that may hold new tokens
+    int step;               // workgroups of a sequence and KV head: each takes every step-th page of new tokens
 };
 
 struct SelectParams {
@@ -471,7 +471,7 @@ hipError_t launch_append(const Batch& bt, const Cache& c, int d, int page, const
                          const Rotation& r, const Heads& q, const Heads& q_out, int Hq, hipStream_t s);
 // (the launches: hipErrorNotSupported if a grid is too large, before any of them)
 hipError_t launch_cache_fwd(FwdParams p, const FwdPlan& plan, int d, int page, bool e4m3, hipStream_t s);
-hipError_t launch_cache_bounds(const BoundsParams& p, int d, int page, hipStream_t s);
+hipError_t launch_cache_bounds(BoundsParams p, int most, int d, int page, hipStream_t s);
 hipError_t launch_cache_select(SelectParams p, const SelectPlan& plan, int d, int page, bool e4m3, hipStream_t s);
 hipError_t launch_cache_fwd_blocks(BlocksParams p, const FwdPlan& plan, int d, int page, bool e4m3, hipStream_t s);
 hipError_t launch_cache_fwd_shared(SharedParams p, const SharedPlan& plan, int d, int page, bool e4m3, hipStream_t s);

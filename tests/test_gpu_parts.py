@@ -833,3 +833,30 @@ def test_calls_of_no_sequences_with_wide_tables(A, page):
         lists = A.cache_select(q, c, some, torch.full((2,), W * page, dtype=torch.int32, device="cuda"), b, 3,
                                blocks=torch.full((2, 1, 2, 3), 9, dtype=torch.int32, device="cuda"))
         assert (lists == -1).all()
+
+
+@pytest.mark.parametrize("B,W,Hkv,page", [(3, 1 << 20, 16, 64), (3, 400000, 16, 128), (300, 40000, 1, 128), (300, 100000, 1, 128), (700, 30000, 8, 64)])
+def test_bounds_of_all_tokens_with_wide_tables(A, B, W, Hkv, page):
+    """max_q=None on tables with room for far more tokens than there are, more than a batch may have (2^30) and than
+    a launch has workgroups for (2^24): the bounds are those of the tokens there are."""
+    log(f"bounds of wide tables B={B} W={W} Hkv={Hkv} page={page}")
+    rng = np.random.default_rng(B)
+    c = R.make_cache(rng, 4, Hkv, page, 64, [700, 130, 1, 1000])
+    wide = torch.full((B, W), -1, dtype=torch.int32, device="cuda")
+    lens = np.zeros(B, dtype=np.int32)
+    at = [0, B // 2, B - 1]
+    for b, i in zip(at, range(3)):
+        wide[b, :c.pages.shape[1]] = dev(c.pages[i])
+        lens[b] = c.lens[i]
+    given = np.full((c.n_pages, Hkv, 2, 64), 1.5)
+    got = dev_bounds(given)
+    A.cache_bounds(dev_cache(A, c), wide, dev(lens), got)
+    few = R.Pages(c.k, c.v, c.ks, c.vs, c.pages[:3], c.lens[:3])
+    assert np.array_equal(values(got), P.bounds(few, given, max_q=W * page))
+    # a sequence that fills its table
+    last = torch.full((1, W), int(c.pages[3, 0]), dtype=torch.int32, device="cuda")
+    last[0, W - c.pages.shape[1]:] = dev(c.pages[3])
+    got = dev_bounds(given)
+    A.cache_bounds(dev_cache(A, c), last, dev(np.array([W * page], dtype=np.int32)), got)
+    full = R.Pages(c.k, c.v, c.ks, c.vs, c.pages[3:], np.array([c.pages.shape[1] * page], dtype=np.int32))
+    assert np.array_equal(values(got), P.bounds(full, given, max_q=W * page))

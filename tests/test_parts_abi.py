@@ -199,3 +199,9 @@ print("done")
 """
     r = subprocess.run([sys.executable, "-c", code], cwd=ROOT, capture_output=True, text=True, timeout=300)
     assert r.returncode == 0 and r.stdout.split() == ["done"], (r.returncode, r.stdout, r.stderr[-2000:])
+
+
+@pytest.mark.parametrize("B,Hkv", [(1 << 23, 2), (1 << 8, 1 << 16), ((1 << 30) - 1, 1)])
+def test_bounds_of_too_many_heads_are_unsupported(A, B, Hkv):
+    for cu in (None, FAKE):
+        assert A.attn_fp8_cache_bounds(cache(A, Hkv=Hkv), batch(A, B=B, T=B, cu=cu), FAKE, None) == -2
