@@ -860,3 +860,46 @@ def test_bounds_of_all_tokens_with_wide_tables(A, B, W, Hkv, page):
     A.cache_bounds(dev_cache(A, c), last, dev(np.array([W * page], dtype=np.int32)), got)
     full = R.Pages(c.k, c.v, c.ks, c.vs, c.pages[3:], np.array([c.pages.shape[1] * page], dtype=np.int32))
     assert np.array_equal(values(got), P.bounds(full, given, max_q=W * page))
+
+
+# Table widths and lengths of a choice's four forms, by the number of its lists and the pages there may be:
+# parts of a list by workgroups of their own (few lists of many pages), a workgroup a list for up to 16384 pages,
+# for up to 2048 of many lists (four waves) and of few (eight).
+FORMS = {"split": (2, 700), "large": (140, 2100), "many": (300, 400), "few": (140, 300)}
+
+
+@pytest.mark.parametrize("kind", ["bf16", "e4m3"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("G,run", [(4, 3), (3, 11), (8, 40)])
+@pytest.mark.parametrize("form", FORMS)
+def test_select_in_each_form(A, form, G, run, d, kind):
+    """Every kernel of the choice: 16-row tiles (run * G up to 16), 32-row tiles of fewer and of more tiles than waves."""
+    B, W = FORMS[form]
+    rng = np.random.default_rng(B + G + d)
+    heads = 2 if form == "split" else 1
+    c = R.make_cache(rng, 1, heads, 64, d, [64 * 40])
+    lens = rng.integers(1, 64 * 9, B)
+    lens[0], lens[B // 2] = 64 * W - 5, 64 * W * 3 // 4
+    pages = rng.choice(c.pages[0], (B, W)).astype(np.int32)
+    c = R.Pages(c.k, c.v, c.ks, c.vs, pages, lens.astype(np.int32))
+    new = [int(min(n, 1 + i % run)) for i, n in enumerate(lens)]
+    new[0] = new[B // 2] = run
+    size = A.attn_fp8_cache_select_workspace_bytes(A.attn_fp8_cache(None, None, None, None, c.n_pages, heads, 64, d),
+                                                   A.attn_fp8_batch(None, None, None, B, W, sum(new), run), heads * G, 17, run, 0)
+    assert size == (0, 4 * B * heads * W if form == "split" else 0) and (W > 2048) == (form == "large") and (B > 256) == (form == "many")
+    log(f"select form={form} G={G} run={run} d={d} {kind}")
+    choose(A, c, any_queries(rng, sum(new), G * heads, d, kind), G, 17, kind, new=new, run=run)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "e4m3"])
+@pytest.mark.parametrize("d,page,n,take", [(128, 64, 131001, 128), (64, 64, 1 << 20, 300), (128, 128, 1 << 21, 16384)])
+def test_select_for_one_long_request(A, d, page, n, take, kind):
+    """Up to 16384 pages of one sequence, single tokens of four heads: parts of the list by several workgroups."""
+    rng = np.random.default_rng(n)
+    c = R.make_cache(rng, 1, 1, page, d, [page * 40])
+    W = -(-n // page)
+    c.pages = np.concatenate([c.pages, rng.choice(c.pages[0], (1, W - 40))], 1).astype(np.int32)
+    c.lens = np.array([n], dtype=np.int32)
+    log(f"select one long request n={n} page={page} d={d} take={take} {kind}")
+    got = choose(A, c, any_queries(rng, 1, 4, d, kind), 4, take, kind)
+    assert (got >= 0).sum() == min(take, W)
