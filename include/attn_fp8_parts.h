@@ -44,14 +44,17 @@ int attn_fp8_cache_bounds(const attn_fp8_cache *cache, const attn_fp8_batch *bat
  *   2^x sum_c max(Q_c least_c, Q_c largest_c),   Q = q 2^-e rounded to whole numbers (ties to even),
  * e the least whole number with |q| <= 127 2^e in all channels, x = e + k byte - 127 held to
  * -96 .. 96.  (All sums are exact in FP32.)  A query row with a channel that is not finite takes
- * no part; a block without such a row scores -inf.  The list holds, in ascending order, `take` of
- * the blocks that the run's last token sees a key of and that have a page: the first n_first,
- * the last n_last, and those of the highest scores, equal ones from the lowest block on.  What is
- * left of the list is -1, and so are the lists of runs without tokens.
+ * no part; a block whose first key no other row sees scores -inf.  The list holds, in ascending
+ * order, `take` of the blocks that the run's last token sees a key of and that have a page: the
+ * first n_first, the last n_last, and those of the highest scores, equal ones from the lowest block
+ * on.  What is left of the list is -1, and so are the lists of runs without tokens.
  *   q          as for attn_fp8_cache_fwd.
  *   bounds     of attn_fp8_cache_bounds, for all blocks that are seen.
  *   blocks     out.
- *   take       1 .. 16384; n_first, n_last >= 0, together at most take.
+ *   take       1 .. 16384; n_first, n_last >= 0, together at most take.  With causal = 1 the pages
+ *              that a run's own tokens lie in are among the last 1 + ceil((run - 1) / page): with a
+ *              smaller n_last a list may lack the own page of the run's earlier tokens, and such a
+ *              token may see no key.
  *   run        >= 1.
  *   max_len    no lens[b] is larger (keys from max_len on are not seen); 0: W * page.  More than
  *              16384 blocks are ATTN_ERR_UNSUPPORTED.  The plan goes by it.

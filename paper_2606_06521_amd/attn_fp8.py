@@ -555,8 +555,9 @@ def cache_select(q, cache, pages, lens, bounds, take, *, cu=None, max_q=None, ru
     """The `take` pages of each run of `run` new tokens and KV head whose bounds allow the largest
     scores of the run's queries, as places in the sequence's row of pages: int32
     [B, ceil(max_q / run), Hkv, take], ascending, then -1.  The first n_first and the last n_last
-    of the pages that the run sees are always among them; equal scores: the earlier page.
-    q and the others as for cache_fwd."""
+    of the pages that the run sees are always among them; equal scores: the earlier page.  Runs of
+    more than one token may cross the end of a page: all of them keep their own page, and so see
+    themselves, with n_last = 1 + ceil((run - 1) / page).  q and the others as for cache_fwd."""
     return _call(stream, _binding.select, q, cache, pages, lens, bounds, take, cu, max_q, run, n_first, n_last, causal,
                  max_len, blocks)
 

@@ -903,3 +903,22 @@ def test_select_for_one_long_request(A, d, page, n, take, kind):
     log(f"select one long request n={n} page={page} d={d} take={take} {kind}")
     got = choose(A, c, any_queries(rng, 1, 4, d, kind), 4, take, kind)
     assert (got >= 0).sum() == min(take, W)
+
+
+@pytest.mark.parametrize("page", [64, 128])
+@pytest.mark.parametrize("run", [1, 2, 16, 64, 65, 100, 128, 129, 200])
+def test_tokens_of_a_run_keep_their_own_pages(A, run, page):
+    """n_last = 1 + ceil((run - 1) / page): a run that crosses the ends of pages has the pages of all of its tokens, so
+    every token sees itself."""
+    rng = np.random.default_rng(run)
+    lens, new = [900, 517, 64, 300], [400, 129, 64, 7]
+    c = R.make_cache(rng, 4, 1, page, 64, lens)
+    q = any_queries(rng, sum(new), 2, 64, "bf16")
+    n_last = 1 + -(-(run - 1) // page)
+    log(f"select keeps own pages run={run} page={page}")
+    got = choose(A, c, q, 2, n_last, new=new, run=run, n_first=0, n_last=n_last)
+    for b in range(4):
+        for i in range(new[b]):
+            assert (lens[b] - new[b] + i) // page in got[b, i // run, 0]
+    out, lse = over_blocks(A, c, q, got, 2, new=new, run=run)
+    assert np.isfinite(lse).all()
