@@ -172,6 +172,10 @@ __device__ inline float* part_of(const P& p, const Share& x, int tile_rows, int 
 
 constexpr int kSeesAll = 1 << 30;   // (past every key)
 
+// The last key that has to be there for a row: one of no sequence masks none and needs none (its Q may be
+// anything, and so may pages that lie behind all sequences).
+__device__ inline int seen_by(int last) { return last == kSeesAll ? -1 : last; }
+
 // The last keys that the rows row0 .. row0 + rows - 1 of all tokens see, of the sequences that
 // they belong to; a token of none sees all (its row is not used).
 __device__ inline void common_last(const SharedParams& p, int row0, int rows, int* last)

@@ -922,3 +922,33 @@ def test_tokens_of_a_run_keep_their_own_pages(A, run, page):
             assert (lens[b] - new[b] + i) // page in got[b, i // run, 0]
     out, lse = over_blocks(A, c, q, got, 2, new=new, run=run)
     assert np.isfinite(lse).all()
+
+
+@pytest.mark.parametrize("kind", ["bf16", "e4m3"])
+@pytest.mark.parametrize("d,page", [(64, 64), (64, 128), (128, 64), (128, 128)])
+@pytest.mark.parametrize("pre_rows", [16, 128])
+def test_shared_rows_of_no_sequence_take_no_part(A, pre_rows, d, page, kind):
+    """Rows of q behind the last sequence, and shared pages that lie behind all of them, may hold anything: the
+    result is the same to the last bit."""
+    rng = np.random.default_rng(71 + d + page)
+    shared, W, G = 7, 9, 4
+    lens, new = [5 * page - 3, 4 * page + 9, 4 * page + 30], [9, 1, 7]
+    c = P.share(R.make_cache(rng, 3, 2, page, d, [W * page] * 3), shared)
+    c.lens = np.array(lens, dtype=np.int32)
+    T = next(t for t in (40, 300, 600, 1000, 2000, 4000, 8000, 16000)
+             if P.shared_plan(3, 2, G, t, 9, shared, W * page, page, d, n_cu()).pre.rows == pre_rows)
+    q = np.zeros((T, 2 * G, d))
+    q[:sum(new)] = R.make_queries(rng, sum(new), 2 * G, d)
+    log(f"shared rows of no sequence rows={pre_rows} T={T} d={d} page={page} {kind}")
+    want = over_shared(A, c, q, shared, G, kind, new=new)
+    for pad in (math.inf, math.nan, 448.0):
+        x = q.copy()
+        x[sum(new):, ::2] = pad
+        got = over_shared(A, c, x, shared, G, kind, new=new, check=False)
+        assert np.array_equal(got[0], want[0]) and np.array_equal(got[1], want[1]), pad
+    x = q.copy()
+    x[sum(new):] = 400.0
+    for p in c.pages[0, 5:shared]:
+        c.k[p], c.v[p], c.ks[p], c.vs[p] = 0x7E, 0x7F, 254, 255
+    got = over_shared(A, c, x, shared, G, kind, new=new, check=False)
+    assert np.array_equal(got[0], want[0]) and np.array_equal(got[1], want[1])
