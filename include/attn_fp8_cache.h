@@ -122,8 +122,8 @@ int attn_fp8_cache_append(const attn_fp8_cache *cache, const attn_fp8_batch *bat
  * sums in FP32 relative to a power of two per row (which may lie 2^16 below its
  * largest: sums of values beyond 2^111 / lens[b] may pass FP32's range); lse = ln l.
  * A query that sees no key gets out = 0 and lse = -inf.  The matrix cores add the
- * products of P V in eights and drop what lies 13 bits below the largest of them: 6e-5
- * of the result (relative norm), below a BF16 out's rounding, visible in an F32 one.
+ * products of P V in eights and drop what lies 13 bits below the largest of them: 5e-5
+ * to 1e-4 of the result (relative norm), below a BF16 out's rounding, visible in an F32 one.
  * The rounding of P itself is 1.7e-2 (777 keys) to 3.7e-2 (131001) of the softmax
  * over the same codes.
  *   q          [T][Hq][d], BF16 or E4M3 (F32 and F16 queries are the caller's to

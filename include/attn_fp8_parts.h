@@ -3,7 +3,8 @@
  * are chosen for the queries by bounds on their keys, and pages that the sequences of a batch
  * begin with.  Cache, batch, heads, statuses, alignment and streams are those of
  * attn_fp8_cache.h; a call validates its arguments before any HIP call, enqueues its kernels
- * on `stream`, allocates nothing and keeps nothing between calls.
+ * on `stream`, allocates nothing and keeps nothing between calls.  Outputs and workspaces overlap
+ * none of a call's other arrays.
  *
  * What the definition of attn_fp8_cache_fwd makes of a key does not depend on the other keys
  * but for groups of 32 in a page, so attention over parts of the cache is that of the whole

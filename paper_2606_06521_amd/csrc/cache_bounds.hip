@@ -5,7 +5,7 @@
 // are compared as signed bytes, in the upper halves of 16-bit numbers (a negative code's
 // magnitude is complemented, which orders them), two to an instruction.
 // What bounds it: single tokens the chain of loads (length, page, K) and the launch, 4.1 us for
-// 16 sequences; prompts of 22.6 MB of K (4 x 8 heads, up to 8192 keys, d = 128) 10.2 us, the same
+// 16 sequences; prompts of 22.6 MB of K (4 x 8 heads, up to 8192 keys, d = 128) 9.1 to 10.2 us, the same
 // chain and then 4 us of the stream: all workgroups start at once and each has its whole page on the way.
 #include "cache_common.hpp"
 

@@ -14,7 +14,7 @@
 // 16 keys of two neighbouring lane groups.  So a group's maximum M_g takes one
 // exchange of lanes; 2^(x - M_g) is rounded to E4M3 and M_g - M goes to the matrix
 // core as the operand's scale, V's page scale as the other operand's.  (The core adds
-// products in eights and drops what lies 13 bits below their largest: 6e-5 of the
+// products in eights and drops what lies 13 bits below their largest: 5e-5 to 1e-4 of the
 // result, where a code is rounded at 2^-4; bf16 products run at half its rate.)  No
 // accumulator is rescaled as long as the row's reference M, taken at its first
 // keys, holds within 2^kSlack.  So the waves need no barrier until they add up

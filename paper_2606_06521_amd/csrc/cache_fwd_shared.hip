@@ -7,7 +7,7 @@
 //
 // Measured at d = 128, 32/8 heads: single tokens of 32 sequences behind 16384 common keys and up to 1024 of their own
 // 28.7 us (72 MB read; 23 for both kinds of tile in one launch, 6 for the merge); chunks of up to 192
-// tokens of 8 such sequences 208 to 211 us, 1.09 PFLOP/s (196 in the tiles, 13 for the merge, which
+// tokens of 8 such sequences 206 to 214 us, 1.06 to 1.11 PFLOP/s (196 in the tiles, 13 for the merge, which
 // reads 44 MB).
 #include "cache_merge.hpp"
 

@@ -19,9 +19,11 @@
 // the choice, 6.0 us for 4 sequences of 777 keys; 8.4 for 16 x 8 heads x 256 pages of 128 channels
 // (8.4 MB of bounds; pairwise ranks in the place of the histograms 11.3).  Few lists of many pages are scored by several
 // workgroups a list and chosen by a second launch: 8 lists x 2047 pages 11.0 us, by one workgroup
-// a list 32.3.  A chunk (64 runs of 32 tokens x 4 heads on 128 pages, 8 heads) 13.5 us: 3 for q at
-// the rate of memory, 1.2 to round it, 1.6 for the choice (26.4 with bounds
-// loaded by the lanes that multiply them, which reads every line 8 times).
+// a list 32.3.  A chunk (64 runs of 32 tokens x 4 heads on 128 pages, 8 heads) 13.5 us (26.4 with bounds
+// loaded by the lanes that multiply them, which reads every line 8 times), in phases: of a wave's 25 thousand
+// cycles the vector unit, which two waves share, is busy for 49 %, the matrix core for 16 %, LDS for 10 %, and
+// a wave waits for 34 %; q (16.8 MB, 3 us at the rate of memory) comes from HBM once, by lanes that
+// read each line eight times.
 #include "cache_common.hpp"
 
 #include <algorithm>
@@ -497,7 +499,8 @@ __global__ void __launch_bounds__(64 * NW) select_kernel(SelectParams p, int pag
                         best = fmax_f(best, __shfl_xor(best, 16, 64));
                     if (h == 0 && byte >= 0 && block < nb) {
                         const uint32_t k = key_of(best);
-                        if (by_rows < row_tiles || by_rows > 1)
+                        // (a single tile of rows: one wave has the page, once)
+                        if (by_rows > 1)
                             atomicMax(&key[block], k);
                         else
                             key[block] = k;
