@@ -440,18 +440,19 @@ PyObject* select(PyObject*, PyObject* const* a, Py_ssize_t n)
         value_error("take is at least 1");
     const void* bounds = bounds_of(a[4], s.c, s.at);
     const std::array<int64_t, 4> full = {shape[0], shape[1], shape[2], take};
+    const int max_len = int_arg(a[12], "max_len");
+    // (the sizes are the library's to refuse, before lists of them are allocated)
+    size_t bytes = 0;
+    int st = attn_fp8_cache_select_workspace_bytes(&s.c, &s.bt, (int)s.Hq, take, run, max_len, &bytes);
+    if (st)
+        return PyLong_FromLong(st);
     const at::Tensor lists = a[13] == Py_None ? s.at.empty(full, at::kInt) : tensor(a[13], "blocks");
     int32_t* blocks = dense<int32_t>(lists, "blocks", s.at, at::kInt, full);
-    const int max_len = int_arg(a[12], "max_len");
-    size_t bytes = 0;
     at::Tensor ws;
-    int st = attn_fp8_cache_select_workspace_bytes(&s.c, &s.bt, (int)s.Hq, take, run, max_len, &bytes);
-    if (!st) {
-        if (bytes)
-            ws = s.at.empty({(int64_t)bytes}, at::kByte);
-        st = attn_fp8_cache_select(&s.c, &s.bt, &s.hq, (int)s.Hq, bounds, blocks, take, run, int_arg(a[9], "n_first"),
-                                   int_arg(a[10], "n_last"), truth(a[11]), max_len, bytes ? ws.data_ptr() : nullptr, bytes, s.at.stream);
-    }
+    if (bytes)
+        ws = s.at.empty({(int64_t)bytes}, at::kByte);
+    st = attn_fp8_cache_select(&s.c, &s.bt, &s.hq, (int)s.Hq, bounds, blocks, take, run, int_arg(a[9], "n_first"),
+                               int_arg(a[10], "n_last"), truth(a[11]), max_len, bytes ? ws.data_ptr() : nullptr, bytes, s.at.stream);
     return st ? PyLong_FromLong(st) : wrap(lists);
     END_HANDLE_TH_ERRORS
 }

@@ -952,3 +952,20 @@ def test_shared_rows_of_no_sequence_take_no_part(A, pre_rows, d, page, kind):
         c.k[p], c.v[p], c.ks[p], c.vs[p] = 0x7E, 0x7F, 254, 255
     got = over_shared(A, c, x, shared, G, kind, new=new, check=False)
     assert np.array_equal(got[0], want[0]) and np.array_equal(got[1], want[1])
+
+
+def test_select_refuses_sizes_before_it_allocates(A):
+    """A list of more pages than the call takes is refused by its size, not by the memory that it would need."""
+    c = A.kv_cache(3, 8, 64, page=64)
+    pages = torch.zeros((64, 4), dtype=torch.int32, device="cuda")
+    lens = torch.full((64,), 200, dtype=torch.int32, device="cuda")
+    q = torch.zeros((64, 8, 64), dtype=torch.bfloat16, device="cuda")
+    b = A.key_bounds(3, 8, 64)
+    torch.cuda.synchronize()
+    torch.cuda.reset_peak_memory_stats()
+    before = torch.cuda.max_memory_allocated()
+    for take in (16385, 1 << 18, (1 << 31) - 1):
+        log(f"refused take={take}")
+        with pytest.raises(A.AttnError):
+            A.cache_select(q, c, pages, lens, b, take)
+    assert torch.cuda.max_memory_allocated() == before
